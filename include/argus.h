@@ -100,9 +100,11 @@ enum {
                                       listing counts) */
   ARGUS_DEV_L2_DOMAIN = 64,        /* argus_l2: a mean duration at or above 2^40 ns (that cell is left out) */
   ARGUS_DEV_COMPACT_CAPACITY = 128, /* argus_compact: the records did not all fit in the caller's buffer */
-  ARGUS_DEV_SUMMARY_STALLED = 256   /* argus_summarize: a bounded wait inside the kernel expired in every one of
+  ARGUS_DEV_SUMMARY_STALLED = 256,  /* argus_summarize: a bounded wait inside the kernel expired in every one of
                                        its redo passes over some segment (never expected: it means a defect in
                                        the library or the device); that segment's cells may be incomplete */
+  ARGUS_DEV_TOKEN_RANGE = 512,     /* argus_embedding: a token id at or above n_vocab (taken as padding) */
+  ARGUS_DEV_LOGITS = 1024          /* argus_balance: a token with a NaN logit or no finite largest one (left out) */
 };
 
 int argus_abi_version(void);

@@ -7,7 +7,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libargus.so")
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ["api.hip", "summarize.hip", "cross_rank.hip", "iter_windows.hip", "kde.hip", "w1.hip", "l2.hip", "compact.hip"]
+SOURCES = ["api.hip", "summarize.hip", "cross_rank.hip", "iter_windows.hip", "kde.hip", "w1.hip", "l2.hip", "compact.hip",
+           "ops_api.hip", "embedding.hip", "layer_norm.hip", "balance.hip", "attention.hip", "attention_bwd.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HIP_FLAGS = [
@@ -27,7 +28,7 @@ def _compile(src: str) -> str:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, SOURCES))
     tmp = LIB + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]

@@ -13,25 +13,6 @@ __global__ void clear_kernel(int32_t* status, uint32_t* queue) {
   if (queue) *queue = 0;
 }
 
-// Per-device cache of "is gfx950": 0 unknown, 1 yes, 2 no.
-std::atomic<int> g_arch_ok[64];
-
-int check_device() {
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return ARGUS_EHIP;
-  if (dev < 0 || dev >= 64) return ARGUS_EUNSUPPORTED;
-  int v = g_arch_ok[dev].load(std::memory_order_relaxed);
-  if (v == 0) {
-    hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return ARGUS_EHIP;
-    v = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : 2;
-    g_arch_ok[dev].store(v, std::memory_order_relaxed);
-  }
-  return v == 1 ? ARGUS_OK : ARGUS_EUNSUPPORTED;
-}
-
-int status_of(hipError_t e) { return e == hipSuccess ? ARGUS_OK : ARGUS_EHIP; }
-
 // Scratch of argus_summarize_noalloc: the work-queue counter of the
 // persistent summarize kernel, in device memory that the library never
 // allocates. Each device holds its own copy until the process ends; in host
@@ -57,6 +38,23 @@ int scratch_of_current_device(void** ptr) {
 }
 
 }  // namespace
+
+// Per-device cache of "is gfx950": 0 unknown, 1 yes, 2 no.
+static std::atomic<int> g_arch_ok[64];
+
+int check_device() {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return ARGUS_EHIP;
+  if (dev < 0 || dev >= 64) return ARGUS_EUNSUPPORTED;
+  int v = g_arch_ok[dev].load(std::memory_order_relaxed);
+  if (v == 0) {
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return ARGUS_EHIP;
+    v = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : 2;
+    g_arch_ok[dev].store(v, std::memory_order_relaxed);
+  }
+  return v == 1 ? ARGUS_OK : ARGUS_EUNSUPPORTED;
+}
 
 hipError_t launch_clear(int32_t* dev_status, uint32_t* queue, hipStream_t st) {
   if (!dev_status && !queue) return hipSuccess;

@@ -194,6 +194,11 @@ hipError_t launch_compact(const CompactLaunch& a, hipStream_t st);
 // Zero the optional device status word and the optional queue counter.
 hipError_t launch_clear(int32_t* dev_status, uint32_t* queue, hipStream_t st);
 
+// Host side of every entry point: the current device is a gfx950 (ARGUS_OK),
+// and the status of a launch.
+int check_device();
+inline int status_of(hipError_t e) { return e == hipSuccess ? ARGUS_OK : ARGUS_EHIP; }
+
 constexpr size_t kSummarizeWorkspace = 256;
 
 }  // namespace argus

@@ -1,0 +1,256 @@
+// Softmax attention over packed documents, forward.
+//
+// S^T = K Q^T per tile of keys, with the running maximum and sum of each
+// query, and O^T += V^T P^T. The transposed products keep a query in one lane
+// (two lanes, one to each half of a tile's keys), so its maximum, sum and
+// rescaling are plain registers, and P^T is the second product's operand as it
+// comes out of the first.
+#include "attention_tile.h"
+
+#pragma clang fp contract(fast)
+
+namespace argus {
+using namespace attn;
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kKeys = 64;  // keys of a tile
+
+struct FwdArgs {
+  Docs d;
+  const __bf16 *q, *k, *v;
+  __bf16* o;
+  float* lse;
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;
+  int32_t H, N, D, causal, slots;
+  float scale;
+};
+
+// One workgroup checks the offsets and sets the status word.
+__global__ __launch_bounds__(256) void attn_check(Docs d, uint32_t* bad, int32_t* dev_status) {
+  __shared__ int any;
+  if (threadIdx.x == 0) any = d.q_off[0] != 0 || d.k_off[0] != 0 || d.q_off[d.n_docs] != d.n_q ||
+                              d.k_off[d.n_docs] != d.n_k;
+  __syncthreads();
+  bool b = false;
+  for (int i = threadIdx.x; i < d.n_docs; i += 256) b |= d.q_off[i] > d.q_off[i + 1] || d.k_off[i] > d.k_off[i + 1];
+  if (b) any = 1;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    *bad = any;
+    if (dev_status) *dev_status = any ? (int32_t)ARGUS_DEV_BAD_SEGMENT : 0;
+  }
+}
+
+// Malformed offsets: every query sees no key.
+__device__ void fill_empty(const FwdArgs& a) {
+  const int64_t n = a.d.n_q * a.H;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+    a.lse[i] = -__builtin_inff();
+    for (int j = 0; j < a.D; ++j) a.o[i * a.D + j] = (__bf16)0.0f;
+  }
+}
+
+template <int DP, int NQ>
+__global__ __launch_bounds__(kThreads) void attn_fwd(FwdArgs a) {
+  constexpr int kRows = 4 * 32 * NQ;  // queries of a workgroup
+  constexpr int KS = DP / 16, DT = DP / 32;
+  __shared__ __align__(16) __bf16 kt[2][kKeys * DP];
+  __shared__ __align__(16) __bf16 vt[2][kKeys * DP];
+  if (a.d.bad && *a.d.bad) return fill_empty(a);
+  const int item = (int)xcd_item(blockIdx.x, gridDim.x);
+  const int G = a.H / a.N, per = a.slots * G, n = item / per, rest = item % per;
+  const int h = n * G + rest % G, slot = a.slots - 1 - rest / G;  // later tiles see more keys: first
+  int row0;
+  const int di = slot_doc(a.d.q_off, a.d.n_docs, kRows, slot, row0);
+  const Doc doc = doc_at(a.d, di);
+  if (row0 >= doc.nq) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
+  const int q0 = row0 + w * 32 * NQ;  // the wavefront's first query
+  const int shift = doc.nk - doc.nq;  // query i sees keys up to i + shift
+  const float sc = score_scale(a.scale);
+
+  bf16x8 qf[NQ][KS];
+  {
+    const __bf16* qb = a.q + (doc.q0 + row0) * a.q_tok + (int64_t)h * a.q_head;
+    const auto r = rows_rsrc(qb, doc.nq - row0, a.q_tok, a.D);
+#pragma unroll
+    for (int u = 0; u < NQ; ++u)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int c = 16 * ks + 8 * half, row = w * 32 * NQ + u * 32 + (lane & 31);
+        const int off = c < a.D ? (int)(((int64_t)row * a.q_tok + c) * 2) : 0x7ffffff0;
+        qf[u][ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+      }
+  }
+  f32x16 acc[NQ][DT];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int u = 0; u < NQ; ++u) {
+    m[u] = -__builtin_inff();
+    l[u] = 0;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[u][t][i] = 0;
+  }
+  // keys that some query of the workgroup sees
+  int last_row = row0 + kRows - 1 < doc.nq - 1 ? row0 + kRows - 1 : doc.nq - 1;
+  int64_t seen = a.causal ? (int64_t)last_row + shift + 1 : doc.nk;
+  const int nk = seen < 0 ? 0 : seen < doc.nk ? (int)seen : doc.nk;
+  const int tiles = (nk + kKeys - 1) / kKeys;
+  const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
+  const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
+  Stage<DP, kKeys, kThreads> sk, sv;
+  auto load = [&](int t) {
+    const int64_t first = (int64_t)t * kKeys;
+    sk.load(rows_rsrc(kb + first * a.k_tok, doc.nk - first, a.k_tok, a.D), 0, a.k_tok, a.D);
+    sv.load(rows_rsrc(vb + first * a.v_tok, doc.nk - first, a.v_tok, a.D), 0, a.v_tok, a.D);
+  };
+  if (tiles > 0) {
+    load(0);
+    sk.store(kt[0]);
+    sv.store(vt[0]);
+  }
+  __syncthreads();
+  for (int t = 0; t < tiles; ++t) {
+    const int cur = t & 1;
+    if (t + 1 < tiles) load(t + 1);
+    const __bf16 *K = kt[cur], *V = vt[cur];
+    const int key0 = t * kKeys;
+    f32x16 s[NQ][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int u = 0; u < NQ; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[u][b][i] = 0;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 ka = read_rows<DP>(K, 32 * b, ks);
+#pragma unroll
+        for (int u = 0; u < NQ; ++u) s[u][b] = mfma(ka, qf[u][ks], s[u][b]);
+      }
+    }
+    // the tiles at the causal edge and at the document's end
+    const bool edge = key0 + kKeys > doc.nk || (a.causal && (int64_t)key0 + kKeys - 1 > (int64_t)q0 + shift);
+    if (edge) {
+#pragma unroll
+      for (int u = 0; u < NQ; ++u) {
+        const int64_t q = q0 + u * 32 + (lane & 31);
+        int64_t lim = a.causal ? q + shift : doc.nk - 1;
+        if (lim > doc.nk - 1) lim = doc.nk - 1;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
+            s[u][b][i] = key <= lim ? s[u][b][i] : -__builtin_inff();
+          }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < NQ; ++u) {
+      float mx = s[u][0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][b][i]);
+      mx = fmaxf(mx, other_half(mx)) * sc;
+      // The sums are kept against an earlier maximum until it is passed by
+      // 2^8: the probabilities then stay below 2^8, which 32 bits and a
+      // bfloat16 operand hold as exactly as those below 1.
+      const float mn = fmaxf(m[u], mx);
+      if (__ballot(mn > m[u] + 8.0f)) {
+        const float al = exp2_fast(m[u] - (mn > -__builtin_inff() ? mn : 0.0f));
+        m[u] = mn;
+        l[u] *= al;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[u][d][i] *= al;
+      }
+      const float mm = m[u] > -__builtin_inff() ? m[u] : 0.0f;
+      float sum = 0;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float p = exp2_fast(s[u][b][i] * sc - mm);
+          s[u][b][i] = p;
+          sum += p;
+        }
+      l[u] += sum;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        bf16x8 p[NQ];
+#pragma unroll
+        for (int u = 0; u < NQ; ++u) p[u] = as_operand(s[u][b], k2);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const bf16x8 va = read_cols<DP>(V, 32 * b + 16 * k2, 32 * d);
+#pragma unroll
+          for (int u = 0; u < NQ; ++u) acc[u][d] = mfma(va, p[u], acc[u][d]);
+        }
+      }
+    if (t + 1 < tiles) {
+      sk.store(kt[cur ^ 1]);
+      sv.store(vt[cur ^ 1]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int u = 0; u < NQ; ++u) {
+    const float z = l[u] + other_half(l[u]);
+    const int q = q0 + u * 32 + (lane & 31);
+    if (q >= doc.nq) continue;
+    const int64_t row = (doc.q0 + q) * a.H + h;
+    const float rz = z > 0 ? 1.0f / z : z == 0 ? 0.0f : z;  // NaN stays
+    if (half == 0) a.lse[row] = z == 0 ? -__builtin_inff() : m[u] * kLn2 + __logf(z);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int at = 32 * d + 2 * i + 4 * half;
+        bf16x4 o4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o4[j] = (__bf16)(acc[u][d][i + j] * rz);
+        if (at < a.D) *(bf16x4*)(a.o + row * a.D + at) = o4;
+      }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attn_check(const argus_attention_t& p, uint32_t* bad, hipStream_t st) {
+  if (!p.q_off) return launch_clear(p.dev_status, nullptr, st);
+  Docs d{p.q_off, p.k_off, p.n_docs, p.n_q, p.n_k, nullptr};
+  hipLaunchKernelGGL(attn_check, dim3(1), dim3(256), 0, st, d, bad, p.dev_status);
+  return hipGetLastError();
+}
+
+size_t attention_workspace_bytes(const argus_attention_t&) { return 256; }
+
+hipError_t launch_attention(const argus_attention_t& p, const void* q, const void* k, const void* v, void* o,
+                            float* lse, void* ws, hipStream_t st) {
+  const hipError_t e = launch_attn_check(p, (uint32_t*)ws, st);
+  if (e != hipSuccess || p.n_q == 0) return e;
+  constexpr int NQ = 1, kRows = 128 * NQ;
+  const int64_t slots = p.q_off ? slots_of(p.n_q, kRows, p.n_docs) : ceil_div(p.n_q, kRows);
+  FwdArgs a{{p.q_off, p.k_off, p.n_docs, p.n_q, p.n_k, p.q_off ? (const uint32_t*)ws : nullptr},
+            (const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (__bf16*)o, lse,
+            p.q_tok, p.q_head, p.k_tok, p.k_head, p.v_tok, p.v_head,
+            p.n_heads, p.n_kv_heads, p.head_dim, p.causal, (int32_t)slots, p.scale};
+  const int64_t grid = slots * p.n_heads;
+  if (grid > (1 << 23)) return hipErrorInvalidConfiguration;
+  auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+    return hipGetLastError();
+  };
+  return p.head_dim <= 64 ? go(attn_fwd<64, NQ>) : go(attn_fwd<128, NQ>);
+}
+
+}  // namespace argus

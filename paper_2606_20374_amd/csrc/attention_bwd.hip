@@ -1,0 +1,336 @@
+// Softmax attention over packed documents, backward.
+//
+//   P = exp(S - lse),  dP = dO V^T,  dS = P (dP - delta),  delta = dO . O
+//   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
+// The probabilities are recomputed from q, k and lse. Three launches:
+//   prep   delta and lse (in units of log2) per head and query; offsets check
+//   dkv    a workgroup owns 128 keys of a key head, 32 to a wavefront, with K
+//          and V as operands in registers, and takes the queries of all its
+//          query heads through LDS. S = Q K^T keeps a key in one lane, so P
+//          and dS are the operands of dV^T += dO^T P and dK^T += Q^T dS as
+//          they are.
+//   dq     a workgroup owns 128 queries and takes the keys through LDS:
+//          S^T = K Q^T keeps a query in one lane, dQ^T += K^T dS^T.
+// S and dP are computed in both: 7 products in place of 5, and no sum between
+// workgroups, so no atomics and a fixed order.
+#include "attention_tile.h"
+
+#pragma clang fp contract(fast)
+
+namespace argus {
+using namespace attn;
+
+hipError_t launch_attn_check(const argus_attention_t& p, uint32_t* bad, hipStream_t st);
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kOwn = 128;   // rows a workgroup owns
+constexpr int kStep = 64;   // rows of the other side taken at a time
+
+struct BwdArgs {
+  Docs d;
+  const __bf16 *q, *k, *v, *o, *go;
+  const float* lse;
+  __bf16 *dq, *dk, *dv;
+  float* delta;  // [H][n_q]
+  float* lse2;   // [H][n_q]
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;
+  int32_t H, N, D, causal, slots;
+  float scale;
+};
+
+// A query and head to sixteen lanes.
+__global__ __launch_bounds__(256) void attn_prep(BwdArgs a) {
+  const int lane = threadIdx.x & 15;
+  const int64_t n = a.d.n_q * a.H;
+  for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < n; i += (int64_t)gridDim.x * 16) {
+    float s = 0;
+    const int c = lane * 8;
+    if (c < a.D) {
+      const bf16x8 x = *(const bf16x8*)(a.go + i * a.D + c), y = *(const bf16x8*)(a.o + i * a.D + c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += (float)x[j] * (float)y[j];
+    }
+    s = row_sum(s);
+    if (lane == 0) {
+      const int64_t t = i / a.H, at = (i - t * a.H) * a.d.n_q + t;
+      const float l = a.lse[i];
+      a.delta[at] = s;
+      // a query that sees nothing: exp2(s - infinity) = 0 for every key
+      a.lse2[at] = l > -__builtin_inff() ? l * kLog2e : __builtin_inff();
+    }
+  }
+}
+
+// Zeros for n rows of dim elements, spread over the grid.
+__device__ void fill_zero(__bf16* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads)
+    p[i] = (__bf16)0.0f;
+}
+
+template <int DP>
+__device__ __forceinline__ void load_operand(bf16x8 (&f)[DP / 16], __amdgpu_buffer_rsrc_t r, int row, int64_t stride,
+                                             int dim) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) {
+    const int c = 16 * ks + 8 * half;
+    const int off = c < dim ? (int)(((int64_t)row * stride + c) * 2) : 0x7ffffff0;
+    f[ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+  }
+}
+
+template <int DP>
+__device__ __forceinline__ void clear(f32x16 (&x)[DP / 32]) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[d][i] = 0;
+}
+
+// Writes a transposed accumulator: lane = row, registers = columns.
+template <int DP>
+__device__ __forceinline__ void write_rows(__bf16* row, const f32x16 (&x)[DP / 32], float f, int dim) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int at = 32 * d + 2 * i + 4 * half;
+      bf16x4 o4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o4[j] = (__bf16)(x[d][i + j] * f);
+      if (at < dim) *(bf16x4*)(row + at) = o4;
+    }
+}
+
+template <int DP>
+__global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
+  constexpr int KS = DP / 16, DT = DP / 32;
+  __shared__ __align__(16) __bf16 qt[2][kStep * DP];
+  __shared__ __align__(16) __bf16 gt[2][kStep * DP];
+  __shared__ __align__(16) float ls[2][kStep], ds[2][kStep];
+  if (a.d.bad && *a.d.bad) {
+    fill_zero(a.dk, a.d.n_k * a.N * a.D);
+    fill_zero(a.dv, a.d.n_k * a.N * a.D);
+    return;
+  }
+  const int item = (int)xcd_item(blockIdx.x, gridDim.x), n = item / a.slots, slot = item % a.slots, G = a.H / a.N;
+  int row0;
+  const int di = slot_doc(a.d.k_off, a.d.n_docs, kOwn, slot, row0);
+  const Doc doc = doc_at(a.d, di);
+  if (row0 >= doc.nk) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
+  const int shift = doc.nk - doc.nq, key0 = row0 + w * 32, key = key0 + (lane & 31);
+  const float sc = score_scale(a.scale);
+  bf16x8 kf[KS], vf[KS];
+  load_operand<DP>(kf, rows_rsrc(a.k + (doc.k0 + row0) * a.k_tok + (int64_t)n * a.k_head, doc.nk - row0, a.k_tok, a.D),
+                   w * 32 + (lane & 31), a.k_tok, a.D);
+  load_operand<DP>(vf, rows_rsrc(a.v + (doc.k0 + row0) * a.v_tok + (int64_t)n * a.v_head, doc.nk - row0, a.v_tok, a.D),
+                   w * 32 + (lane & 31), a.v_tok, a.D);
+  f32x16 dk[DT], dv[DT];
+  clear<DP>(dk);
+  clear<DP>(dv);
+  // queries from the first that sees a key of the workgroup on
+  int first = 0;
+  if (a.causal && row0 > shift) first = (row0 - shift) / kStep * kStep;
+  const int per = first < doc.nq ? (doc.nq - first + kStep - 1) / kStep : 0, tiles = per * G;
+  Stage<DP, kStep, kThreads> sq, sg;
+  float stat = 0;
+  const int64_t o_tok = (int64_t)a.H * a.D;
+  auto load = [&](int t) {
+    const int h = n * G + t / per, q0 = first + t % per * kStep;
+    sq.load(rows_rsrc(a.q + (doc.q0 + q0) * a.q_tok + (int64_t)h * a.q_head, doc.nq - q0, a.q_tok, a.D), 0, a.q_tok, a.D);
+    sg.load(rows_rsrc(a.go + (doc.q0 + q0) * o_tok + (int64_t)h * a.D, doc.nq - q0, o_tok, a.D), 0, o_tok, a.D);
+    if (threadIdx.x < 2 * kStep) {
+      const int i = threadIdx.x & (kStep - 1);
+      const bool is_lse = threadIdx.x < kStep;
+      stat = is_lse ? __builtin_inff() : 0.0f;
+      if (q0 + i < doc.nq) stat = (is_lse ? a.lse2 : a.delta)[(int64_t)h * a.d.n_q + doc.q0 + q0 + i];
+    }
+  };
+  auto put = [&](int b) {
+    sq.store(qt[b]);
+    sg.store(gt[b]);
+    if (threadIdx.x < kStep) ls[b][threadIdx.x] = stat;
+    else if (threadIdx.x < 2 * kStep) ds[b][threadIdx.x - kStep] = stat;
+  };
+  if (tiles > 0) {
+    load(0);
+    put(0);
+  }
+  __syncthreads();
+  for (int t = 0; t < tiles; ++t) {
+    const int cur = t & 1, q0 = first + t % per * kStep;
+    if (t + 1 < tiles) load(t + 1);
+#pragma unroll
+    for (int b = 0; b < kStep / 32; ++b) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mfma(read_rows<DP>(qt[cur], 32 * b, ks), kf[ks], s);
+        dp = mfma(read_rows<DP>(gt[cur], 32 * b, ks), vf[ks], dp);
+      }
+      const bool edge = key0 + 32 > doc.nk || (a.causal && (int64_t)key0 + 31 > (int64_t)q0 + 32 * b + shift);
+#pragma unroll
+      for (int i4 = 0; i4 < 16; i4 += 4) {
+        const int r = 32 * b + 2 * i4 + 4 * half;
+        const float4 l4 = *(const float4*)&ls[cur][r], d4 = *(const float4*)&ds[cur][r];
+        const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = exp2_fast(s[i4 + j] * sc - lv[j]);
+          s[i4 + j] = p;
+          dp[i4 + j] = p * (dp[i4 + j] - dl[j]);
+          if (edge) {
+            const bool see = key < doc.nk && (!a.causal || (int64_t)key <= (int64_t)q0 + r + j + shift);
+            s[i4 + j] = see ? s[i4 + j] : 0.0f;
+            dp[i4 + j] = see ? dp[i4 + j] : 0.0f;
+          }
+        }
+      }
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        const bf16x8 p = as_operand(s, k2), d = as_operand(dp, k2);
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+          dv[c] = mfma(read_cols<DP>(gt[cur], 32 * b + 16 * k2, 32 * c), p, dv[c]);
+          dk[c] = mfma(read_cols<DP>(qt[cur], 32 * b + 16 * k2, 32 * c), d, dk[c]);
+        }
+      }
+    }
+    if (t + 1 < tiles) put(cur ^ 1);
+    __syncthreads();
+  }
+  if (key < doc.nk) {
+    const int64_t row = ((doc.k0 + key) * a.N + n) * a.D;
+    write_rows<DP>(a.dk + row, dk, a.scale, a.D);
+    write_rows<DP>(a.dv + row, dv, 1.0f, a.D);
+  }
+}
+
+template <int DP>
+__global__ __launch_bounds__(kThreads) void attn_dq(BwdArgs a) {
+  constexpr int KS = DP / 16, DT = DP / 32;
+  __shared__ __align__(16) __bf16 kt[2][kStep * DP];
+  __shared__ __align__(16) __bf16 vt[2][kStep * DP];
+  if (a.d.bad && *a.d.bad) return fill_zero(a.dq, a.d.n_q * a.H * a.D);
+  const int item = (int)xcd_item(blockIdx.x, gridDim.x);
+  const int G = a.H / a.N, per = a.slots * G, n = item / per, rest = item % per;
+  const int h = n * G + rest % G, slot = a.slots - 1 - rest / G;
+  int row0;
+  const int di = slot_doc(a.d.q_off, a.d.n_docs, kOwn, slot, row0);
+  const Doc doc = doc_at(a.d, di);
+  if (row0 >= doc.nq) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
+  const int q0 = row0 + w * 32, q = q0 + (lane & 31), shift = doc.nk - doc.nq;
+  const float sc = score_scale(a.scale);
+  const int64_t o_tok = (int64_t)a.H * a.D;
+  bf16x8 qf[KS], gf[KS];
+  load_operand<DP>(qf, rows_rsrc(a.q + (doc.q0 + row0) * a.q_tok + (int64_t)h * a.q_head, doc.nq - row0, a.q_tok, a.D),
+                   w * 32 + (lane & 31), a.q_tok, a.D);
+  load_operand<DP>(gf, rows_rsrc(a.go + (doc.q0 + row0) * o_tok + (int64_t)h * a.D, doc.nq - row0, o_tok, a.D),
+                   w * 32 + (lane & 31), o_tok, a.D);
+  float lse2 = __builtin_inff(), delta = 0;
+  if (q < doc.nq) {
+    lse2 = a.lse2[(int64_t)h * a.d.n_q + doc.q0 + q];
+    delta = a.delta[(int64_t)h * a.d.n_q + doc.q0 + q];
+  }
+  f32x16 acc[DT];
+  clear<DP>(acc);
+  const int last_row = row0 + kOwn - 1 < doc.nq - 1 ? row0 + kOwn - 1 : doc.nq - 1;
+  const int64_t seen = a.causal ? (int64_t)last_row + shift + 1 : doc.nk;
+  const int nk = seen < 0 ? 0 : seen < doc.nk ? (int)seen : doc.nk, tiles = (nk + kStep - 1) / kStep;
+  const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
+  const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
+  Stage<DP, kStep, kThreads> sk, sv;
+  auto load = [&](int t) {
+    const int64_t f = (int64_t)t * kStep;
+    sk.load(rows_rsrc(kb + f * a.k_tok, doc.nk - f, a.k_tok, a.D), 0, a.k_tok, a.D);
+    sv.load(rows_rsrc(vb + f * a.v_tok, doc.nk - f, a.v_tok, a.D), 0, a.v_tok, a.D);
+  };
+  if (tiles > 0) {
+    load(0);
+    sk.store(kt[0]);
+    sv.store(vt[0]);
+  }
+  __syncthreads();
+  int64_t lim = a.causal ? (int64_t)q + shift : doc.nk - 1;
+  if (lim > doc.nk - 1) lim = doc.nk - 1;
+  for (int t = 0; t < tiles; ++t) {
+    const int cur = t & 1, key0 = t * kStep;
+    if (t + 1 < tiles) load(t + 1);
+#pragma unroll
+    for (int b = 0; b < kStep / 32; ++b) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mfma(read_rows<DP>(kt[cur], 32 * b, ks), qf[ks], s);
+        dp = mfma(read_rows<DP>(vt[cur], 32 * b, ks), gf[ks], dp);
+      }
+      const bool edge = key0 + 32 * b + 32 > doc.nk || (a.causal && (int64_t)key0 + 32 * b + 31 > (int64_t)q0 + shift);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        dp[i] = exp2_fast(s[i] * sc - lse2) * (dp[i] - delta);
+        if (edge) dp[i] = key0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4 <= lim ? dp[i] : 0.0f;
+      }
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        const bf16x8 d = as_operand(dp, k2);
+#pragma unroll
+        for (int c = 0; c < DT; ++c) acc[c] = mfma(read_cols<DP>(kt[cur], 32 * b + 16 * k2, 32 * c), d, acc[c]);
+      }
+    }
+    if (t + 1 < tiles) {
+      sk.store(kt[cur ^ 1]);
+      sv.store(vt[cur ^ 1]);
+    }
+    __syncthreads();
+  }
+  if (q < doc.nq) write_rows<DP>(a.dq + ((doc.q0 + q) * a.H + h) * a.D, acc, a.scale, a.D);
+}
+
+}  // namespace
+
+size_t attention_bwd_workspace_bytes(const argus_attention_t& p) {
+  return 256 + 2 * align256((size_t)p.n_q * (size_t)p.n_heads * sizeof(float));
+}
+
+hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, const void* q, const void* k,
+                                const void* v, const void* o, const float* lse, void* dq, void* dk, void* dv,
+                                void* ws, hipStream_t st) {
+  hipError_t e = launch_attn_check(p, (uint32_t*)ws, st);
+  if (e != hipSuccess) return e;
+  const size_t part = align256((size_t)p.n_q * (size_t)p.n_heads * sizeof(float));
+  float* delta = (float*)((uint8_t*)ws + 256);
+  float* lse2 = (float*)((uint8_t*)ws + 256 + part);
+  BwdArgs a{{p.q_off, p.k_off, p.n_docs, p.n_q, p.n_k, p.q_off ? (const uint32_t*)ws : nullptr},
+            (const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (const __bf16*)o, (const __bf16*)d_o, lse,
+            (__bf16*)dq, (__bf16*)dk, (__bf16*)dv, delta, lse2,
+            p.q_tok, p.q_head, p.k_tok, p.k_head, p.v_tok, p.v_head,
+            p.n_heads, p.n_kv_heads, p.head_dim, p.causal, 0, p.scale};
+  const bool wide = p.head_dim > 64;
+  if (p.n_q > 0) {
+    const int64_t need = ceil_div(p.n_q * p.n_heads, 16), grid = need < 8192 ? need : 8192;
+    hipLaunchKernelGGL(attn_prep, dim3((unsigned)grid), dim3(256), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  auto go = [&](auto kern, int64_t tokens, int64_t heads) {
+    if (tokens == 0) return hipSuccess;
+    const int64_t slots = p.q_off ? slots_of(tokens, kOwn, p.n_docs) : ceil_div(tokens, kOwn);
+    if (slots * heads > (1 << 23)) return hipErrorInvalidConfiguration;
+    a.slots = (int32_t)slots;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(slots * heads)), dim3(kThreads), 0, st, a);
+    return hipGetLastError();
+  };
+  e = wide ? go(attn_dkv<128>, p.n_k, p.n_kv_heads) : go(attn_dkv<64>, p.n_k, p.n_kv_heads);
+  if (e != hipSuccess) return e;
+  return wide ? go(attn_dq<128>, p.n_q, p.n_heads) : go(attn_dq<64>, p.n_q, p.n_heads);
+}
+
+}  // namespace argus

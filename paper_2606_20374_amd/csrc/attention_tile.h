@@ -1,0 +1,159 @@
+// Tiles of the attention kernels: documents, rows in LDS, matrix operands.
+//
+// All products are v_mfma_f32_32x32x16_bf16. Its lanes are 32 columns in two
+// halves h = lane / 32; with column c = lane % 32 and j = 0 .. 7,
+//   A holds A[row c][k = 8 h + j], B holds B[k = 8 h + j][column c], and of
+//   the result a lane holds rows 8 (i / 4) + 4 h + i % 4, i = 0 .. 15, of
+//   column c.
+// A result whose rows are the next product's k needs no exchange between
+// lanes: registers 8 t .. 8 t + 7 are taken as the B operand of k-step t, and
+// the A operand is read with the same order of k, which is rows
+// 16 t + 4 h + (0 .. 3) and 16 t + 8 + 4 h + (0 .. 3). A row-major tile gives
+// such an operand, transposed, by two ds_read_b64_tr_b16.
+#pragma once
+
+#include "ops_internal.h"
+
+namespace argus {
+namespace attn {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Documents and the workspace's flag (1: the offsets are malformed).
+struct Docs {
+  const int64_t *q_off, *k_off;
+  int32_t n_docs;
+  int64_t n_q, n_k;
+  const uint32_t* bad;
+};
+struct Doc {
+  int64_t q0, k0;
+  int32_t nq, nk;
+};
+
+__device__ __forceinline__ Doc doc_at(const Docs& d, int i) {
+  if (!d.q_off) return {0, 0, (int32_t)d.n_q, (int32_t)d.n_k};
+  const int64_t q0 = d.q_off[i], k0 = d.k_off[i];
+  return {q0, k0, (int32_t)(d.q_off[i + 1] - q0), (int32_t)(d.k_off[i + 1] - k0)};
+}
+
+// Tiles of `rows` rows over all documents without a table: document i has
+// the slots from off[i] / rows + i on, enough for its tiles, since
+// ceil((b - a) / rows) <= b / rows - a / rows + 1. Returns the document of a
+// slot and the tile's first row in it (which may lie past its end).
+__device__ __forceinline__ int slot_doc(const int64_t* off, int n_docs, int rows, int slot, int& first) {
+  int lo = 0, hi = n_docs - 1;
+  if (off) {
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((int)(off[mid] / rows) + mid <= slot) lo = mid;
+      else hi = mid - 1;
+    }
+    first = (slot - ((int)(off[lo] / rows) + lo)) * rows;
+  } else {
+    first = slot * rows;
+  }
+  return lo;
+}
+inline int64_t slots_of(int64_t tokens, int rows, int32_t n_docs) { return tokens / rows + n_docs; }
+
+// Rows [0, n) of a document's tile as a buffer: what lies past the last row
+// reads as zeros. `stride` in elements.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const __bf16* first, int64_t n, int64_t stride, int dim) {
+  int64_t bytes = n > 0 ? ((n - 1) * stride + dim) * 2 : 0;
+  if (bytes > 0x7ffffff0) bytes = 0x7ffffff0;  // tiles past that have a base of their own
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(first), (short)0, (int)bytes, 0x00020000);
+}
+
+// Place of 16-byte piece c of row r in a tile of DP elements a row: pieces
+// are exchanged within a row so that neither the rows' reads (8 or 16 rows,
+// one piece) nor the transposed ones (4 rows, two pieces) meet in a bank.
+template <int DP>
+__device__ __forceinline__ int swz(int r, int c) {
+  int f = ((r & 3) << 1) | ((r >> 2) & 1);
+  if constexpr (DP == 128) f |= r & 8;
+  return c ^ f;
+}
+
+// A tile of ROWS rows on its way through registers.
+template <int DP, int ROWS, int THREADS>
+struct Stage {
+  static constexpr int PIECES = DP / 8;
+  static constexpr int N = ROWS * PIECES / THREADS;
+  static_assert(ROWS * PIECES % THREADS == 0);
+  u32x4 v[N];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int first, int64_t stride, int dim) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = at % PIECES;
+      // pieces past the head dimension read as zeros like rows past the end
+      const int off = c * 8 < dim ? (int)(((int64_t)(first + row) * stride + c * 8) * 2) : 0x7ffffff0;
+      v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void store(__bf16* tile) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = at % PIECES;
+      *(u32x4*)(tile + row * DP + swz<DP>(row, c) * 8) = v[i];
+    }
+  }
+};
+
+// A operand: rows r0 + lane % 32, k = 16 ks + 8 h + j.
+template <int DP>
+__device__ __forceinline__ bf16x8 read_rows(const __bf16* tile, int r0, int ks) {
+  const int lane = threadIdx.x & 63, r = r0 + (lane & 31);
+  return *(const bf16x8*)(tile + r * DP + swz<DP>(r, 2 * ks + (lane >> 5)) * 8);
+}
+
+// A operand, transposed: row index of A = column c0 + lane % 32 of the tile,
+// k = rows r0 + 4 h + (0 .. 3) and r0 + 8 + 4 h + (0 .. 3). Sixteen lanes read
+// four rows of sixteen columns and each gets one column.
+template <int DP>
+__device__ __forceinline__ bf16x8 read_cols(const __bf16* tile, int r0, int c0) {
+  const int lane = threadIdx.x & 63, i = lane & 15, c = c0 + (lane & 16) + 4 * (i & 3);
+  const int r = r0 + 4 * (lane >> 5) + (i >> 2);
+  typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+  auto at = [&](int row) {
+    return (lds_ptr)(uintptr_t)(__attribute__((address_space(3))) void*)(
+        (__attribute__((address_space(3))) __bf16*)tile + row * DP + swz<DP>(row, c >> 3) * 8 + (c & 7));
+  };
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(r)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(r + 8));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Registers 8 t .. 8 t + 7 of a result, rounded to bfloat16, as a B operand.
+__device__ __forceinline__ bf16x8 as_operand(const f32x16& x, int t) {
+  bf16x8 r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = (__bf16)x[8 * t + j];
+  return r;
+}
+
+__device__ __forceinline__ float other_half(float v) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return __builtin_bit_cast(float, (uint32_t)((threadIdx.x & 32) ? s[0] : s[1]));
+}
+
+// Scale of the scores in units of log2. Not 0, so that a masked score, which
+// is -infinity, stays that.
+__device__ __forceinline__ float score_scale(float scale) { return fmaxf(scale * kLog2e, 0x1p-100f); }
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+}  // namespace attn
+}  // namespace argus
