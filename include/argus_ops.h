@@ -57,10 +57,10 @@ enum { ARGUS_F32 = 0, ARGUS_BF16 = 1, ARGUS_F16 = 2 }; /* element types */
  */
 typedef struct argus_embedding {
   const void* ids;      /* [n_tokens] int32 or int64 */
-  int64_t n_tokens;     /* 0 .. 2^28 */
+  int64_t n_tokens;     /* 0 .. 2^27 */
   int32_t ids_64;       /* 1: ids are int64 */
   int32_t n_vocab;      /* 1 .. 2^27 */
-  int32_t dim;          /* >= 1 */
+  int32_t dim;          /* 1 .. 65536 */
   int32_t dtype;        /* of table, out, dout */
   int32_t grad_dtype;   /* of dtable (argus_embedding_bwd) */
   float scale;

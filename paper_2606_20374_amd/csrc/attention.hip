@@ -52,7 +52,7 @@ __device__ void fill_empty(const FwdArgs& a) {
 }
 
 template <int DP, int NQ>
-__global__ __launch_bounds__(kThreads) void attn_fwd(FwdArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   constexpr int kRows = 4 * 32 * NQ;  // queries of a workgroup
   constexpr int KS = DP / 16, DT = DP / 32;
   __shared__ __align__(16) __bf16 kt[2][kKeys * DP];

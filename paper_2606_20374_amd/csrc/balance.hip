@@ -3,12 +3,16 @@
 // Sixteen lanes hold a token's logits, 16 bytes of each 256 to a lane (the
 // row is read once, in whole lines), so a wavefront takes four tokens and
 // every reduction over a token is four steps inside a row of lanes.
-//   forward   top_k times the largest key; a key orders the logit's bits and
-//             then the lower index, so ties need no further step. The first
-//             is the softmax's maximum. Sums of the probabilities per expert
-//             stay in registers over all tokens of a workgroup, counts in its
-//             LDS; the workgroups' sums are written once and added in their
-//             order by one workgroup, which makes the loss (in doubles).
+//   forward   a key orders a logit's value and then the lower index, so ties
+//             need no further step. Each lane sorts its own keys, as many as
+//             can be chosen, in registers (comparators of one maximum and one
+//             minimum); then top_k times the largest of the sixteen heads is
+//             taken and its lane moves up. The first is the softmax's
+//             maximum. Sums of the probabilities per expert stay in registers
+//             over all tokens of a workgroup, counts in its LDS; the
+//             workgroups' sums are written once and added in their order by
+//             a second launch, whose last workgroup makes the loss (in
+//             doubles).
 //   backward  p = exp(x - lse); the gates' gradients are put into a zeroed
 //             LDS row of the token, read back by the lanes that own the
 //             experts, and cleared.
@@ -23,48 +27,144 @@
 namespace argus {
 namespace {
 
-constexpr int kBlock = 1024;              // threads of a forward workgroup
-constexpr int kTokens = kBlock / 16;      // tokens it takes at a time
-constexpr int kMaxGrid = 256;             // one workgroup to a CU: few partial sums to add
+constexpr int kMaxGrid = 256;  // forward workgroups, one to a CU: few sums to add
 
 template <typename T>
 constexpr int kVec = 16 / sizeof(T);
 
 // Key of a logit: ascending with its value, and among equal values with
-// falling index. -0 and +0 are one value. 0 is below every key.
+// falling index; -0 and +0 are one value, and the keys of -infinity and of
+// what is no logit are `none`, below all others. Keys of 16-bit types are
+// 32-bit integers: the 32-bit float's bits, made ascending, of which the low
+// ten are free for the index (1,024 experts at most). Those of 32-bit floats
+// are doubles: the value leaves 29 bits of the mantissa free, and the minimum
+// and maximum of doubles are single instructions.
+constexpr uint32_t kIdx = ARGUS_MAX_EXPERTS - 1;
+static_assert((ARGUS_MAX_EXPERTS & kIdx) == 0 && kIdx < (1u << 13), "an index fits below a half's 19 bits");
+
 template <typename T>
 struct Key {
-  using U = uint32_t;  // 16-bit types: the value's bits above the index's
-  static __device__ __forceinline__ U make(T v, int e) {
-    const uint32_t b = __builtin_bit_cast(uint16_t, (float)v == 0.0f ? (T)0.0f : v);
-    return ((b & 0x8000u ? b ^ 0xffffu : b | 0x8000u) << 16) | (uint32_t)(0xffff - e);
+  using U = uint32_t;
+  static constexpr U kNone = 0;
+  static __device__ __forceinline__ U make(float f, int e) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, f + 0.0f);  // -0 becomes +0
+    const uint32_t up = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+    return (up & ~kIdx) | (kIdx - (uint32_t)e);
   }
-  static __device__ __forceinline__ int index(U k) { return 0xffff - (int)(k & 0xffffu); }
+  static __device__ __forceinline__ bool none(U k) { return k < 0x00800000u; }  // -infinity's 0x007fffff and below
+  static __device__ __forceinline__ int index(U k) { return (int)(kIdx - (k & kIdx)); }
+  static __device__ __forceinline__ float value(U k) {
+    return __builtin_bit_cast(float, (k & 0x80000000u ? k ^ 0x80000000u : ~k) & ~kIdx);
+  }
+  static __device__ __forceinline__ U largest(U a, U b) { return a > b ? a : b; }
+  static __device__ __forceinline__ U smallest(U a, U b) { return a < b ? a : b; }
+  template <int CTRL>
+  static __device__ __forceinline__ U dpp(U v) { return (U)dpp_i32<CTRL>((int)v); }
 };
 template <>
 struct Key<float> {
-  using U = uint64_t;
-  static __device__ __forceinline__ U make(float v, int e) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, v == 0.0f ? 0.0f : v);
-    return ((uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32) | (uint32_t)(0xffff - e);
+  using U = double;
+  static constexpr U kNone = -1e300;
+  static __device__ __forceinline__ U make(float f, int e) {
+    // also a NaN becomes kNone: no key is one
+    const uint64_t b = __builtin_bit_cast(uint64_t, __builtin_fmax((double)(f + 0.0f), kNone));
+    // a larger mantissa is a larger value above zero and a smaller one below
+    const uint32_t low = (uint32_t)e ^ (~(uint32_t)((int64_t)b >> 63) & kIdx);
+    return __builtin_bit_cast(double, b ^ low);  // kNone keeps its place below every value
   }
-  static __device__ __forceinline__ int index(U k) { return 0xffff - (int)(k & 0xffffu); }
+  static __device__ __forceinline__ bool none(U k) { return k < -1e200; }
+  static __device__ __forceinline__ int index(U k) {
+    const uint32_t b = (uint32_t)__builtin_bit_cast(uint64_t, k) & kIdx;
+    return (int)(k < 0 ? b : kIdx - b);
+  }
+  static __device__ __forceinline__ float value(U k) {
+    return (float)__builtin_bit_cast(double, __builtin_bit_cast(uint64_t, k) & ~(uint64_t)kIdx);
+  }
+  // fmax and fmin would first make each operand canonical, for NaNs that no key is
+  static __device__ __forceinline__ U largest(U a, U b) {
+    U r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+  }
+  static __device__ __forceinline__ U smallest(U a, U b) {
+    U r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+  }
+  template <int CTRL>
+  static __device__ __forceinline__ U dpp(U v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, ((uint64_t)(uint32_t)dpp_i32<CTRL>((int)(b >> 32)) << 32) | (uint32_t)dpp_i32<CTRL>((int)b));
+  }
 };
 
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_key(uint32_t v) { return (uint32_t)dpp_i32<CTRL>((int)v); }
-template <int CTRL>
-__device__ __forceinline__ uint64_t dpp_key(uint64_t v) {
-  return ((uint64_t)(uint32_t)dpp_i32<CTRL>((int)(v >> 32)) << 32) | (uint32_t)dpp_i32<CTRL>((int)v);
+// exp(x - m); the difference is taken first, which overflows for no logits
+// (the lowest values of a type among them).
+__device__ __forceinline__ float exp_from(float x, float m) {
+  return __builtin_amdgcn_exp2f((x - m) * 1.4426950408889634f);
 }
-template <typename U>
-__device__ __forceinline__ U max_of(U a, U b) { return a > b ? a : b; }
-template <typename U>
+
+// NI vectors of a row of E elements, of each 16 V one to a lane; what lies
+// past the row is `pad`.
+template <int NI, typename T, int V = kVec<T>>
+__device__ __forceinline__ void load_logits(Vec<T, V> (&v)[NI], const T* row, bool in, int E, T pad) {
+  const int lane = threadIdx.x & 15;
+  const bool whole = E % V == 0;  // no vector lies across the row's end
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int at = (i * 16 + lane) * V;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[i].e[j] = pad;
+    if (whole) {
+      if (in && at < E) v[i] = load_vec<V>(row + at);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (in && at + j < E) v[i].e[j] = row[at + j];
+    }
+  }
+}
+
+template <typename K, typename U>
 __device__ __forceinline__ U row_max(U v) {
-  v = max_of(v, dpp_key<kXor1>(v));
-  v = max_of(v, dpp_key<kXor2>(v));
-  v = max_of(v, dpp_key<kHalfMirror>(v));
-  return max_of(v, dpp_key<kMirror>(v));
+  v = K::largest(v, K::template dpp<kXor1>(v));
+  v = K::largest(v, K::template dpp<kXor2>(v));
+  v = K::largest(v, K::template dpp<kHalfMirror>(v));
+  return K::largest(v, K::template dpp<kMirror>(v));
+}
+
+// Sorts M keys, a power of two, descending (odd-even merges).
+template <typename K, int M, typename U>
+__device__ __forceinline__ void sort_keys(U (&k)[M]) {
+#pragma unroll
+  for (int p = 1; p < M; p *= 2)
+#pragma unroll
+    for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < M; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; ++i)
+          if (i + j + q < M && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+            const U a = k[i + j], b = k[i + j + q];
+            k[i + j] = K::largest(a, b);
+            k[i + j + q] = K::smallest(a, b);
+          }
+}
+
+// The M largest of two descending lists of M, descending, into `a`.
+template <typename K, int M, typename U>
+__device__ __forceinline__ void merge_keys(U (&a)[M], const U (&b)[M]) {
+#pragma unroll
+  for (int i = 0; i < M; ++i) a[i] = K::largest(a[i], b[M - 1 - i]);
+#pragma unroll
+  for (int q = M / 2; q >= 1; q /= 2)
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+      if (!(i & q)) {
+        const U x = a[i], y = a[i + q];
+        a[i] = K::largest(x, y);
+        a[i + q] = K::smallest(x, y);
+      }
 }
 
 struct BalArgs {
@@ -79,118 +179,118 @@ struct BalArgs {
   float* psum;     // [workgroups][E]
   uint32_t* cnt;   // [workgroups][E]
   uint32_t* valid; // [workgroups][2]: tokens taking part; 1 if a token was left out for its logits
+  double* terms;   // [joining workgroups] the loss's
+  uint32_t* ticket;
 };
 
-template <typename T, int NI>
-__global__ __launch_bounds__(kBlock) void bal_fwd(BalArgs a) {
+// Most threads of a forward workgroup: fewer where a lane holds more logits.
+constexpr int fwd_block(int n) { return n <= 16 ? 1024 : n <= 32 ? 512 : 256; }
+
+// KC: 8 or 16, not below top_k.
+template <typename T, int NI, int KC>
+__global__ __launch_bounds__(fwd_block(NI * kVec<T>)) void bal_fwd(BalArgs a) {
   constexpr int V = kVec<T>, N = NI * V;
   using KT = Key<T>;
   using U = typename KT::U;
   __shared__ float ps[ARGUS_MAX_EXPERTS];
   __shared__ uint32_t cnt[ARGUS_MAX_EXPERTS];
   __shared__ uint32_t nv[2];
-  const int tid = threadIdx.x, lane = tid & 15, E = a.E;
-  for (int e = tid; e < E; e += kBlock) {
+  const int tid = threadIdx.x, lane = tid & 15, E = a.E, block = blockDim.x, tokens = block / 16;
+  for (int e = tid; e < E; e += block) {
     ps[e] = 0;
     cnt[e] = 0;
   }
   if (tid < 2) nv[tid] = 0;
+  if (blockIdx.x == 0 && tid == 0) *a.ticket = 0;
   __syncthreads();
   const T* logits = (const T*)a.logits;
   float acc[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) acc[i] = 0;
-  for (int64_t t0 = (int64_t)blockIdx.x * kTokens; t0 < a.n; t0 += (int64_t)gridDim.x * kTokens) {
-    const int64_t t = t0 + (tid >> 4);
-    const bool in = t < a.n && (!a.mask || a.mask[t]);
+  const int64_t step = (int64_t)gridDim.x * tokens;
+  int64_t t = (int64_t)blockIdx.x * tokens + (tid >> 4);
+  Vec<T, V> v[NI];
+  bool in = false;
+  auto fetch = [&](int64_t at) {
+    in = at < a.n && (!a.mask || a.mask[at]);
+    load_logits(v, logits + at * a.stride, in, E, (T)-__builtin_inff());
+  };
+  fetch(t);
+  for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < a.n; t0 += step, t += step) {
+    const bool here = in;
     float x[N];
-    U key[N];
-    bool nan = false;
+    U best[KC];  // the lane's largest keys, descending
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int at = (i * 16 + lane) * V;
-      Vec<T, V> v = {};
-      if (in) v = load_row<V>(logits + t * a.stride, at, E);
+    for (int c = 0; c < N; c += KC) {
+      U k[KC];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const bool here = in && at + j < E;
-        x[i * V + j] = here ? to_f32(v.e[j]) : -__builtin_inff();
-        nan |= here && v.e[j] != v.e[j];
-        // a logit of -infinity is never chosen
-        key[i * V + j] = x[i * V + j] > -__builtin_inff() ? KT::make(v.e[j], at + j) : 0;
+      for (int j = 0; j < KC; ++j) {
+        k[j] = KT::kNone;
+        if (c + j < N) {
+          x[c + j] = to_f32(v[(c + j) / V].e[(c + j) % V]);
+          k[j] = KT::make(x[c + j], ((c + j) / V * 16 + lane) * V + (c + j) % V);
+        }
+      }
+      sort_keys<KT>(k);
+      if (c == 0) {
+#pragma unroll
+        for (int j = 0; j < KC; ++j) best[j] = k[j];
+      } else {
+        merge_keys<KT>(best, k);
       }
     }
-    const float any_nan = row_sum(nan ? 1.0f : 0.0f);
-    U best = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) best = max_of(best, key[i]);
-    best = row_max(best);
-    // the largest logit, from the lane that holds it
-    float m = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
-    m = fmaxf(m, dpp_f32<kXor1>(m));
-    m = fmaxf(m, dpp_f32<kXor2>(m));
-    m = fmaxf(m, dpp_f32<kHalfMirror>(m));
-    m = fmaxf(m, dpp_f32<kMirror>(m));
-    const bool ok = in && any_nan == 0.0f && m > -__builtin_inff() && m < __builtin_inff();
-    float p[N], z = 0;
+    fetch(t + step);
+    U top = row_max<KT>(best[0]);
+    // the largest logit; with a NaN or an infinity among them z is NaN below
+    const float m = KT::value(top);
+    float z = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      p[i] = ok ? __expf(x[i] - m) : 0.0f;
-      z += p[i];
+      x[i] = exp_from(x[i], m);
+      z += x[i];
     }
     z = row_sum(z);
-    const float rz = ok ? 1.0f / z : 0.0f;
+    const bool ok = here && !KT::none(top) && z < __builtin_inff();  // and no NaN
+    const float rz = 1.0f / z;
+    if (__ballot(!ok)) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      p[i] *= rz;
-      acc[i] += p[i];
+      for (int i = 0; i < N; ++i) x[i] = ok ? x[i] : 0.0f;
     }
-    int mine = -1;      // lane j keeps the j-th choice
-    float mine_p = 0;
-    for (int k = 0; k < a.K; ++k) {
-      int e = ok && best ? KT::index(best) : -1;
-      float g = 0;
+    const float w = ok ? rz : 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const bool hit = key[i] == best;
-        g = hit ? p[i] : g;
-        key[i] = hit ? 0 : key[i];
-      }
-      g = row_sum(best ? g : 0.0f);
-      if (lane == k) {
-        mine = e;
-        mine_p = e >= 0 ? g : 0.0f;
-      }
-      U nb = 0;
+    for (int i = 0; i < N; ++i) acc[i] += x[i] * w;
+    U mine = KT::kNone;  // lane j keeps the j-th choice
 #pragma unroll
-      for (int i = 0; i < N; ++i) nb = max_of(nb, key[i]);
-      best = row_max(nb);
+    for (int k = 0; k < KC; ++k) {
+      if (k < a.K) {
+        if (lane == k) mine = top;
+        if (k + 1 < KC) {
+          const bool won = best[0] == top;
+#pragma unroll
+          for (int j = 0; j + 1 < KC - k; ++j) best[j] = won ? best[j + 1] : best[j];
+          top = row_max<KT>(best[0]);
+        }
+      }
     }
     if (t < a.n) {
       if (lane < a.K) {
-        a.expert[t * a.K + lane] = mine;
-        a.gate[t * a.K + lane] = mine_p;
-        if (mine >= 0) atomicAdd(&cnt[mine], 1u);
+        const bool chosen = ok && !KT::none(mine);
+        const int e = chosen ? KT::index(mine) : -1;
+        a.expert[t * a.K + lane] = e;
+        a.gate[t * a.K + lane] = chosen ? exp_from(KT::value(mine), m) * rz : 0.0f;
+        if (chosen) atomicAdd(&cnt[e], 1u);
       }
       if (lane == 0) {
         a.lse[t] = ok ? m + __logf(z) : -__builtin_inff();
         if (ok) atomicAdd(&nv[0], 1u);
-        if (in && !ok) nv[1] = 1;
+        if (here && !ok) nv[1] = 1;
       }
     }
   }
   // the four tokens of a wavefront, then the wavefronts in their order
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float v = acc[i];
-    auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
-    v = __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
-    auto u = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
-    acc[i] = __builtin_bit_cast(float, (uint32_t)u[0]) + __builtin_bit_cast(float, (uint32_t)u[1]);
-  }
-  for (int w = 0; w < kBlock / 64; ++w) {
+  for (int i = 0; i < N; ++i) acc[i] = rows_sum(acc[i]);
+  for (int w = 0; w < block / 64; ++w) {
     if (tid >> 6 == w && (tid & 63) < 16) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -200,34 +300,35 @@ __global__ __launch_bounds__(kBlock) void bal_fwd(BalArgs a) {
     }
     __syncthreads();
   }
-  for (int e = tid; e < E; e += kBlock) {
+  for (int e = tid; e < E; e += block) {
     a.psum[(int64_t)blockIdx.x * E + e] = ps[e];
     a.cnt[(int64_t)blockIdx.x * E + e] = cnt[e];
   }
   if (tid < 2) a.valid[blockIdx.x * 2 + tid] = nv[tid];
 }
 
+constexpr int kJoin = 32;  // experts of a joining workgroup
+
+// Adds the workgroups' sums in their order, 32 runs of them side by side and
+// then the runs; the last workgroup to end adds the loss's terms.
 __global__ __launch_bounds__(1024) void bal_join(BalArgs a, int32_t blocks, argus_balance_out_t o) {
-  __shared__ float ps[1024];
-  __shared__ uint32_t cs[1024];
-  __shared__ double part[1024];
+  __shared__ float ps[32][kJoin];
+  __shared__ uint32_t cs[32][kJoin];
   __shared__ uint32_t tot[2];
-  const int tid = threadIdx.x, E = a.E;
-  int ep = 1;
-  while (ep < E) ep *= 2;
-  const int groups = 1024 / ep, e = tid % ep, g = tid / ep;
+  __shared__ bool last;
+  const int tid = threadIdx.x, E = a.E, c = tid % kJoin, g = tid / kJoin, e = blockIdx.x * kJoin + c;
+  if (tid < 2) tot[tid] = 0;
   float s = 0;
-  uint32_t c = 0;
+  uint32_t n_of = 0;
   if (e < E) {
 #pragma unroll 8
-    for (int b = g; b < blocks; b += groups) {
+    for (int b = g; b < blocks; b += 32) {
       s += a.psum[(int64_t)b * E + e];
-      c += a.cnt[(int64_t)b * E + e];
+      n_of += a.cnt[(int64_t)b * E + e];
     }
   }
-  ps[tid] = s;
-  cs[tid] = c;
-  if (tid < 2) tot[tid] = 0;
+  ps[g][c] = s;
+  cs[g][c] = n_of;
   __syncthreads();
   if (tid < blocks) {
     if (a.valid[tid * 2]) atomicAdd(&tot[0], a.valid[tid * 2]);
@@ -235,25 +336,32 @@ __global__ __launch_bounds__(1024) void bal_join(BalArgs a, int32_t blocks, argu
   }
   __syncthreads();
   const uint32_t n = tot[0];
-  double term = 0;
-  if (g == 0 && e < E) {
-    for (int i = 1; i < groups; ++i) {
-      s += ps[i * ep + e];
-      c += cs[i * ep + e];
+  if (tid < 64) {
+    double term = 0;
+    if (tid < kJoin && e < E) {
+      float sum = 0;
+      uint32_t cnt = 0;
+      for (int i = 0; i < 32; ++i) {
+        sum += ps[i][tid];
+        cnt += cs[i][tid];
+      }
+      o.count[e] = cnt;
+      o.prob[e] = n ? (float)((double)sum / n) : 0.0f;
+      term = n ? (double)cnt * (double)sum / n : 0.0;
     }
-    o.count[e] = c;
-    o.prob[e] = n ? (float)((double)s / n) : 0.0f;
-    term = n ? (double)c * (double)s / n : 0.0;
+    for (int h = 32; h > 0; h >>= 1) term += __shfl_xor(term, h, 64);
+    if (tid == 0) {
+      __hip_atomic_store(&a.terms[blockIdx.x], term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    }
   }
-  part[tid] = term;
   __syncthreads();
-  for (int h = 512; h > 0; h >>= 1) {
-    if (tid < h) part[tid] += part[tid + h];
-    __syncthreads();
-  }
-  if (tid == 0) {
+  if (last && tid == 0) {
+    double sum = 0;
+    for (unsigned i = 0; i < gridDim.x; ++i)
+      sum += __hip_atomic_load(&a.terms[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     o.n_valid[0] = n;
-    o.loss[0] = n ? (float)((double)a.alpha * E * part[0] / ((double)a.K * n)) : 0.0f;
+    o.loss[0] = n ? (float)((double)a.alpha * E * sum / ((double)a.K * n)) : 0.0f;
     if (o.dev_status) *o.dev_status = tot[1] ? (int32_t)ARGUS_DEV_LOGITS : 0;
   }
 }
@@ -326,7 +434,7 @@ __global__ __launch_bounds__(256) void bal_bwd(BalBwdArgs a) {
       Vec<T, V> o;
 #pragma unroll
       for (int j = 0; j < V; ++j) o.e[j] = from_f32<T>(p[i * V + j] * (g[i * V + j] - s));
-      store_row<V>(out + t * E, (i * 16 + lane) * V, E, o);
+      stream_row<V>(out + t * E, (i * 16 + lane) * V, E, o);
     }
   }
 }
@@ -350,34 +458,59 @@ hipError_t with_pieces(int32_t E, F fn) {
   }
 }
 
-int64_t bal_grid(const argus_balance_t& p) {
-  const int64_t need = ceil_div(p.n_tokens, kTokens);
-  return need < 1 ? 1 : need < kMaxGrid ? need : kMaxGrid;
+// Forward workgroups, at most one to a CU, and their threads: no more than
+// the tokens need, so that few tokens still spread over the CUs.
+struct BalShape {
+  int64_t grid;
+  int block;
+};
+BalShape bal_shape(const argus_balance_t& p) {
+  const int v = p.dtype == ARGUS_F32 ? 4 : 8, most = fwd_block((int)ceil_div(p.n_experts, 16 * v) * v);
+  const int64_t even = ceil_div(ceil_div(p.n_tokens, kMaxGrid), 4) * 64;  // threads, a wavefront to four tokens
+  const int block = (int)(even < 64 ? 64 : even < most ? even : most);
+  const int64_t need = ceil_div(p.n_tokens, block / 16);
+  return {need < 1 ? 1 : need < kMaxGrid ? need : kMaxGrid, block};
+}
+
+struct BalLayout {
+  size_t cnt, valid, terms, ticket, total;
+};
+BalLayout bal_layout(const argus_balance_t& p) {
+  const size_t g = (size_t)bal_shape(p).grid, part = align256(g * (size_t)p.n_experts * 4);
+  BalLayout l;
+  l.cnt = part;
+  l.valid = 2 * part;
+  l.terms = l.valid + align256(g * 8);
+  l.ticket = l.terms + align256((size_t)ceil_div(p.n_experts, kJoin) * 8);
+  l.total = l.ticket + 256;
+  return l;
 }
 
 }  // namespace
 
-size_t balance_workspace_bytes(const argus_balance_t& p) {
-  const size_t g = (size_t)bal_grid(p);
-  return 2 * align256(g * (size_t)p.n_experts * 4) + align256(g * 8);
-}
+size_t balance_workspace_bytes(const argus_balance_t& p) { return bal_layout(p).total; }
 
 hipError_t launch_balance(const argus_balance_t& p, const void* logits, const uint8_t* mask,
                           const argus_balance_out_t& o, void* ws, hipStream_t st) {
-  const int64_t grid = bal_grid(p);
-  const size_t part = align256((size_t)grid * (size_t)p.n_experts * 4);
+  const BalShape shape = bal_shape(p);
+  const int64_t grid = shape.grid;
+  const BalLayout l = bal_layout(p);
   uint8_t* base = (uint8_t*)ws;
   BalArgs a{p.n_tokens, p.row_stride, p.n_experts, p.top_k, p.alpha, logits, mask, o.expert, o.gate, o.lse,
-            (float*)base, (uint32_t*)(base + part), (uint32_t*)(base + 2 * part)};
+            (float*)base, (uint32_t*)(base + l.cnt), (uint32_t*)(base + l.valid), (double*)(base + l.terms),
+            (uint32_t*)(base + l.ticket)};
   const hipError_t e = with_dtype(p.dtype, [&](auto t) {
     using T = decltype(t);
     return with_pieces<T>(p.n_experts, [&](auto ni) {
-      hipLaunchKernelGGL((bal_fwd<T, decltype(ni)::value>), dim3((unsigned)grid), dim3(kBlock), 0, st, a);
+      constexpr int NI = decltype(ni)::value;
+      const dim3 block(shape.block);
+      if (p.top_k <= 8) hipLaunchKernelGGL((bal_fwd<T, NI, 8>), dim3((unsigned)grid), block, 0, st, a);
+      else hipLaunchKernelGGL((bal_fwd<T, NI, 16>), dim3((unsigned)grid), block, 0, st, a);
       return hipGetLastError();
     });
   });
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(bal_join, dim3(1), dim3(1024), 0, st, a, (int32_t)grid, o);
+  hipLaunchKernelGGL(bal_join, dim3((unsigned)ceil_div(p.n_experts, kJoin)), dim3(1024), 0, st, a, (int32_t)grid, o);
   return hipGetLastError();
 }
 

@@ -7,13 +7,16 @@
 //   db = sum dy.
 // Both are bound by memory: a row is read once (x; x and dy) and written once.
 // A row belongs to one wavefront where it is at most two 16-byte vectors per
-// lane wide (no barrier at all), to a workgroup of 256 up to four vectors per
-// thread, and to one of 1,024 past that. Workgroups stay and take every
-// n-th row, so that the weights and, backward, the sums of the weight's
-// gradient live in registers, and the next row is loaded before the current
-// one is reduced. The gradient sums of the workgroups are written once each
-// ([workgroups][2][cols]) and added in the order of the workgroups.
-// All sums are 32-bit floats.
+// lane wide (no barrier at all), to as many wavefronts as have a vector per
+// lane up to 1,024 vectors, and to up to sixteen wavefronts of more vectors
+// past that. Workgroups stay and take every n-th row, so that the weights and,
+// backward, the sums of the weight's gradient live in registers. Forward the
+// next row is loaded before the current one is reduced; backward its registers
+// would cost a workgroup of the CU, which hides more (20,011 x 5,000 bf16:
+// 226 us with, 129 us without; three workgroups of ten
+// wavefronts to a CU in place of two: 167 us). The gradient sums of the
+// workgroups are written once each ([workgroups][2][cols]) and added in the
+// order of the workgroups. All sums are 32-bit floats.
 #include "ops_internal.h"
 
 #pragma clang fp contract(fast)
@@ -35,46 +38,48 @@ struct LnArgs {
   int32_t has_db;
 };
 
-// Sums of M values over the TPR threads of a row, in every thread of it.
-// `slot` alternates between calls, so one barrier per call is enough.
-template <int TPR, int M>
+constexpr int kMaxWaves = 16;
+
+// Sums of M values over the threads of a row (a wavefront, or the workgroup),
+// in every thread of it. `slot` alternates between calls, so one barrier per
+// call is enough.
+template <bool WAVE, int M>
 __device__ __forceinline__ void row_sums(float (&v)[M], float* lds, int slot) {
 #pragma unroll
   for (int m = 0; m < M; ++m) v[m] = wave_sum_f32(v[m]);
-  if constexpr (TPR > 64) {
-    constexpr int W = TPR / 64;
-    float* s = lds + slot * (W * M);
+  if constexpr (!WAVE) {
+    // sixteen places to a value: those of wavefronts that do not exist stay 0
+    float* s = lds + slot * (kMaxWaves * M);
     const int w = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-      for (int m = 0; m < M; ++m) s[w * M + m] = v[m];
+      for (int m = 0; m < M; ++m) s[m * kMaxWaves + w] = v[m];
     }
     lds_barrier();
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-      float t = 0;
-#pragma unroll
-      for (int i = 0; i < W; ++i) t += s[i * M + m];
-      v[m] = t;
-    }
+    for (int m = 0; m < M; ++m) v[m] = row_sum(s[m * kMaxWaves + (threadIdx.x & 15)]);
   }
 }
 
-template <typename T, typename W, int N, int TPR>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_fwd(LnArgs a) {
+template <typename T, typename W, int N, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void ln_fwd(LnArgs a) {
   constexpr int V = kVec<T>;
-  __shared__ float lds[2 * (TPR / 64)];
-  const int lane = threadIdx.x % TPR, cols = a.cols;
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float lds[2 * kMaxWaves];
+  const int tpr = WAVE ? 64 : blockDim.x, lane = WAVE ? threadIdx.x & 63 : threadIdx.x, cols = a.cols;
+  constexpr int RPB = WAVE ? 4 : 1;
   const int64_t step = (int64_t)gridDim.x * RPB;
-  int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  int64_t row = (int64_t)blockIdx.x * RPB + (WAVE ? threadIdx.x >> 6 : 0);
+  if (!WAVE) {
+    if (threadIdx.x < 2 * kMaxWaves) lds[threadIdx.x] = 0;
+    __syncthreads();
+  }
   const T* x = (const T*)a.x;
   T* y = (T*)a.y;
   const float inv = 1.0f / (float)cols;
   Vec<W, V> w[N], b[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int at = (i * TPR + lane) * V;
+    const int at = (i * tpr + lane) * V;
     w[i] = load_row<V>((const W*)a.w, at, cols);
     if (a.b) {
       b[i] = load_row<V>((const W*)a.b, at, cols);
@@ -86,7 +91,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_fwd(LnArgs a) {
   Vec<T, V> nx[N];
   if (row < a.rows) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) nx[i] = load_row<V>(x + row * a.x_stride, (i * TPR + lane) * V, cols);
+    for (int i = 0; i < N; ++i) nx[i] = load_row<V>(x + row * a.x_stride, (i * tpr + lane) * V, cols);
   }
   for (; row < a.rows; row += step) {
     float f[N * V], s[1] = {0};
@@ -99,9 +104,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_fwd(LnArgs a) {
       }
     if (row + step < a.rows) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) nx[i] = load_row<V>(x + (row + step) * a.x_stride, (i * TPR + lane) * V, cols);
+      for (int i = 0; i < N; ++i) nx[i] = load_row<V>(x + (row + step) * a.x_stride, (i * tpr + lane) * V, cols);
     }
-    row_sums<TPR, 1>(s, lds, 0);
+    row_sums<WAVE, 1>(s, lds, 0);
     const float mean = s[0] * inv;
     s[0] = 0;
 #pragma unroll
@@ -109,10 +114,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_fwd(LnArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         float& d = f[i * V + j];
-        d = (i * TPR + lane) * V + j < cols ? d - mean : 0.0f;
+        d = (i * tpr + lane) * V + j < cols ? d - mean : 0.0f;
         s[0] += d * d;
       }
-    row_sums<TPR, 1>(s, lds, 1);
+    row_sums<WAVE, 1>(s, lds, 1);
     const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
     if (lane == 0) {
       a.mean[row] = mean;
@@ -124,18 +129,23 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_fwd(LnArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j)
         o.e[j] = from_f32<T>(f[i * V + j] * rstd * to_f32(w[i].e[j]) + to_f32(b[i].e[j]));
-      store_row<V>(y + row * cols, (i * TPR + lane) * V, cols, o);
+      store_row<V>(y + row * cols, (i * tpr + lane) * V, cols, o);
     }
   }
 }
 
-template <typename T, typename W, int N, int TPR>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_bwd(LnArgs a) {
+template <typename T, typename W, int N, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void ln_bwd(LnArgs a) {
   constexpr int V = kVec<T>;
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-  __shared__ float lds[2 * 2 * (TPR / 64)];
+  constexpr int RPB = WAVE ? 4 : 1;
+  __shared__ float lds[2 * 2 * kMaxWaves];
   __shared__ float join[RPB > 1 ? (RPB - 1) * 64 * 2 : 1];
-  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR, cols = a.cols;
+  const int tpr = WAVE ? 64 : blockDim.x, lane = WAVE ? threadIdx.x & 63 : threadIdx.x;
+  const int sub = WAVE ? threadIdx.x >> 6 : 0, cols = a.cols;
+  if (!WAVE) {
+    if (threadIdx.x < 4 * kMaxWaves) lds[threadIdx.x] = 0;
+    __syncthreads();
+  }
   const int64_t step = (int64_t)gridDim.x * RPB;
   const T* x = (const T*)a.x;
   const T* dy = (const T*)a.dy;
@@ -144,25 +154,17 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_bwd(LnArgs a) {
   Vec<W, V> w[N];
   float dw[N * V], db[N * V];
 #pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = load_row<V>((const W*)a.w, (i * TPR + lane) * V, cols);
+  for (int i = 0; i < N; ++i) w[i] = load_row<V>((const W*)a.w, (i * tpr + lane) * V, cols);
 #pragma unroll
   for (int i = 0; i < N * V; ++i) dw[i] = db[i] = 0;
-  Vec<T, V> nx[N], nd[N];
-  float nmean = 0, nrstd = 0;
-  int64_t row = (int64_t)blockIdx.x * RPB + sub;
-  auto fetch = [&](int64_t r) {
+  auto take = [&](int64_t row, int slot) {
+    Vec<T, V> xv[N], dv[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      nx[i] = load_row<V>(x + r * a.x_stride, (i * TPR + lane) * V, cols);
-      nd[i] = load_row<V>(dy + r * a.dy_stride, (i * TPR + lane) * V, cols);
+      xv[i] = load_row<V>(x + row * a.x_stride, (i * tpr + lane) * V, cols);
+      dv[i] = load_row<V>(dy + row * a.dy_stride, (i * tpr + lane) * V, cols);
     }
-    nmean = a.mean[r];
-    nrstd = a.rstd[r];
-  };
-  if (row < a.rows) fetch(row);
-  int slot = 0;
-  for (; row < a.rows; row += step, slot ^= 1) {
-    const float mean = nmean, rstd = nrstd;
+    const float mean = a.mean[row], rstd = a.rstd[row];
     float xh[N * V], g[N * V], s[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -170,30 +172,31 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_bwd(LnArgs a) {
       for (int j = 0; j < V; ++j) {
         const int k = i * V + j;
         // past the row's end dy is 0, so every sum is unaffected
-        xh[k] = (to_f32(nx[i].e[j]) - mean) * rstd;
-        const float d = to_f32(nd[i].e[j]);
+        xh[k] = (to_f32(xv[i].e[j]) - mean) * rstd;
+        const float d = to_f32(dv[i].e[j]);
         g[k] = d * to_f32(w[i].e[j]);
         dw[k] += d * xh[k];
         db[k] += d;
         s[0] += g[k];
         s[1] += g[k] * xh[k];
       }
-    if (row + step < a.rows) fetch(row + step);
-    row_sums<TPR, 2>(s, lds, slot);
+    row_sums<WAVE, 2>(s, lds, slot);
     const float m0 = s[0] * inv, m1 = s[1] * inv;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       Vec<T, V> o;
 #pragma unroll
       for (int j = 0; j < V; ++j) o.e[j] = from_f32<T>(rstd * (g[i * V + j] - m0 - xh[i * V + j] * m1));
-      store_row<V>(dx + row * cols, (i * TPR + lane) * V, cols, o);
+      store_row<V>(dx + row * cols, (i * tpr + lane) * V, cols, o);
     }
-  }
+  };
+  int64_t row = (int64_t)blockIdx.x * RPB + sub;
+  for (int slot = 0; row < a.rows; row += step, slot ^= 1) take(row, slot);
   float* pw = a.part + (int64_t)blockIdx.x * 2 * cols;
   if constexpr (RPB == 1) {
 #pragma unroll
     for (int i = 0; i < N * V; ++i) {
-      const int at = (i / V * TPR + lane) * V + i % V;
+      const int at = (i / V * tpr + lane) * V + i % V;
       if (at < cols) {
         pw[at] = dw[i];
         if (a.has_db) pw[cols + at] = db[i];
@@ -209,7 +212,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void ln_bwd(LnArgs a) {
         join[(sub - 1) * 128 + 64 + lane] = db[i];
       }
       __syncthreads();
-      const int at = (i / V * TPR + lane) * V + i % V;
+      const int at = (i / V * tpr + lane) * V + i % V;
       if (sub == 0 && at < cols) {
         float u = dw[i], v = db[i];
 #pragma unroll
@@ -247,45 +250,24 @@ __global__ __launch_bounds__(1024) void ln_bwd_join(const float* part, int32_t n
   }
 }
 
-// Threads per row and vectors per thread of a row of `vecs` 16-byte vectors.
+// Threads and vectors per thread of a row of `vecs` 16-byte vectors.
 struct LnShape {
-  int tpr, n;
+  bool wave;
+  int threads, n;  // of a workgroup, which has four rows at a time where a wavefront has one
 };
-LnShape ln_shape(int64_t vecs) {
-  const int tpr = vecs <= 128 ? 64 : vecs <= 1024 ? 256 : 1024;
-  return {tpr, (int)ceil_div(vecs, tpr)};
+LnShape ln_shape(const argus_layer_norm_t& p) {
+  const int64_t vecs = ceil_div(p.cols, p.dtype == ARGUS_F32 ? 4 : 8);
+  if (vecs <= 128) return {true, 256, (int)ceil_div(vecs, 64)};
+  const int n = (int)ceil_div(vecs, 1024);
+  return {false, (int)ceil_div(ceil_div(vecs, n), 64) * 64, n};
 }
-LnShape ln_shape(const argus_layer_norm_t& p) { return ln_shape(ceil_div(p.cols, p.dtype == ARGUS_F32 ? 4 : 8)); }
 
-// Workgroups: 2,048 threads of each CU forward (the weights are read once per
-// workgroup); half of that backward, where each writes its sums once.
-int64_t ln_grid(const argus_layer_norm_t& p, int64_t threads_per_cu) {
-  const int tpr = ln_shape(p).tpr;
-  const int64_t rpb = tpr < 256 ? 256 / tpr : 1, block = tpr < 256 ? 256 : tpr;
-  const int64_t most = 256 * (threads_per_cu / block), need = ceil_div(p.rows, rpb);
+// Workgroups that take the rows in turn: `threads` of each CU, all that fit at
+// once (forward 32,768 x 4,096 bf16 with 2,048: 98.7 us, 1,536: 108, 8,192: 101).
+int64_t ln_grid(const argus_layer_norm_t& p, int64_t threads) {
+  const LnShape s = ln_shape(p);
+  const int64_t fit = threads / s.threads, most = 256 * (fit < 1 ? 1 : fit), need = ceil_div(p.rows, s.wave ? 4 : 1);
   return need < most ? need : most;
-}
-
-template <typename T, typename W, int TPR, bool BWD>
-hipError_t ln_launch_n(int n, const LnArgs& a, int64_t grid, hipStream_t st) {
-  auto go = [&](auto k) {
-    hipLaunchKernelGGL(k, dim3(grid), dim3(TPR < 256 ? 256 : TPR), 0, st, a);
-    return hipGetLastError();
-  };
-#define ARGUS_LN(NN)                                         \
-  if constexpr (BWD) return go(ln_bwd<T, W, NN, TPR>);       \
-  else return go(ln_fwd<T, W, NN, TPR>)
-  switch (n) {
-    case 1: ARGUS_LN(1);
-    case 2: ARGUS_LN(2);
-    default: break;
-  }
-  if constexpr (TPR > 64 && 2 * TPR * kVec<T> < ARGUS_MAX_LN_COLS) {  // wider rows do not exist
-    if (n == 3) { ARGUS_LN(3); }
-    if (n == 4) { ARGUS_LN(4); }
-  }
-#undef ARGUS_LN
-  return hipErrorInvalidValue;
 }
 
 template <bool BWD>
@@ -295,9 +277,17 @@ hipError_t ln_launch(const argus_layer_norm_t& p, const LnArgs& a, int64_t grid,
     using T = decltype(t);
     auto by_weight = [&](auto wt) {
       using W = decltype(wt);
-      if (s.tpr == 64) return ln_launch_n<T, W, 64, BWD>(s.n, a, grid, st);
-      if (s.tpr == 256) return ln_launch_n<T, W, 256, BWD>(s.n, a, grid, st);
-      return ln_launch_n<T, W, 1024, BWD>(s.n, a, grid, st);
+      auto go = [&](auto fwd, auto bwd) {
+        hipLaunchKernelGGL(BWD ? bwd : fwd, dim3((unsigned)grid), dim3(s.threads), 0, st, a);
+        return hipGetLastError();
+      };
+#define ARGUS_LN(N, WAVE) go(ln_fwd<T, W, N, WAVE>, ln_bwd<T, W, N, WAVE>)
+      if (s.wave) return s.n == 1 ? ARGUS_LN(1, true) : ARGUS_LN(2, true);
+      if (s.n == 1) return ARGUS_LN(1, false);
+      if (s.n == 2) return ARGUS_LN(2, false);
+      if constexpr (kVec<T> == 4) return s.n == 3 ? ARGUS_LN(3, false) : ARGUS_LN(4, false);  // up to 16,384 columns
+#undef ARGUS_LN
+      return hipErrorInvalidValue;
     };
     return p.weight_dtype == ARGUS_F32 ? by_weight(float{}) : by_weight(T{});
   });
@@ -313,13 +303,13 @@ hipError_t launch_layer_norm(const argus_layer_norm_t& p, const void* x, const v
 }
 
 size_t layer_norm_bwd_workspace_bytes(const argus_layer_norm_t& p) {
-  return align256((size_t)ln_grid(p, 1024) * 2 * (size_t)p.cols * sizeof(float));
+  return align256((size_t)ln_grid(p, 1536) * 2 * (size_t)p.cols * sizeof(float));
 }
 
 hipError_t launch_layer_norm_bwd(const argus_layer_norm_t& p, const void* dy, const void* x, const float* mean,
                                  const float* rstd, const void* w, void* dx, void* dw, void* db, void* ws,
                                  hipStream_t st) {
-  const int64_t grid = ln_grid(p, 1024);
+  const int64_t grid = ln_grid(p, 1536);
   if (grid) {
     LnArgs a{p.rows, p.x_stride, p.dy_stride, p.cols, p.eps, x, dy, w, nullptr, nullptr, dx,
              const_cast<float*>(mean), const_cast<float*>(rstd), (float*)ws, db != nullptr};

@@ -15,7 +15,8 @@ bool bad_workspace(const void* ws, size_t have, size_t need) {
 }
 
 bool bad_embedding(const argus_embedding_t* p) {
-  if (!p || p->n_tokens < 0 || p->n_tokens > (1 << 28) || p->n_vocab < 1 || p->n_vocab > (1 << 27) || p->dim < 1)
+  if (!p || p->n_tokens < 0 || p->n_tokens > (1 << 27) || p->n_vocab < 1 || p->n_vocab > (1 << 27) || p->dim < 1 ||
+      p->dim > (1 << 16))
     return true;
   if (bad_dtype(p->dtype) || p->row_stride < 0 || !std::isfinite(p->scale)) return true;
   if (p->ids_64 != 0 && p->ids_64 != 1) return true;
@@ -74,7 +75,8 @@ int argus_embedding(const argus_embedding_t* p, const void* table, void* out, vo
 }
 
 size_t argus_embedding_bwd_workspace(const argus_embedding_t* p) {
-  if (!p || p->n_tokens < 0 || p->n_tokens > (1 << 28) || p->dim < 1) return 0;
+  if (!p || p->n_tokens < 0 || p->n_tokens > (1 << 27) || p->n_vocab < 1 || p->dim < 1 || p->dim > (1 << 16))
+    return 0;
   return embedding_bwd_workspace_bytes(*p);
 }
 

@@ -34,6 +34,17 @@ __device__ __forceinline__ void store_vec(T* p, const Vec<T, N>& v) {
   __builtin_memcpy(p, &v, sizeof(v));
 }
 
+// Past the caches: for large outputs that are written once and not read here.
+template <int N, typename T>
+__device__ __forceinline__ void stream_vec(T* p, const Vec<T, N>& v) {
+  if constexpr (sizeof(v) == 16) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+  } else {
+    store_vec<N>(p, v);
+  }
+}
+
 // Elements [i, i + N) of a row of n: whole vectors, and the elements that
 // exist of the one across the row's end (the others are 0).
 template <int N, typename T>
@@ -53,6 +64,12 @@ __device__ __forceinline__ void store_row(T* row, int i, int n, const Vec<T, N>&
 #pragma unroll
   for (int j = 0; j < N; ++j)
     if (i + j < n) row[i + j] = v.e[j];
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void stream_row(T* row, int i, int n, const Vec<T, N>& v) {
+  if (i + N <= n) stream_vec<N>(row + i, v);
+  else store_row<N>(row, i, n, v);
 }
 
 template <int CTRL>
@@ -75,13 +92,14 @@ __device__ __forceinline__ float row_sum(float v) {
   v += dpp_f32<kMirror>(v);
   return v;
 }
-__device__ __forceinline__ float wave_sum_f32(float v) {
-  v = row_sum(v);
+// Sum over the four rows of a wavefront, lane by lane, in every row.
+__device__ __forceinline__ float rows_sum(float v) {
   auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
   v = __builtin_bit_cast(float, (uint32_t)a[0]) + __builtin_bit_cast(float, (uint32_t)a[1]);
   auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
   return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
 }
+__device__ __forceinline__ float wave_sum_f32(float v) { return rows_sum(row_sum(v)); }
 
 // Host side: calls fn with a value of the element type.
 template <typename F>

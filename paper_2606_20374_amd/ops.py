@@ -14,7 +14,7 @@ from typing import Optional
 
 import torch
 
-from .argus import ArgusError, _check, _ptr, _stream, lib
+from .argus import ArgusError, _check, _ptr, lib
 
 DEV_TOKEN_RANGE, DEV_LOGITS = 512, 1024
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -99,6 +99,12 @@ def _need(t: torch.Tensor, shape: tuple, dtype, what: str):
 
 def _empty(shape, dtype, device):
     return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _stream(device) -> int:
+    # the current stream's handle alone: a torch Stream object costs more than
+    # a small operator's launches
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _space(out: dict, need: int, device):
@@ -217,11 +223,12 @@ def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: 
 
 # -------------------------------------------------------------------- balance
 def alloc_balance(n_tokens: int, n_experts: int, top_k: int, device="cuda") -> dict:
-    return {"expert": _empty((n_tokens, top_k), torch.int32, device),
-            "gate": _empty((n_tokens, top_k), torch.float32, device), "lse": _empty(n_tokens, torch.float32, device),
-            "count": _empty(n_experts, torch.int32, device), "prob": _empty(n_experts, torch.float32, device),
-            "n_valid": _empty(1, torch.int32, device), "loss": _empty(1, torch.float32, device),
-            "dev_status": _empty(1, torch.int32, device)}
+    # two allocations in place of eight: a small router's time is its host time
+    nk = n_tokens * top_k
+    gate, lse, prob, loss = _empty(nk + n_tokens + n_experts + 1, torch.float32, device).split([nk, n_tokens, n_experts, 1])
+    expert, count, n_valid, status = _empty(nk + n_experts + 2, torch.int32, device).split([nk, n_experts, 1, 1])
+    return {"expert": expert.view(n_tokens, top_k), "gate": gate.view(n_tokens, top_k), "lse": lse, "count": count,
+            "prob": prob, "n_valid": n_valid, "loss": loss, "dev_status": status}
 
 
 def balance(logits: torch.Tensor, top_k: int, mask: Optional[torch.Tensor] = None, alpha: float = 0.01,

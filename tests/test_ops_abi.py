@@ -25,7 +25,7 @@ def _embedding(**kw):
 
 
 @pytest.mark.parametrize("kw", [dict(ids=None), dict(ids=P + 4), dict(n_tokens=-1), dict(n_tokens=2**28 + 1), dict(ids_64=2),
-                                dict(n_vocab=0), dict(n_vocab=2**27 + 1), dict(dim=0), dict(dtype=3), dict(dtype=-1),
+                                dict(n_vocab=0), dict(n_vocab=2**27 + 1), dict(dim=0), dict(dim=65_537), dict(dtype=3), dict(dtype=-1),
                                 dict(scale=float("nan")), dict(scale=float("inf")), dict(row_stride=-1)])
 def test_embedding_refuses(kw):
     p = _embedding(**kw)
