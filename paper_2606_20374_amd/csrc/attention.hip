@@ -55,8 +55,9 @@ template <int DP, int NQ>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   constexpr int kRows = 4 * 32 * NQ;  // queries of a workgroup
   constexpr int KS = DP / 16, DT = DP / 32;
-  __shared__ __align__(16) __bf16 kt[2][kKeys * DP];
-  __shared__ __align__(16) __bf16 vt[2][kKeys * DP];
+  // four arrays, not two of two: reads of one tile then do not wait for the
+  // loads of the next
+  __shared__ __align__(16) __bf16 kt0[kKeys * DP], kt1[kKeys * DP], vt0[kKeys * DP], vt1[kKeys * DP];
   if (a.d.bad && *a.d.bad) return fill_empty(a);
   const int item = (int)xcd_item(blockIdx.x, gridDim.x);
   const int G = a.H / a.N, per = a.slots * G, n = item / per, rest = item % per;
@@ -101,22 +102,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   const int tiles = (nk + kKeys - 1) / kKeys;
   const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
   const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
-  Stage<DP, kKeys, kThreads> sk, sv;
-  auto load = [&](int t) {
+  const TileLoad<DP, kKeys, kThreads> lk(a.k_tok, a.D), lv(a.v_tok, a.D);
+  auto load = [&](int t, __bf16* K, __bf16* V) __attribute__((always_inline)) {
     const int64_t first = (int64_t)t * kKeys;
-    sk.load(rows_rsrc(kb + first * a.k_tok, doc.nk - first, a.k_tok, a.D), 0, a.k_tok, a.D);
-    sv.load(rows_rsrc(vb + first * a.v_tok, doc.nk - first, a.v_tok, a.D), 0, a.v_tok, a.D);
+    lk.load(rows_rsrc(kb + first * a.k_tok, doc.nk - first, a.k_tok, a.D), K);
+    lv.load(rows_rsrc(vb + first * a.v_tok, doc.nk - first, a.v_tok, a.D), V);
   };
-  if (tiles > 0) {
-    load(0);
-    sk.store(kt[0]);
-    sv.store(vt[0]);
-  }
-  __syncthreads();
-  for (int t = 0; t < tiles; ++t) {
-    const int cur = t & 1;
-    if (t + 1 < tiles) load(t + 1);
-    const __bf16 *K = kt[cur], *V = vt[cur];
+  auto step = [&](int t, const __bf16* K, const __bf16* V, __bf16* next_k, __bf16* next_v)
+                  __attribute__((always_inline)) {
+    if (t + 1 < tiles) load(t + 1, next_k, next_v);
     const int key0 = t * kKeys;
     f32x16 s[NQ][2];
 #pragma unroll
@@ -196,11 +190,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
           for (int u = 0; u < NQ; ++u) acc[u][d] = mfma(va, p[u], acc[u][d]);
         }
       }
-    if (t + 1 < tiles) {
-      sk.store(kt[cur ^ 1]);
-      sv.store(vt[cur ^ 1]);
-    }
+    wait_loads();
     __syncthreads();
+  };
+  if (tiles > 0) load(0, kt0, vt0);
+  wait_loads();
+  __syncthreads();
+  for (int t = 0; t < tiles; t += 2) {
+    step(t, kt0, vt0, kt1, vt1);
+    if (t + 1 < tiles) step(t + 1, kt1, vt1, kt0, vt0);
   }
 #pragma unroll
   for (int u = 0; u < NQ; ++u) {

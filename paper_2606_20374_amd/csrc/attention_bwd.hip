@@ -108,9 +108,10 @@ __device__ __forceinline__ void write_rows(__bf16* row, const f32x16 (&x)[DP / 3
 template <int DP>
 __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  __shared__ __align__(16) __bf16 qt[2][kStep * DP];
-  __shared__ __align__(16) __bf16 gt[2][kStep * DP];
-  __shared__ __align__(16) float ls[2][kStep], ds[2][kStep];
+  // arrays of their own, so that reads of one tile do not wait for the loads
+  // of the next
+  __shared__ __align__(16) __bf16 qt0[kStep * DP], qt1[kStep * DP], gt0[kStep * DP], gt1[kStep * DP];
+  __shared__ __align__(16) float st0[2 * kStep], st1[2 * kStep];  // lse, then delta
   if (a.d.bad && *a.d.bad) {
     fill_zero(a.dk, a.d.n_k * a.N * a.D);
     fill_zero(a.dv, a.d.n_k * a.N * a.D);
@@ -136,13 +137,13 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
   int first = 0;
   if (a.causal && row0 > shift) first = (row0 - shift) / kStep * kStep;
   const int per = first < doc.nq ? (doc.nq - first + kStep - 1) / kStep : 0, tiles = per * G;
-  Stage<DP, kStep, kThreads> sq, sg;
-  float stat = 0;
   const int64_t o_tok = (int64_t)a.H * a.D;
-  auto load = [&](int t) {
+  const TileLoad<DP, kStep, kThreads> lq(a.q_tok, a.D), lg(o_tok, a.D);
+  float stat = 0;
+  auto load = [&](int t, __bf16* Q, __bf16* GO) __attribute__((always_inline)) {
     const int h = n * G + t / per, q0 = first + t % per * kStep;
-    sq.load(rows_rsrc(a.q + (doc.q0 + q0) * a.q_tok + (int64_t)h * a.q_head, doc.nq - q0, a.q_tok, a.D), 0, a.q_tok, a.D);
-    sg.load(rows_rsrc(a.go + (doc.q0 + q0) * o_tok + (int64_t)h * a.D, doc.nq - q0, o_tok, a.D), 0, o_tok, a.D);
+    lq.load(rows_rsrc(a.q + (doc.q0 + q0) * a.q_tok + (int64_t)h * a.q_head, doc.nq - q0, a.q_tok, a.D), Q);
+    lg.load(rows_rsrc(a.go + (doc.q0 + q0) * o_tok + (int64_t)h * a.D, doc.nq - q0, o_tok, a.D), GO);
     if (threadIdx.x < 2 * kStep) {
       const int i = threadIdx.x & (kStep - 1);
       const bool is_lse = threadIdx.x < kStep;
@@ -150,20 +151,15 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
       if (q0 + i < doc.nq) stat = (is_lse ? a.lse2 : a.delta)[(int64_t)h * a.d.n_q + doc.q0 + q0 + i];
     }
   };
-  auto put = [&](int b) {
-    sq.store(qt[b]);
-    sg.store(gt[b]);
-    if (threadIdx.x < kStep) ls[b][threadIdx.x] = stat;
-    else if (threadIdx.x < 2 * kStep) ds[b][threadIdx.x - kStep] = stat;
+  auto put = [&](float* st) __attribute__((always_inline)) {
+    if (threadIdx.x < 2 * kStep) st[threadIdx.x] = stat;
+    wait_loads();
+    __syncthreads();
   };
-  if (tiles > 0) {
-    load(0);
-    put(0);
-  }
-  __syncthreads();
-  for (int t = 0; t < tiles; ++t) {
-    const int cur = t & 1, q0 = first + t % per * kStep;
-    if (t + 1 < tiles) load(t + 1);
+  auto step = [&](int t, const __bf16* Q, const __bf16* GO, const float* st, __bf16* next_q, __bf16* next_g,
+                  float* next_st) __attribute__((always_inline)) {
+    const int q0 = first + t % per * kStep;
+    if (t + 1 < tiles) load(t + 1, next_q, next_g);
 #pragma unroll
     for (int b = 0; b < kStep / 32; ++b) {
       f32x16 s, dp;
@@ -171,14 +167,14 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
       for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = mfma(read_rows<DP>(qt[cur], 32 * b, ks), kf[ks], s);
-        dp = mfma(read_rows<DP>(gt[cur], 32 * b, ks), vf[ks], dp);
+        s = mfma(read_rows<DP>(Q, 32 * b, ks), kf[ks], s);
+        dp = mfma(read_rows<DP>(GO, 32 * b, ks), vf[ks], dp);
       }
       const bool edge = key0 + 32 > doc.nk || (a.causal && (int64_t)key0 + 31 > (int64_t)q0 + 32 * b + shift);
 #pragma unroll
       for (int i4 = 0; i4 < 16; i4 += 4) {
         const int r = 32 * b + 2 * i4 + 4 * half;
-        const float4 l4 = *(const float4*)&ls[cur][r], d4 = *(const float4*)&ds[cur][r];
+        const float4 l4 = *(const float4*)&st[r], d4 = *(const float4*)&st[kStep + r];
         const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -197,13 +193,18 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
         const bf16x8 p = as_operand(s, k2), d = as_operand(dp, k2);
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-          dv[c] = mfma(read_cols<DP>(gt[cur], 32 * b + 16 * k2, 32 * c), p, dv[c]);
-          dk[c] = mfma(read_cols<DP>(qt[cur], 32 * b + 16 * k2, 32 * c), d, dk[c]);
+          dv[c] = mfma(read_cols<DP>(GO, 32 * b + 16 * k2, 32 * c), p, dv[c]);
+          dk[c] = mfma(read_cols<DP>(Q, 32 * b + 16 * k2, 32 * c), d, dk[c]);
         }
       }
     }
-    if (t + 1 < tiles) put(cur ^ 1);
-    __syncthreads();
+    put(next_st);
+  };
+  if (tiles > 0) load(0, qt0, gt0);
+  put(st0);
+  for (int t = 0; t < tiles; t += 2) {
+    step(t, qt0, gt0, st0, qt1, gt1, st1);
+    if (t + 1 < tiles) step(t + 1, qt1, gt1, st1, qt0, gt0, st0);
   }
   if (key < doc.nk) {
     const int64_t row = ((doc.k0 + key) * a.N + n) * a.D;
@@ -213,10 +214,9 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
 }
 
 template <int DP>
-__global__ __launch_bounds__(kThreads) void attn_dq(BwdArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  __shared__ __align__(16) __bf16 kt[2][kStep * DP];
-  __shared__ __align__(16) __bf16 vt[2][kStep * DP];
+  __shared__ __align__(16) __bf16 kt0[kStep * DP], kt1[kStep * DP], vt0[kStep * DP], vt1[kStep * DP];
   if (a.d.bad && *a.d.bad) return fill_zero(a.dq, a.d.n_q * a.H * a.D);
   const int item = (int)xcd_item(blockIdx.x, gridDim.x);
   const int G = a.H / a.N, per = a.slots * G, n = item / per, rest = item % per;
@@ -246,23 +246,18 @@ __global__ __launch_bounds__(kThreads) void attn_dq(BwdArgs a) {
   const int nk = seen < 0 ? 0 : seen < doc.nk ? (int)seen : doc.nk, tiles = (nk + kStep - 1) / kStep;
   const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
   const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
-  Stage<DP, kStep, kThreads> sk, sv;
-  auto load = [&](int t) {
+  const TileLoad<DP, kStep, kThreads> lk(a.k_tok, a.D), lv(a.v_tok, a.D);
+  auto load = [&](int t, __bf16* K, __bf16* V) __attribute__((always_inline)) {
     const int64_t f = (int64_t)t * kStep;
-    sk.load(rows_rsrc(kb + f * a.k_tok, doc.nk - f, a.k_tok, a.D), 0, a.k_tok, a.D);
-    sv.load(rows_rsrc(vb + f * a.v_tok, doc.nk - f, a.v_tok, a.D), 0, a.v_tok, a.D);
+    lk.load(rows_rsrc(kb + f * a.k_tok, doc.nk - f, a.k_tok, a.D), K);
+    lv.load(rows_rsrc(vb + f * a.v_tok, doc.nk - f, a.v_tok, a.D), V);
   };
-  if (tiles > 0) {
-    load(0);
-    sk.store(kt[0]);
-    sv.store(vt[0]);
-  }
-  __syncthreads();
   int64_t lim = a.causal ? (int64_t)q + shift : doc.nk - 1;
   if (lim > doc.nk - 1) lim = doc.nk - 1;
-  for (int t = 0; t < tiles; ++t) {
-    const int cur = t & 1, key0 = t * kStep;
-    if (t + 1 < tiles) load(t + 1);
+  auto step = [&](int t, const __bf16* K, const __bf16* V, __bf16* next_k, __bf16* next_v)
+                  __attribute__((always_inline)) {
+    const int key0 = t * kStep;
+    if (t + 1 < tiles) load(t + 1, next_k, next_v);
 #pragma unroll
     for (int b = 0; b < kStep / 32; ++b) {
       f32x16 s, dp;
@@ -270,8 +265,8 @@ __global__ __launch_bounds__(kThreads) void attn_dq(BwdArgs a) {
       for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = mfma(read_rows<DP>(kt[cur], 32 * b, ks), qf[ks], s);
-        dp = mfma(read_rows<DP>(vt[cur], 32 * b, ks), gf[ks], dp);
+        s = mfma(read_rows<DP>(K, 32 * b, ks), qf[ks], s);
+        dp = mfma(read_rows<DP>(V, 32 * b, ks), gf[ks], dp);
       }
       const bool edge = key0 + 32 * b + 32 > doc.nk || (a.causal && (int64_t)key0 + 32 * b + 31 > (int64_t)q0 + shift);
 #pragma unroll
@@ -283,14 +278,18 @@ __global__ __launch_bounds__(kThreads) void attn_dq(BwdArgs a) {
       for (int k2 = 0; k2 < 2; ++k2) {
         const bf16x8 d = as_operand(dp, k2);
 #pragma unroll
-        for (int c = 0; c < DT; ++c) acc[c] = mfma(read_cols<DP>(kt[cur], 32 * b + 16 * k2, 32 * c), d, acc[c]);
+        for (int c = 0; c < DT; ++c) acc[c] = mfma(read_cols<DP>(K, 32 * b + 16 * k2, 32 * c), d, acc[c]);
       }
     }
-    if (t + 1 < tiles) {
-      sk.store(kt[cur ^ 1]);
-      sv.store(vt[cur ^ 1]);
-    }
+    wait_loads();
     __syncthreads();
+  };
+  if (tiles > 0) load(0, kt0, vt0);
+  wait_loads();
+  __syncthreads();
+  for (int t = 0; t < tiles; t += 2) {
+    step(t, kt0, vt0, kt1, vt1);
+    if (t + 1 < tiles) step(t + 1, kt1, vt1, kt0, vt0);
   }
   if (q < doc.nq) write_rows<DP>(a.dq + ((doc.q0 + q) * a.H + h) * a.D, acc, a.scale, a.D);
 }

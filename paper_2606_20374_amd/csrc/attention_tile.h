@@ -82,30 +82,36 @@ __device__ __forceinline__ int swz(int r, int c) {
   return c ^ f;
 }
 
-// A tile of ROWS rows on its way through registers.
+// Loads of a tile of ROWS rows straight into LDS, 16 bytes a lane. A
+// wavefront's lanes write consecutive places, so the exchange of pieces is
+// made on the global side: the lane of place c reads piece swz(row, c).
 template <int DP, int ROWS, int THREADS>
-struct Stage {
+struct TileLoad {
   static constexpr int PIECES = DP / 8;
   static constexpr int N = ROWS * PIECES / THREADS;
   static_assert(ROWS * PIECES % THREADS == 0);
-  u32x4 v[N];
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int first, int64_t stride, int dim) {
+  int off[N];  // bytes from the tile's first row
+  __device__ __forceinline__ TileLoad(int64_t stride, int dim) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = at % PIECES;
+      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = swz<DP>(row, at % PIECES);
       // pieces past the head dimension read as zeros like rows past the end
-      const int off = c * 8 < dim ? (int)(((int64_t)(first + row) * stride + c * 8) * 2) : 0x7ffffff0;
-      v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+      off[i] = c * 8 < dim ? (int)((row * stride + c * 8) * 2) : 0x7ffffff0;
     }
   }
-  __device__ __forceinline__ void store(__bf16* tile) const {
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __bf16* tile) const {
+#ifdef __HIP_DEVICE_COMPILE__  // the host's pass has no 16-byte form and drops kernels that name it
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = at % PIECES;
-      *(u32x4*)(tile + row * DP + swz<DP>(row, c) * 8) = v[i];
-    }
+    for (int i = 0; i < N; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          r, (__attribute__((address_space(3))) void*)(tile + (i * THREADS + wave * 64) * 8), 16, off[i], 0, 0, 0);
+#endif
   }
 };
+
+// All of this wavefront's loads have arrived.
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 // A operand: rows r0 + lane % 32, k = 16 ks + 8 h + j.
 template <int DP>
