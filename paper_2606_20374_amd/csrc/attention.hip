@@ -97,11 +97,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   }
   // keys that some query of the workgroup sees
   int last_row = row0 + kRows - 1 < doc.nq - 1 ? row0 + kRows - 1 : doc.nq - 1;
-  int64_t seen = a.causal ? (int64_t)last_row + shift + 1 : doc.nk;
-  const int nk = seen < 0 ? 0 : seen < doc.nk ? (int)seen : doc.nk;
+  const int seen = a.causal ? last_row + shift + 1 : doc.nk;
+  const int nk = seen < 0 ? 0 : seen < doc.nk ? seen : doc.nk;
   const int tiles = (nk + kKeys - 1) / kKeys;
   const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
   const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
+  Reader<DP> rd;
   const TileLoad<DP, kKeys, kThreads> lk(a.k_tok, a.D), lv(a.v_tok, a.D);
   auto load = [&](int t, __bf16* K, __bf16* V) __attribute__((always_inline)) {
     const int64_t first = (int64_t)t * kKeys;
@@ -111,6 +112,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   auto step = [&](int t, const __bf16* K, const __bf16* V, __bf16* next_k, __bf16* next_v)
                   __attribute__((always_inline)) {
     if (t + 1 < tiles) load(t + 1, next_k, next_v);
+    rd.fresh();
     const int key0 = t * kKeys;
     f32x16 s[NQ][2];
 #pragma unroll
@@ -121,18 +123,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
         for (int i = 0; i < 16; ++i) s[u][b][i] = 0;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 ka = read_rows<DP>(K, 32 * b, ks);
+        const bf16x8 ka = rd.rows(K, 32 * b, ks);
 #pragma unroll
         for (int u = 0; u < NQ; ++u) s[u][b] = mfma(ka, qf[u][ks], s[u][b]);
       }
     }
     // the tiles at the causal edge and at the document's end
-    const bool edge = key0 + kKeys > doc.nk || (a.causal && (int64_t)key0 + kKeys - 1 > (int64_t)q0 + shift);
+    const bool edge = key0 + kKeys > doc.nk || (a.causal && key0 + kKeys - 1 > q0 + shift);
     if (edge) {
 #pragma unroll
       for (int u = 0; u < NQ; ++u) {
-        const int64_t q = q0 + u * 32 + (lane & 31);
-        int64_t lim = a.causal ? q + shift : doc.nk - 1;
+        const int q = q0 + u * 32 + (lane & 31);
+        int lim = a.causal ? q + shift : doc.nk - 1;
         if (lim > doc.nk - 1) lim = doc.nk - 1;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
         for (int u = 0; u < NQ; ++u) p[u] = as_operand(s[u][b], k2);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const bf16x8 va = read_cols<DP>(V, 32 * b + 16 * k2, 32 * d);
+          const bf16x8 va = rd.cols(V, 32 * b + 16 * k2, 32 * d);
 #pragma unroll
           for (int u = 0; u < NQ; ++u) acc[u][d] = mfma(va, p[u], acc[u][d]);
         }

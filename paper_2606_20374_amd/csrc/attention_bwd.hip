@@ -33,8 +33,7 @@ struct BwdArgs {
   const __bf16 *q, *k, *v, *o, *go;
   const float* lse;
   __bf16 *dq, *dk, *dv;
-  float* delta;  // [H][n_q]
-  float* lse2;   // [H][n_q]
+  float* stat;   // [H][n_q][2]: lse in units of log2, delta
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;
   int32_t H, N, D, causal, slots;
   float scale;
@@ -56,9 +55,8 @@ __global__ __launch_bounds__(256) void attn_prep(BwdArgs a) {
     if (lane == 0) {
       const int64_t t = i / a.H, at = (i - t * a.H) * a.d.n_q + t;
       const float l = a.lse[i];
-      a.delta[at] = s;
       // a query that sees nothing: exp2(s - infinity) = 0 for every key
-      a.lse2[at] = l > -__builtin_inff() ? l * kLog2e : __builtin_inff();
+      *(float2*)(a.stat + 2 * at) = make_float2(l > -__builtin_inff() ? l * kLog2e : __builtin_inff(), s);
     }
   }
 }
@@ -105,13 +103,20 @@ __device__ __forceinline__ void write_rows(__bf16* row, const f32x16 (&x)[DP / 3
     }
 }
 
+// Heads wider than 64 keep K in LDS, read anew for every step: with dK, dV, V
+// and K in registers only one wavefront fits a SIMD, which then waits for each
+// of its reads. Their steps are half as long, so that two workgroups fit a
+// CU's LDS.
 template <int DP>
-__global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
   constexpr int KS = DP / 16, DT = DP / 32;
+  constexpr bool kInLds = DP > 64;
+  constexpr int kQ = kInLds ? 32 : 64;  // queries of a step
   // arrays of their own, so that reads of one tile do not wait for the loads
   // of the next
-  __shared__ __align__(16) __bf16 qt0[kStep * DP], qt1[kStep * DP], gt0[kStep * DP], gt1[kStep * DP];
-  __shared__ __align__(16) float st0[2 * kStep], st1[2 * kStep];  // lse, then delta
+  __shared__ __align__(16) __bf16 qt0[kQ * DP], qt1[kQ * DP], gt0[kQ * DP], gt1[kQ * DP];
+  __shared__ __align__(16) __bf16 kt[kInLds ? kOwn * DP : 8];
+  __shared__ __align__(16) float st0[2 * kQ], st1[2 * kQ];  // lse and delta of each query
   if (a.d.bad && *a.d.bad) {
     fill_zero(a.dk, a.d.n_k * a.N * a.D);
     fill_zero(a.dv, a.d.n_k * a.N * a.D);
@@ -125,9 +130,10 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
   const int shift = doc.nk - doc.nq, key0 = row0 + w * 32, key = key0 + (lane & 31);
   const float sc = score_scale(a.scale);
-  bf16x8 kf[KS], vf[KS];
-  load_operand<DP>(kf, rows_rsrc(a.k + (doc.k0 + row0) * a.k_tok + (int64_t)n * a.k_head, doc.nk - row0, a.k_tok, a.D),
-                   w * 32 + (lane & 31), a.k_tok, a.D);
+  const auto src_k = rows_rsrc(a.k + (doc.k0 + row0) * a.k_tok + (int64_t)n * a.k_head, doc.nk - row0, a.k_tok, a.D);
+  bf16x8 kf[kInLds ? 1 : KS], vf[KS];
+  if constexpr (kInLds) TileLoad<DP, kOwn, kThreads>(a.k_tok, a.D).load(src_k, kt);
+  else load_operand<DP>(kf, src_k, w * 32 + (lane & 31), a.k_tok, a.D);
   load_operand<DP>(vf, rows_rsrc(a.v + (doc.k0 + row0) * a.v_tok + (int64_t)n * a.v_head, doc.nk - row0, a.v_tok, a.D),
                    w * 32 + (lane & 31), a.v_tok, a.D);
   f32x16 dk[DT], dv[DT];
@@ -135,57 +141,70 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
   clear<DP>(dv);
   // queries from the first that sees a key of the workgroup on
   int first = 0;
-  if (a.causal && row0 > shift) first = (row0 - shift) / kStep * kStep;
-  const int per = first < doc.nq ? (doc.nq - first + kStep - 1) / kStep : 0, tiles = per * G;
+  if (a.causal && row0 > shift) first = (row0 - shift) / kQ * kQ;
+  const int per = first < doc.nq ? (doc.nq - first + kQ - 1) / kQ : 0, tiles = per * G;
   const int64_t o_tok = (int64_t)a.H * a.D;
-  const TileLoad<DP, kStep, kThreads> lq(a.q_tok, a.D), lg(o_tok, a.D);
-  float stat = 0;
-  auto load = [&](int t, __bf16* Q, __bf16* GO) __attribute__((always_inline)) {
-    const int h = n * G + t / per, q0 = first + t % per * kStep;
-    lq.load(rows_rsrc(a.q + (doc.q0 + q0) * a.q_tok + (int64_t)h * a.q_head, doc.nq - q0, a.q_tok, a.D), Q);
-    lg.load(rows_rsrc(a.go + (doc.q0 + q0) * o_tok + (int64_t)h * a.D, doc.nq - q0, o_tok, a.D), GO);
-    if (threadIdx.x < 2 * kStep) {
-      const int i = threadIdx.x & (kStep - 1);
-      const bool is_lse = threadIdx.x < kStep;
-      stat = is_lse ? __builtin_inff() : 0.0f;
-      if (q0 + i < doc.nq) stat = (is_lse ? a.lse2 : a.delta)[(int64_t)h * a.d.n_q + doc.q0 + q0 + i];
+  Reader<DP> rd;
+  const TileLoad<DP, kQ, kThreads> lq(a.q_tok, a.D), lg(o_tok, a.D);
+  int lh = n * G, lt = 0;  // head and step of the next load
+  auto load = [&](__bf16* Q, __bf16* GO, float* st) __attribute__((always_inline)) {
+    const int q0 = first + lt * kQ;
+    lq.load(rows_rsrc(a.q + (doc.q0 + q0) * a.q_tok + (int64_t)lh * a.q_head, doc.nq - q0, a.q_tok, a.D), Q);
+    lg.load(rows_rsrc(a.go + (doc.q0 + q0) * o_tok + (int64_t)lh * a.D, doc.nq - q0, o_tok, a.D), GO);
+    // past the last query zeros: with do = 0 there, neither P nor dS counts
+    if (w < 2 * kQ / 64) {
+      const int64_t left = (int64_t)(doc.nq - q0) * 8;
+      const auto r = __builtin_amdgcn_make_buffer_rsrc(a.stat + 2 * ((int64_t)lh * a.d.n_q + doc.q0 + q0), (short)0,
+                                                       (int)(left < 8 * kQ ? left : 8 * kQ), 0x00020000);
+      load_words(r, st + 64 * __builtin_amdgcn_readfirstlane(w), threadIdx.x * 4);
+    }
+    if (++lt == per) {
+      lt = 0;
+      ++lh;
     }
   };
-  auto put = [&](float* st) __attribute__((always_inline)) {
-    if (threadIdx.x < 2 * kStep) st[threadIdx.x] = stat;
+  auto arrive = [&]() __attribute__((always_inline)) {
     wait_loads();
     __syncthreads();
   };
+  int q0 = first;  // first query of the step
   auto step = [&](int t, const __bf16* Q, const __bf16* GO, const float* st, __bf16* next_q, __bf16* next_g,
                   float* next_st) __attribute__((always_inline)) {
-    const int q0 = first + t % per * kStep;
-    if (t + 1 < tiles) load(t + 1, next_q, next_g);
+    if (t + 1 < tiles) load(next_q, next_g, next_st);
+    rd.fresh();
+    Reader<DP> rk = rd;  // of the wavefront's own keys
 #pragma unroll
-    for (int b = 0; b < kStep / 32; ++b) {
+    for (int j = 0; j < 4; ++j) rk.row[j] += w * 32 * DP * 2;
+#pragma unroll
+    for (int b = 0; b < kQ / 32; ++b) {
       f32x16 s, dp;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = mfma(read_rows<DP>(Q, 32 * b, ks), kf[ks], s);
-        dp = mfma(read_rows<DP>(GO, 32 * b, ks), vf[ks], dp);
+        bf16x8 k;
+        if constexpr (kInLds) k = rk.rows(kt, 0, ks);
+        else k = kf[ks];
+        s = mfma(rd.rows(Q, 32 * b, ks), k, s);
+        dp = mfma(rd.rows(GO, 32 * b, ks), vf[ks], dp);
       }
-      const bool edge = key0 + 32 > doc.nk || (a.causal && (int64_t)key0 + 31 > (int64_t)q0 + 32 * b + shift);
+      if (key0 + 32 > doc.nk || (a.causal && key0 + 31 > q0 + 32 * b + shift)) {
+        // the first of the step's rows that sees the key, counted from row 4 half on
+        int from = a.causal ? key - shift - q0 - 32 * b - 4 * half : -64;
+        if (key >= doc.nk) from = 64;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 >= from ? s[i] : -__builtin_inff();
+      }
 #pragma unroll
       for (int i4 = 0; i4 < 16; i4 += 4) {
         const int r = 32 * b + 2 * i4 + 4 * half;
-        const float4 l4 = *(const float4*)&st[r], d4 = *(const float4*)&st[kStep + r];
-        const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
+        const float4 a4 = *(const float4*)&st[2 * r], b4 = *(const float4*)&st[2 * r + 4];
+        const float lv[4] = {a4.x, a4.z, b4.x, b4.z}, dl[4] = {a4.y, a4.w, b4.y, b4.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float p = exp2_fast(s[i4 + j] * sc - lv[j]);
           s[i4 + j] = p;
           dp[i4 + j] = p * (dp[i4 + j] - dl[j]);
-          if (edge) {
-            const bool see = key < doc.nk && (!a.causal || (int64_t)key <= (int64_t)q0 + r + j + shift);
-            s[i4 + j] = see ? s[i4 + j] : 0.0f;
-            dp[i4 + j] = see ? dp[i4 + j] : 0.0f;
-          }
         }
       }
 #pragma unroll
@@ -193,15 +212,16 @@ __global__ __launch_bounds__(kThreads) void attn_dkv(BwdArgs a) {
         const bf16x8 p = as_operand(s, k2), d = as_operand(dp, k2);
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-          dv[c] = mfma(read_cols<DP>(GO, 32 * b + 16 * k2, 32 * c), p, dv[c]);
-          dk[c] = mfma(read_cols<DP>(Q, 32 * b + 16 * k2, 32 * c), d, dk[c]);
+          dv[c] = mfma(rd.cols(GO, 32 * b + 16 * k2, 32 * c), p, dv[c]);
+          dk[c] = mfma(rd.cols(Q, 32 * b + 16 * k2, 32 * c), d, dk[c]);
         }
       }
     }
-    put(next_st);
+    q0 = q0 + kQ < first + per * kQ ? q0 + kQ : first;
+    arrive();
   };
-  if (tiles > 0) load(0, qt0, gt0);
-  put(st0);
+  if (tiles > 0) load(qt0, gt0, st0);
+  arrive();
   for (int t = 0; t < tiles; t += 2) {
     step(t, qt0, gt0, st0, qt1, gt1, st1);
     if (t + 1 < tiles) step(t + 1, qt1, gt1, st1, qt0, gt0, st0);
@@ -236,28 +256,31 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
                    w * 32 + (lane & 31), o_tok, a.D);
   float lse2 = __builtin_inff(), delta = 0;
   if (q < doc.nq) {
-    lse2 = a.lse2[(int64_t)h * a.d.n_q + doc.q0 + q];
-    delta = a.delta[(int64_t)h * a.d.n_q + doc.q0 + q];
+    const float2 st = *(const float2*)(a.stat + 2 * ((int64_t)h * a.d.n_q + doc.q0 + q));
+    lse2 = st.x;
+    delta = st.y;
   }
   f32x16 acc[DT];
   clear<DP>(acc);
   const int last_row = row0 + kOwn - 1 < doc.nq - 1 ? row0 + kOwn - 1 : doc.nq - 1;
-  const int64_t seen = a.causal ? (int64_t)last_row + shift + 1 : doc.nk;
-  const int nk = seen < 0 ? 0 : seen < doc.nk ? (int)seen : doc.nk, tiles = (nk + kStep - 1) / kStep;
+  const int seen = a.causal ? last_row + shift + 1 : doc.nk;
+  const int nk = seen < 0 ? 0 : seen < doc.nk ? seen : doc.nk, tiles = (nk + kStep - 1) / kStep;
   const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
   const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
+  Reader<DP> rd;
   const TileLoad<DP, kStep, kThreads> lk(a.k_tok, a.D), lv(a.v_tok, a.D);
   auto load = [&](int t, __bf16* K, __bf16* V) __attribute__((always_inline)) {
     const int64_t f = (int64_t)t * kStep;
     lk.load(rows_rsrc(kb + f * a.k_tok, doc.nk - f, a.k_tok, a.D), K);
     lv.load(rows_rsrc(vb + f * a.v_tok, doc.nk - f, a.v_tok, a.D), V);
   };
-  int64_t lim = a.causal ? (int64_t)q + shift : doc.nk - 1;
+  int lim = a.causal ? q + shift : doc.nk - 1;
   if (lim > doc.nk - 1) lim = doc.nk - 1;
   auto step = [&](int t, const __bf16* K, const __bf16* V, __bf16* next_k, __bf16* next_v)
                   __attribute__((always_inline)) {
     const int key0 = t * kStep;
     if (t + 1 < tiles) load(t + 1, next_k, next_v);
+    rd.fresh();
 #pragma unroll
     for (int b = 0; b < kStep / 32; ++b) {
       f32x16 s, dp;
@@ -265,20 +288,21 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
       for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = mfma(read_rows<DP>(K, 32 * b, ks), qf[ks], s);
-        dp = mfma(read_rows<DP>(V, 32 * b, ks), gf[ks], dp);
+        s = mfma(rd.rows(K, 32 * b, ks), qf[ks], s);
+        dp = mfma(rd.rows(V, 32 * b, ks), gf[ks], dp);
       }
-      const bool edge = key0 + 32 * b + 32 > doc.nk || (a.causal && (int64_t)key0 + 32 * b + 31 > (int64_t)q0 + shift);
+      if (key0 + 32 * b + 32 > doc.nk || (a.causal && key0 + 32 * b + 31 > q0 + shift)) {
+        const int to = lim - key0 - 32 * b - 4 * half;  // the last key of the step that is seen
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        dp[i] = exp2_fast(s[i] * sc - lse2) * (dp[i] - delta);
-        if (edge) dp[i] = key0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4 <= lim ? dp[i] : 0.0f;
+        for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 <= to ? s[i] : -__builtin_inff();
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dp[i] = exp2_fast(s[i] * sc - lse2) * (dp[i] - delta);
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         const bf16x8 d = as_operand(dp, k2);
 #pragma unroll
-        for (int c = 0; c < DT; ++c) acc[c] = mfma(read_cols<DP>(K, 32 * b + 16 * k2, 32 * c), d, acc[c]);
+        for (int c = 0; c < DT; ++c) acc[c] = mfma(rd.cols(K, 32 * b + 16 * k2, 32 * c), d, acc[c]);
       }
     }
     wait_loads();
@@ -297,7 +321,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
 }  // namespace
 
 size_t attention_bwd_workspace_bytes(const argus_attention_t& p) {
-  return 256 + 2 * align256((size_t)p.n_q * (size_t)p.n_heads * sizeof(float));
+  return 256 + align256((size_t)p.n_q * (size_t)p.n_heads * 2 * sizeof(float));
 }
 
 hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, const void* q, const void* k,
@@ -305,12 +329,9 @@ hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, con
                                 void* ws, hipStream_t st) {
   hipError_t e = launch_attn_check(p, (uint32_t*)ws, st);
   if (e != hipSuccess) return e;
-  const size_t part = align256((size_t)p.n_q * (size_t)p.n_heads * sizeof(float));
-  float* delta = (float*)((uint8_t*)ws + 256);
-  float* lse2 = (float*)((uint8_t*)ws + 256 + part);
   BwdArgs a{{p.q_off, p.k_off, p.n_docs, p.n_q, p.n_k, p.q_off ? (const uint32_t*)ws : nullptr},
             (const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (const __bf16*)o, (const __bf16*)d_o, lse,
-            (__bf16*)dq, (__bf16*)dk, (__bf16*)dv, delta, lse2,
+            (__bf16*)dq, (__bf16*)dk, (__bf16*)dv, (float*)((uint8_t*)ws + 256),
             p.q_tok, p.q_head, p.k_tok, p.k_head, p.v_tok, p.v_head,
             p.n_heads, p.n_kv_heads, p.head_dim, p.causal, 0, p.scale};
   const bool wide = p.head_dim > 64;

@@ -47,7 +47,7 @@ bool bad_attention(const argus_attention_t* p) {
   if (p->head_dim < 8 || p->head_dim > ARGUS_MAX_HEAD_DIM || p->head_dim % 8 != 0) return true;
   if ((p->causal != 0 && p->causal != 1) || p->dtype != ARGUS_BF16) return true;
   if (!(p->scale >= 0.0f) || !std::isfinite(p->scale)) return true;
-  if (p->n_q < 0 || p->n_q > INT32_MAX || p->n_k < 0 || p->n_k > INT32_MAX) return true;
+  if (p->n_q < 0 || p->n_q > (1 << 30) || p->n_k < 0 || p->n_k > (1 << 30)) return true;
   if ((p->q_off == nullptr) != (p->k_off == nullptr) || (!p->q_off && p->n_docs != 1)) return true;
   if (misaligned(p->q_off, 8) || misaligned(p->k_off, 8)) return true;
   // a tile's rows are addressed with 32-bit offsets from its first one
