@@ -145,6 +145,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
   const int per = first < doc.nq ? (doc.nq - first + kQ - 1) / kQ : 0, tiles = per * G;
   const int64_t o_tok = (int64_t)a.H * a.D;
   Reader<DP> rd;
+  const uint32_t own = w * 32 * DP * 2;  // the wavefront's keys in their tile
   const TileLoad<DP, kQ, kThreads> lq(a.q_tok, a.D), lg(o_tok, a.D);
   int lh = n * G, lt = 0;  // head and step of the next load
   auto load = [&](__bf16* Q, __bf16* GO, float* st) __attribute__((always_inline)) {
@@ -172,9 +173,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
                   float* next_st) __attribute__((always_inline)) {
     if (t + 1 < tiles) load(next_q, next_g, next_st);
     rd.fresh();
-    Reader<DP> rk = rd;  // of the wavefront's own keys
-#pragma unroll
-    for (int j = 0; j < 4; ++j) rk.row[j] += w * 32 * DP * 2;
 #pragma unroll
     for (int b = 0; b < kQ / 32; ++b) {
       f32x16 s, dp;
@@ -183,7 +181,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         bf16x8 k;
-        if constexpr (kInLds) k = rk.rows(kt, 0, ks);
+        if constexpr (kInLds) k = rd.rows(kt, 0, ks, own);
         else k = kf[ks];
         s = mfma(rd.rows(Q, 32 * b, ks), k, s);
         dp = mfma(rd.rows(GO, 32 * b, ks), vf[ks], dp);

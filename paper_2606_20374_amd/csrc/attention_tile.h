@@ -72,12 +72,16 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const __bf16* first,
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16*>(first), (short)0, (int)bytes, 0x00020000);
 }
 
-// Place of 16-byte piece c of row r of a tile: pieces are exchanged within a
-// row so that neither the rows' reads (8 rows, one piece) nor the transposed
-// ones (4 rows, two pieces) meet in a bank.
-// Only the low three bits of a piece's number are exchanged, so the others
-// stay additions, which the instructions' offsets hold.
-__device__ __forceinline__ int swz(int r, int c) { return c ^ (((r & 3) << 1) | ((r >> 2) & 1)); }
+// Place of 16-byte piece c of row r of a tile of DP elements a row: pieces are
+// exchanged within a row so that in neither kind of read two lanes of one
+// cycle (16 lanes of 16 bytes, 32 of 8: 64 banks) meet in a bank. Rows' reads
+// take one piece of 16 rows; the transposed ones four neighbouring pieces of
+// four rows. 64-element rows lie two to the banks' width.
+template <int DP>
+__device__ __forceinline__ int swz(int r, int c) {
+  if constexpr (DP == 128) return c ^ (((r & 3) << 2) | ((r >> 2) & 3));
+  else return c ^ (((r & 2) << 1) | ((r >> 2) & 3));
+}
 
 // Loads of a tile of ROWS rows straight into LDS, 16 bytes a lane. A
 // wavefront's lanes write consecutive places, so the exchange of pieces is
@@ -91,7 +95,7 @@ struct TileLoad {
   __device__ __forceinline__ TileLoad(int64_t stride, int dim) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = swz(row, at % PIECES);
+      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = swz<DP>(row, at % PIECES);
       // pieces past the head dimension read as zeros like rows past the end
       off[i] = c * 8 < dim ? (int)((row * stride + c * 8) * 2) : 0x7ffffff0;
     }
@@ -117,34 +121,38 @@ __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, float* word
 // All of this wavefront's loads have arrived.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
-// Reads of tiles of DP elements a row. Six byte offsets of the lane serve
+// Reads of tiles of DP elements a row. A few byte offsets of the lane serve
 // every tile: what else moves an operand is a constant, which the
 // instructions hold.
 template <int DP>
 struct Reader {
+  static constexpr int KS = DP / 16, DT = DP / 32;
   typedef __attribute__((address_space(3))) const char* lds_ptr;
   typedef __attribute__((address_space(3))) s16x4* tr_ptr;
-  uint32_t row[4], col[2];
+  uint32_t row[KS], col[DT][2];
   __device__ __forceinline__ Reader() {
     const int lane = threadIdx.x & 63, r = lane & 31, i = lane & 15, c = (lane & 16) + 4 * (i & 3);
     const int rc = 4 * (lane >> 5) + (i >> 2);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) row[j] = (r * DP + swz(r, 2 * j + (lane >> 5)) * 8) * 2;
+    for (int j = 0; j < KS; ++j) row[j] = (r * DP + swz<DP>(r, 2 * j + (lane >> 5)) * 8) * 2;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) col[j] = (rc * DP + swz(rc, (c >> 3) + 4 * j) * 8 + (c & 7)) * 2;
+    for (int j = 0; j < DT; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        col[j][u] = ((rc + 8 * u) * DP + swz<DP>(rc + 8 * u, (c >> 3) + 4 * j) * 8 + (c & 7)) * 2;
   }
   // Keeps the sums of offsets and constants out of registers: called once a
   // step, it hides that they are the same ones.
   __device__ __forceinline__ void fresh() {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(row[j]));
+    for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(row[j]));
 #pragma unroll
-    for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(col[j]));
+    for (int j = 0; j < DT; ++j) asm volatile("" : "+v"(col[j][0]), "+v"(col[j][1]));
   }
   // A (or B) operand: rows r0 + lane % 32, k = 16 ks + 8 h + j; r0 a multiple of 32.
-  __device__ __forceinline__ bf16x8 rows(const __bf16* tile, int r0, int ks) const {
+  __device__ __forceinline__ bf16x8 rows(const __bf16* tile, int r0, int ks, uint32_t more = 0) const {
     const lds_ptr p = (lds_ptr)(__attribute__((address_space(3))) const void*)tile;
-    return *(__attribute__((address_space(3))) const bf16x8*)(p + row[ks & 3] + (r0 * DP * 2 + (ks >> 2) * 128));
+    return *(__attribute__((address_space(3))) const bf16x8*)(p + (row[ks] + more) + r0 * DP * 2);
   }
   // A operand, transposed: row index of A = column c0 + lane % 32 of the tile,
   // k = rows r0 + 4 h + (0 .. 3) and r0 + 8 + 4 h + (0 .. 3); r0 a multiple of
@@ -152,9 +160,8 @@ struct Reader {
   // gets one column.
   __device__ __forceinline__ bf16x8 cols(const __bf16* tile, int r0, int c0) const {
     const lds_ptr p = (lds_ptr)(__attribute__((address_space(3))) const void*)tile;
-    const lds_ptr at = p + col[(c0 >> 5) & 1] + (r0 * DP * 2 + (c0 >> 6) * 128);
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)at);
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at + 8 * DP * 2));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + col[c0 / 32][0] + r0 * DP * 2));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + col[c0 / 32][1] + r0 * DP * 2));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
   }
