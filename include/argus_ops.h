@@ -192,7 +192,7 @@ typedef struct argus_attention {
   int32_t causal;      /* 0 or 1 */
   int32_t dtype;       /* ARGUS_BF16 */
   float scale;         /* finite, >= 0 */
-  int64_t n_q, n_k;    /* tokens of all documents, 0 .. 2^30 */
+  int64_t n_q, n_k;    /* tokens of all documents, 0 .. 2^30; (tokens / 128 + n_docs) times the heads below 2^23 */
   const int64_t* q_off; /* [n_docs + 1] or NULL (then k_off is NULL and n_docs 1) */
   const int64_t* k_off; /* [n_docs + 1] or NULL */
   /* strides of the token and head dimensions: multiples of 8, at least

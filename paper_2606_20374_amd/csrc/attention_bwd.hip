@@ -20,13 +20,14 @@
 namespace argus {
 using namespace attn;
 
-hipError_t launch_attn_check(const argus_attention_t& p, uint32_t* bad, hipStream_t st);
+size_t attn_plan_bytes(const argus_attention_t& p, bool both);
+hipError_t launch_attn_plan(const argus_attention_t& p, void* ws, Plan* queries, Plan* keys, hipStream_t st);
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kOwn = 128;   // rows a workgroup owns
-constexpr int kStep = 64;   // rows of the other side taken at a time
+constexpr int kOwn = kTile;  // rows a workgroup owns
+constexpr int kStep = 64;    // rows of the other side taken at a time
 
 struct BwdArgs {
   Docs d;
@@ -35,7 +36,8 @@ struct BwdArgs {
   __bf16 *dq, *dk, *dv;
   float* stat;   // [H][n_q][2]: lse in units of log2, delta
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;
-  int32_t H, N, D, causal, slots;
+  int32_t H, N, D, causal;
+  Plan plan;
   float scale;
 };
 
@@ -117,16 +119,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
   __shared__ __align__(16) __bf16 qt0[kQ * DP], qt1[kQ * DP], gt0[kQ * DP], gt1[kQ * DP];
   __shared__ __align__(16) __bf16 kt[kInLds ? kOwn * DP : 8];
   __shared__ __align__(16) float st0[2 * kQ], st1[2 * kQ];  // lse and delta of each query
-  if (a.d.bad && *a.d.bad) {
+  if (*a.d.bad) {
     fill_zero(a.dk, a.d.n_k * a.N * a.D);
     fill_zero(a.dv, a.d.n_k * a.N * a.D);
     return;
   }
-  const int item = (int)xcd_item(blockIdx.x, gridDim.x), n = item / a.slots, slot = item % a.slots, G = a.H / a.N;
-  int row0;
-  const int di = slot_doc(a.d.k_off, a.d.n_docs, kOwn, slot, row0);
+  int n, di, row0;
+  if (!my_tile(a.plan, a.N, n, di, row0)) return;
   const Doc doc = doc_at(a.d, di);
-  if (row0 >= doc.nk) return;
+  const int G = a.H / a.N;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
   const int shift = doc.nk - doc.nq, key0 = row0 + w * 32, key = key0 + (lane & 31);
   const float sc = score_scale(a.scale);
@@ -175,6 +176,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
     rd.fresh();
 #pragma unroll
     for (int b = 0; b < kQ / 32; ++b) {
+      // the wavefront owns no key, or none that a query of these sees
+      if (key0 >= doc.nk || (a.causal && q0 + 32 * b + 31 + shift < key0)) continue;
       f32x16 s, dp;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
@@ -235,14 +238,11 @@ template <int DP>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
   constexpr int KS = DP / 16, DT = DP / 32;
   __shared__ __align__(16) __bf16 kt0[kStep * DP], kt1[kStep * DP], vt0[kStep * DP], vt1[kStep * DP];
-  if (a.d.bad && *a.d.bad) return fill_zero(a.dq, a.d.n_q * a.H * a.D);
-  const int item = (int)xcd_item(blockIdx.x, gridDim.x);
-  const int G = a.H / a.N, per = a.slots * G, n = item / per, rest = item % per;
-  const int h = n * G + rest % G, slot = a.slots - 1 - rest / G;
-  int row0;
-  const int di = slot_doc(a.d.q_off, a.d.n_docs, kOwn, slot, row0);
+  if (*a.d.bad) return fill_zero(a.dq, a.d.n_q * a.H * a.D);
+  int h, di, row0;
+  if (!my_tile(a.plan, a.H, h, di, row0)) return;
   const Doc doc = doc_at(a.d, di);
-  if (row0 >= doc.nq) return;
+  const int n = h / (a.H / a.N);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
   const int q0 = row0 + w * 32, q = q0 + (lane & 31), shift = doc.nk - doc.nq;
   const float sc = score_scale(a.scale);
@@ -281,6 +281,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
     rd.fresh();
 #pragma unroll
     for (int b = 0; b < kStep / 32; ++b) {
+      // the wavefront owns no query, or none that sees a key of these
+      if (q0 >= doc.nq || (a.causal && key0 + 32 * b > q0 + 31 + shift)) continue;
       f32x16 s, dp;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0;
@@ -319,36 +321,34 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
 }  // namespace
 
 size_t attention_bwd_workspace_bytes(const argus_attention_t& p) {
-  return 256 + align256((size_t)p.n_q * (size_t)p.n_heads * 2 * sizeof(float));
+  return attn_plan_bytes(p, true) + align256((size_t)p.n_q * (size_t)p.n_heads * 2 * sizeof(float));
 }
 
 hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, const void* q, const void* k,
                                 const void* v, const void* o, const float* lse, void* dq, void* dk, void* dv,
                                 void* ws, hipStream_t st) {
-  hipError_t e = launch_attn_check(p, (uint32_t*)ws, st);
+  Plan queries, keys;
+  hipError_t e = launch_attn_plan(p, ws, &queries, &keys, st);
   if (e != hipSuccess) return e;
-  BwdArgs a{{p.q_off, p.k_off, p.n_docs, p.n_q, p.n_k, p.q_off ? (const uint32_t*)ws : nullptr},
+  BwdArgs a{{p.q_off, p.k_off, p.n_docs, p.n_q, p.n_k, (const uint32_t*)ws},
             (const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (const __bf16*)o, (const __bf16*)d_o, lse,
-            (__bf16*)dq, (__bf16*)dk, (__bf16*)dv, (float*)((uint8_t*)ws + 256),
+            (__bf16*)dq, (__bf16*)dk, (__bf16*)dv, (float*)((uint8_t*)ws + attn_plan_bytes(p, true)),
             p.q_tok, p.q_head, p.k_tok, p.k_head, p.v_tok, p.v_head,
-            p.n_heads, p.n_kv_heads, p.head_dim, p.causal, 0, p.scale};
+            p.n_heads, p.n_kv_heads, p.head_dim, p.causal, keys, p.scale};
   const bool wide = p.head_dim > 64;
   if (p.n_q > 0) {
     const int64_t need = ceil_div(p.n_q * p.n_heads, 16), grid = need < 8192 ? need : 8192;
     hipLaunchKernelGGL(attn_prep, dim3((unsigned)grid), dim3(256), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  auto go = [&](auto kern, int64_t tokens, int64_t heads) {
-    if (tokens == 0) return hipSuccess;
-    const int64_t slots = p.q_off ? slots_of(tokens, kOwn, p.n_docs) : ceil_div(tokens, kOwn);
-    if (slots * heads > (1 << 23)) return hipErrorInvalidConfiguration;
-    a.slots = (int32_t)slots;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(slots * heads)), dim3(kThreads), 0, st, a);
+  auto go = [&](auto kern, int64_t heads) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.plan.n * heads)), dim3(kThreads), 0, st, a);
     return hipGetLastError();
   };
-  e = wide ? go(attn_dkv<128>, p.n_k, p.n_kv_heads) : go(attn_dkv<64>, p.n_k, p.n_kv_heads);
-  if (e != hipSuccess) return e;
-  return wide ? go(attn_dq<128>, p.n_q, p.n_heads) : go(attn_dq<64>, p.n_q, p.n_heads);
+  if (p.n_k > 0 && (e = wide ? go(attn_dkv<128>, p.n_kv_heads) : go(attn_dkv<64>, p.n_kv_heads)) != hipSuccess) return e;
+  a.plan = queries;
+  if (p.n_q == 0) return hipSuccess;
+  return wide ? go(attn_dq<128>, p.n_heads) : go(attn_dq<64>, p.n_heads);
 }
 
 }  // namespace argus

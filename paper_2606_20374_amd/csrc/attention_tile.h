@@ -44,25 +44,37 @@ __device__ __forceinline__ Doc doc_at(const Docs& d, int i) {
   return {q0, k0, (int32_t)(d.q_off[i + 1] - q0), (int32_t)(d.k_off[i + 1] - k0)};
 }
 
-// Tiles of `rows` rows over all documents without a table: document i has
-// the slots from off[i] / rows + i on, enough for its tiles, since
-// ceil((b - a) / rows) <= b / rows - a / rows + 1. Returns the document of a
-// slot and the tile's first row in it (which may lie past its end).
-__device__ __forceinline__ int slot_doc(const int64_t* off, int n_docs, int rows, int slot, int& first) {
-  int lo = 0, hi = n_docs - 1;
-  if (off) {
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if ((int)(off[mid] / rows) + mid <= slot) lo = mid;
-      else hi = mid - 1;
-    }
-    first = (slot - ((int)(off[lo] / rows) + lo)) * rows;
+// Workgroups own tiles of kTile rows of a document, queries or keys. The
+// plan lists them, those of long documents first (they would otherwise begin
+// when the others end); entries past the last tile have the document -1.
+// ceil((b - a) / kTile) <= b / kTile - a / kTile + 1, so tokens / kTile + 1 for
+// each document is enough.
+constexpr int kTile = 128;
+struct Plan {
+  const int2* tile;  // document, first row in it
+  int32_t n;         // entries, at least as many as tiles
+};
+inline int64_t plan_entries(int64_t tokens, int32_t n_docs) { return tokens / kTile + n_docs; }
+
+// Tile and head of this workgroup. Heads that divide evenly over the eight
+// XCDs (workgroups go to them in turn) stay on one each, neighbours together,
+// so that an XCD's L2 holds the keys and values of few heads.
+__device__ __forceinline__ bool my_tile(const Plan& plan, int heads, int& head, int& doc, int& row0) {
+  const int b = blockIdx.x;
+  int nth;
+  if (heads % 8 == 0) {
+    const int per = heads / 8;
+    nth = (b >> 3) / per;
+    head = (b & 7) * per + (b >> 3) % per;
   } else {
-    first = slot * rows;
+    nth = b / heads;
+    head = b % heads;
   }
-  return lo;
+  const int2 t = plan.tile[nth];
+  doc = __builtin_amdgcn_readfirstlane(t.x);
+  row0 = __builtin_amdgcn_readfirstlane(t.y);
+  return doc >= 0;
 }
-inline int64_t slots_of(int64_t tokens, int rows, int32_t n_docs) { return tokens / rows + n_docs; }
 
 // Rows [0, n) of a document's tile as a buffer: what lies past the last row
 // reads as zeros. `stride` in elements.
@@ -120,6 +132,17 @@ __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, float* word
 
 // All of this wavefront's loads have arrived.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// All but its last N, and all of its LDS reads; then the workgroup's other
+// wavefronts as well. A fence would wait for every load; this barrier orders
+// LDS alone, whose reads are waited for here and whose writes by loads above.
+template <int N>
+__device__ __forceinline__ void wait_but_last() {
+  static_assert(N < 64);
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4 << 14));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // Reads of tiles of DP elements a row. A few byte offsets of the lane serve
 // every tile: what else moves an operand is a constant, which the

@@ -50,6 +50,9 @@ bool bad_attention(const argus_attention_t* p) {
   if (p->n_q < 0 || p->n_q > (1 << 30) || p->n_k < 0 || p->n_k > (1 << 30)) return true;
   if ((p->q_off == nullptr) != (p->k_off == nullptr) || (!p->q_off && p->n_docs != 1)) return true;
   if (misaligned(p->q_off, 8) || misaligned(p->k_off, 8)) return true;
+  // one launch takes all tiles of all heads
+  if ((p->n_q / 128 + p->n_docs) * p->n_heads >= (1 << 23) || (p->n_k / 128 + p->n_docs) * p->n_kv_heads >= (1 << 23))
+    return true;
   // a tile's rows are addressed with 32-bit offsets from its first one
   for (int64_t x : {p->q_tok, p->k_tok, p->v_tok})
     if (x < p->head_dim || x % 8 != 0 || x > (1 << 21)) return true;

@@ -312,8 +312,7 @@ def _attention(q, k, v, q_off, k_off, causal, scale, status):
 
 def alloc_attention(n_q: int, n_heads: int, head_dim: int, device="cuda") -> dict:
     return {"o": _empty((n_q, n_heads, head_dim), torch.bfloat16, device),
-            "lse": _empty((n_q, n_heads), torch.float32, device), "dev_status": _empty(1, torch.int32, device),
-            "_workspace": _empty(256, torch.uint8, device)}
+            "lse": _empty((n_q, n_heads), torch.float32, device), "dev_status": _empty(1, torch.int32, device)}
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_off: Optional[torch.Tensor] = None,
