@@ -11,8 +11,10 @@
 //          they are.
 //   dq     a workgroup owns 128 queries and takes the keys through LDS:
 //          S^T = K Q^T keeps a query in one lane, dQ^T += K^T dS^T.
-// S and dP are computed in both: 7 products in place of 5, and no sum between
-// workgroups, so no atomics and a fixed order.
+// S and dP are computed in both: 7 products in place of 5, and no atomics:
+// sums have a fixed order. Where tiles and heads are few, several workgroups
+// share one (the queries of dkv's, the keys of dq's in equal parts) and write
+// 32-bit sums that a further launch adds in their order.
 #include "attention_tile.h"
 
 #pragma clang fp contract(fast)
@@ -38,6 +40,8 @@ struct BwdArgs {
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;
   int32_t H, N, D, causal;
   Plan plan;
+  int32_t parts;  // workgroups that share a tile and head
+  float* sums;    // parts > 1: [parts][rows][D] (dkv: of dk, then of dv)
   float scale;
 };
 
@@ -91,6 +95,36 @@ __device__ __forceinline__ void clear(f32x16 (&x)[DP / 32]) {
 
 // Writes a transposed accumulator: lane = row, registers = columns.
 template <int DP>
+__device__ __forceinline__ void write_sums(float* row, const f32x16 (&x)[DP / 32], int dim) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int at = 32 * d + 2 * i + 4 * half;
+      if (at < dim) *(float4*)(row + at) = make_float4(x[d][i], x[d][i + 1], x[d][i + 2], x[d][i + 3]);
+    }
+}
+
+// Adds the parts' sums in their order: n elements, eight to a thread.
+__global__ __launch_bounds__(256) void attn_join(const float* sums, int32_t parts, int64_t n, float scale, __bf16* out,
+                                                 const uint32_t* bad) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= n || *bad) return;  // n is a multiple of 8
+  float4 u = *(const float4*)(sums + i), v = *(const float4*)(sums + i + 4);
+  for (int p = 1; p < parts; ++p) {
+    const float4 a = *(const float4*)(sums + p * n + i), b = *(const float4*)(sums + p * n + i + 4);
+    u = make_float4(u.x + a.x, u.y + a.y, u.z + a.z, u.w + a.w);
+    v = make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w);
+  }
+  const float f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+  bf16x8 o;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) o[j] = (__bf16)(f[j] * scale);
+  *(bf16x8*)(out + i) = o;
+}
+
+template <int DP>
 __device__ __forceinline__ void write_rows(__bf16* row, const f32x16 (&x)[DP / 32], float f, int dim) {
   const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
@@ -124,10 +158,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
     fill_zero(a.dv, a.d.n_k * a.N * a.D);
     return;
   }
-  int n, di, row0;
-  if (!my_tile(a.plan, a.N, n, di, row0)) return;
+  int vn, di, row0;
+  if (!my_tile(a.plan, a.N * a.parts, vn, di, row0)) return;
   const Doc doc = doc_at(a.d, di);
-  const int G = a.H / a.N;
+  const int G = a.H / a.N, n = vn / a.parts, part = vn % a.parts;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
   const int shift = doc.nk - doc.nq, key0 = row0 + w * 32, key = key0 + (lane & 31);
   const float sc = score_scale(a.scale);
@@ -143,12 +177,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
   // queries from the first that sees a key of the workgroup on
   int first = 0;
   if (a.causal && row0 > shift) first = (row0 - shift) / kQ * kQ;
-  const int per = first < doc.nq ? (doc.nq - first + kQ - 1) / kQ : 0, tiles = per * G;
+  const int per = first < doc.nq ? (doc.nq - first + kQ - 1) / kQ : 0;
+  // this part's steps, of all heads' one after the other
+  const int begin = (int)((int64_t)per * G * part / a.parts), end = (int)((int64_t)per * G * (part + 1) / a.parts);
+  const int tiles = end - begin;
   const int64_t o_tok = (int64_t)a.H * a.D;
   Reader<DP> rd;
   const uint32_t own = w * 32 * DP * 2;  // the wavefront's keys in their tile
   const TileLoad<DP, kQ, kThreads> lq(a.q_tok, a.D), lg(o_tok, a.D);
-  int lh = n * G, lt = 0;  // head and step of the next load
+  int lh = n * G + (per ? begin / per : 0), lt = per ? begin % per : 0;  // head and step of the next load
   auto load = [&](__bf16* Q, __bf16* GO, float* st) __attribute__((always_inline)) {
     const int q0 = first + lt * kQ;
     lq.load(rows_rsrc(a.q + (doc.q0 + q0) * a.q_tok + (int64_t)lh * a.q_head, doc.nq - q0, a.q_tok, a.D), Q);
@@ -169,7 +206,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
     wait_loads();
     __syncthreads();
   };
-  int q0 = first;  // first query of the step
+  int q0 = first + lt * kQ;  // first query of the step
   auto step = [&](int t, const __bf16* Q, const __bf16* GO, const float* st, __bf16* next_q, __bf16* next_g,
                   float* next_st) __attribute__((always_inline)) {
     if (t + 1 < tiles) load(next_q, next_g, next_st);
@@ -228,9 +265,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
     if (t + 1 < tiles) step(t + 1, qt1, gt1, st1, qt0, gt0, st0);
   }
   if (key < doc.nk) {
-    const int64_t row = ((doc.k0 + key) * a.N + n) * a.D;
-    write_rows<DP>(a.dk + row, dk, a.scale, a.D);
-    write_rows<DP>(a.dv + row, dv, 1.0f, a.D);
+    const int64_t row = ((doc.k0 + key) * a.N + n) * a.D, all = a.d.n_k * a.N * a.D;
+    if (a.parts == 1) {
+      write_rows<DP>(a.dk + row, dk, a.scale, a.D);
+      write_rows<DP>(a.dv + row, dv, 1.0f, a.D);
+    } else {
+      write_sums<DP>(a.sums + part * all + row, dk, a.D);
+      write_sums<DP>(a.sums + (a.parts + part) * all + row, dv, a.D);
+    }
   }
 }
 
@@ -239,10 +281,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
   constexpr int KS = DP / 16, DT = DP / 32;
   __shared__ __align__(16) __bf16 kt0[kStep * DP], kt1[kStep * DP], vt0[kStep * DP], vt1[kStep * DP];
   if (*a.d.bad) return fill_zero(a.dq, a.d.n_q * a.H * a.D);
-  int h, di, row0;
-  if (!my_tile(a.plan, a.H, h, di, row0)) return;
+  int vh, di, row0;
+  if (!my_tile(a.plan, a.H * a.parts, vh, di, row0)) return;
   const Doc doc = doc_at(a.d, di);
-  const int n = h / (a.H / a.N);
+  const int h = vh / a.parts, part = vh % a.parts, n = h / (a.H / a.N);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
   const int q0 = row0 + w * 32, q = q0 + (lane & 31), shift = doc.nk - doc.nq;
   const float sc = score_scale(a.scale);
@@ -262,7 +304,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
   clear<DP>(acc);
   const int last_row = row0 + kOwn - 1 < doc.nq - 1 ? row0 + kOwn - 1 : doc.nq - 1;
   const int seen = a.causal ? last_row + shift + 1 : doc.nk;
-  const int nk = seen < 0 ? 0 : seen < doc.nk ? seen : doc.nk, tiles = (nk + kStep - 1) / kStep;
+  const int nk = seen < 0 ? 0 : seen < doc.nk ? seen : doc.nk, all_tiles = (nk + kStep - 1) / kStep;
+  const int begin = (int)((int64_t)all_tiles * part / a.parts), tiles = (int)((int64_t)all_tiles * (part + 1) / a.parts);
   const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
   const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
   Reader<DP> rd;
@@ -308,20 +351,56 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
     wait_loads();
     __syncthreads();
   };
-  if (tiles > 0) load(0, kt0, vt0);
+  if (begin < tiles) load(begin, kt0, vt0);
   wait_loads();
   __syncthreads();
-  for (int t = 0; t < tiles; t += 2) {
+  for (int t = begin; t < tiles; t += 2) {
     step(t, kt0, vt0, kt1, vt1);
     if (t + 1 < tiles) step(t + 1, kt1, vt1, kt0, vt0);
   }
-  if (q < doc.nq) write_rows<DP>(a.dq + ((doc.q0 + q) * a.H + h) * a.D, acc, a.scale, a.D);
+  if (q < doc.nq) {
+    const int64_t row = ((doc.q0 + q) * a.H + h) * a.D;
+    if (a.parts == 1) write_rows<DP>(a.dq + row, acc, a.scale, a.D);
+    else write_sums<DP>(a.sums + part * a.d.n_q * a.H * a.D + row, acc, a.D);
+  }
+}
+
+}  // namespace
+
+namespace {
+
+// Workgroups that share a tile: as many as make kEnough in all (two to a CU,
+// twice), while each still has kPart rows of a document of average length to
+// take. One document of 8,192, 8 heads of 128 that share one key head: 2,595
+// us unshared, 607 us shared; 32 heads over 8, two of 2,048: 456 and 306 us.
+// Sharing where there are 1,456 workgroups, or documents of 512, loses the
+// sums' traffic (13 packed documents: 232 us unshared, 298 with twice kEnough).
+constexpr int64_t kEnough = 1024, kPart = 512, kMostParts = 8;
+int32_t parts_of(int64_t own, int64_t other, int32_t n_docs, int64_t heads, int64_t heads_taken) {
+  const int64_t blocks = plan_entries(own, n_docs) * heads;
+  int64_t parts = ceil_div(kEnough, blocks), most = other / n_docs * heads_taken / kPart;
+  if (parts > most) parts = most;
+  if (parts > kMostParts) parts = kMostParts;
+  return parts < 1 ? 1 : (int32_t)parts;
+}
+struct Parts {
+  int32_t dkv, dq;
+  size_t bytes;
+};
+Parts parts_of(const argus_attention_t& p) {
+  Parts r;
+  r.dkv = parts_of(p.n_k, p.n_q, p.n_docs, p.n_kv_heads, p.n_heads / p.n_kv_heads);
+  r.dq = parts_of(p.n_q, p.n_k, p.n_docs, p.n_heads, 1);
+  const size_t kv = r.dkv > 1 ? (size_t)2 * r.dkv * (size_t)p.n_k * p.n_kv_heads * p.head_dim * 4 : 0;
+  const size_t q = r.dq > 1 ? (size_t)r.dq * (size_t)p.n_q * p.n_heads * p.head_dim * 4 : 0;
+  r.bytes = align256(kv > q ? kv : q);
+  return r;
 }
 
 }  // namespace
 
 size_t attention_bwd_workspace_bytes(const argus_attention_t& p) {
-  return attn_plan_bytes(p, true) + align256((size_t)p.n_q * (size_t)p.n_heads * 2 * sizeof(float));
+  return attn_plan_bytes(p, true) + align256((size_t)p.n_q * (size_t)p.n_heads * 2 * sizeof(float)) + parts_of(p).bytes;
 }
 
 hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, const void* q, const void* k,
@@ -330,11 +409,14 @@ hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, con
   Plan queries, keys;
   hipError_t e = launch_attn_plan(p, ws, &queries, &keys, st);
   if (e != hipSuccess) return e;
+  const Parts parts = parts_of(p);
+  uint8_t* stat = (uint8_t*)ws + attn_plan_bytes(p, true);
   BwdArgs a{{p.q_off, p.k_off, p.n_docs, p.n_q, p.n_k, (const uint32_t*)ws},
             (const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (const __bf16*)o, (const __bf16*)d_o, lse,
-            (__bf16*)dq, (__bf16*)dk, (__bf16*)dv, (float*)((uint8_t*)ws + attn_plan_bytes(p, true)),
+            (__bf16*)dq, (__bf16*)dk, (__bf16*)dv, (float*)stat,
             p.q_tok, p.q_head, p.k_tok, p.k_head, p.v_tok, p.v_head,
-            p.n_heads, p.n_kv_heads, p.head_dim, p.causal, keys, p.scale};
+            p.n_heads, p.n_kv_heads, p.head_dim, p.causal, keys, parts.dkv,
+            (float*)(stat + align256((size_t)p.n_q * (size_t)p.n_heads * 2 * sizeof(float))), p.scale};
   const bool wide = p.head_dim > 64;
   if (p.n_q > 0) {
     const int64_t need = ceil_div(p.n_q * p.n_heads, 16), grid = need < 8192 ? need : 8192;
@@ -342,13 +424,25 @@ hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, con
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   auto go = [&](auto kern, int64_t heads) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)(a.plan.n * heads)), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.plan.n * heads * a.parts)), dim3(kThreads), 0, st, a);
     return hipGetLastError();
   };
-  if (p.n_k > 0 && (e = wide ? go(attn_dkv<128>, p.n_kv_heads) : go(attn_dkv<64>, p.n_kv_heads)) != hipSuccess) return e;
-  a.plan = queries;
+  auto join = [&](int64_t n, int first, float scale, void* out) {
+    hipLaunchKernelGGL(attn_join, dim3((unsigned)ceil_div(n, 8 * 256)), dim3(256), 0, st, a.sums + first * n, a.parts, n,
+                       scale, (__bf16*)out, (const uint32_t*)ws);
+    return hipGetLastError();
+  };
+  if (p.n_k > 0) {
+    if ((e = wide ? go(attn_dkv<128>, p.n_kv_heads) : go(attn_dkv<64>, p.n_kv_heads)) != hipSuccess) return e;
+    const int64_t n = p.n_k * p.n_kv_heads * p.head_dim;
+    if (a.parts > 1 && ((e = join(n, 0, p.scale, dk)) != hipSuccess || (e = join(n, a.parts, 1.0f, dv)) != hipSuccess))
+      return e;
+  }
   if (p.n_q == 0) return hipSuccess;
-  return wide ? go(attn_dq<128>, p.n_heads) : go(attn_dq<64>, p.n_heads);
+  a.plan = queries;
+  a.parts = parts.dq;
+  if ((e = wide ? go(attn_dq<128>, p.n_heads) : go(attn_dq<64>, p.n_heads)) != hipSuccess || a.parts == 1) return e;
+  return join(p.n_q * p.n_heads * p.head_dim, 0, p.scale, dq);
 }
 
 }  // namespace argus
