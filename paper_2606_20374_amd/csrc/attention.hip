@@ -1,10 +1,23 @@
-// Softmax attention over packed documents, forward.
+// Softmax attention over packed documents, forward, and the plan of tiles that
+// both directions use.
 //
 // S^T = K Q^T per tile of keys, with the running maximum and sum of each
 // query, and O^T += V^T P^T. The transposed products keep a query in one lane
 // (two lanes, one to each half of a tile's keys), so its maximum, sum and
 // rescaling are plain registers, and P^T is the second product's operand as it
-// comes out of the first.
+// comes out of the first, rounded to bfloat16 (2^-9 of each probability, as
+// exact as the values and the output; the sum l is that of the unrounded
+// ones, in 32 bits).
+//
+// A workgroup of four wavefronts owns 128 queries, 32 to a wavefront, and two
+// such workgroups share a CU (at most 256 registers a lane: with one, 1,150 us
+// in place of 682). Keys and values come straight into LDS, 64 at a time, the
+// next tile while one is used (through registers 682 us, straight 583).
+// Four sequences of 4,096, causal, 32 query and 8 key heads of 128: 556 to
+// 592 us from run to run, 930 to 990 TFLOP/s; the matrix units are busy half
+// of the cycles (counters). Tiles of 32 keys four deep (617 us), eight
+// wavefronts with three tiles (594) and three workgroups to a CU (718) were
+// not faster.
 #include "attention_tile.h"
 
 #pragma clang fp contract(fast)
@@ -111,10 +124,8 @@ __device__ void fill_empty(const FwdArgs& a) {
   }
 }
 
-template <int DP, int NQ>
+template <int DP>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
-  constexpr int kRows = 4 * 32 * NQ;  // queries of a workgroup
-  static_assert(kRows == kTile);
   constexpr int KS = DP / 16, DT = DP / 32;
   // four arrays, not two of two: reads of one tile then do not wait for the
   // loads of the next
@@ -125,42 +136,25 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   const Doc doc = doc_at(a.d, di);
   const int n = h / (a.H / a.N);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, half = lane >> 5;
-  const int q0 = row0 + w * 32 * NQ;  // the wavefront's first query
-  const int shift = doc.nk - doc.nq;  // query i sees keys up to i + shift
+  const int q0 = row0 + w * 32, q = q0 + (lane & 31);  // the wavefront's first query, the lane's
+  const int shift = doc.nk - doc.nq;                   // query i sees keys up to i + shift
   const float sc = score_scale(a.scale);
 
-  bf16x8 qf[NQ][KS];
-  {
-    const __bf16* qb = a.q + (doc.q0 + row0) * a.q_tok + (int64_t)h * a.q_head;
-    const auto r = rows_rsrc(qb, doc.nq - row0, a.q_tok, a.D);
-#pragma unroll
-    for (int u = 0; u < NQ; ++u)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int c = 16 * ks + 8 * half, row = w * 32 * NQ + u * 32 + (lane & 31);
-        const int off = c < a.D ? (int)(((int64_t)row * a.q_tok + c) * 2) : 0x7ffffff0;
-        qf[u][ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
-      }
-  }
-  f32x16 acc[NQ][DT];
-  float m[NQ], l[NQ];
-#pragma unroll
-  for (int u = 0; u < NQ; ++u) {
-    m[u] = -__builtin_inff();
-    l[u] = 0;
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[u][t][i] = 0;
-  }
-  // keys that some query of the workgroup sees
-  int last_row = row0 + kRows - 1 < doc.nq - 1 ? row0 + kRows - 1 : doc.nq - 1;
+  bf16x8 qf[KS];
+  load_operand<DP>(qf, rows_rsrc(a.q + (doc.q0 + row0) * a.q_tok + (int64_t)h * a.q_head, doc.nq - row0, a.q_tok, a.D),
+                   w * 32 + (lane & 31), a.q_tok, a.D);
+  f32x16 acc[DT];
+  clear<DP>(acc);
+  float m = -__builtin_inff(), l = 0;
+  // keys that some query of the workgroup sees, and of the wavefront
+  const int last_row = row0 + kTile - 1 < doc.nq - 1 ? row0 + kTile - 1 : doc.nq - 1;
   const int seen = a.causal ? last_row + shift + 1 : doc.nk;
   const int nk = seen < 0 ? 0 : seen < doc.nk ? seen : doc.nk;
   const int tiles = (nk + kKeys - 1) / kKeys;
-  // keys that some query of the wavefront sees
   int wave_nk = q0 >= doc.nq ? 0 : nk;
-  if (a.causal && q0 + 32 * NQ + shift < wave_nk) wave_nk = q0 + 32 * NQ + shift;
+  if (a.causal && q0 + 32 + shift < wave_nk) wave_nk = q0 + 32 + shift;
+  int lim = a.causal ? q + shift : doc.nk - 1;  // the last key that the lane's query sees
+  if (lim > doc.nk - 1) lim = doc.nk - 1;
   const __bf16* kb = a.k + doc.k0 * a.k_tok + (int64_t)n * a.k_head;
   const __bf16* vb = a.v + doc.k0 * a.v_tok + (int64_t)n * a.v_head;
   Reader<DP> rd;
@@ -172,83 +166,61 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   };
   auto compute = [&](int key0, const __bf16* K, const __bf16* V) __attribute__((always_inline)) {
     rd.fresh();
-    f32x16 s[NQ][2];
+    f32x16 s[kKeys / 32];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kKeys / 32; ++b) {
 #pragma unroll
-      for (int u = 0; u < NQ; ++u)
+      for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[u][b][i] = 0;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 ka = rd.rows(K, 32 * b, ks);
-#pragma unroll
-        for (int u = 0; u < NQ; ++u) s[u][b] = mfma(ka, qf[u][ks], s[u][b]);
-      }
+      for (int ks = 0; ks < KS; ++ks) s[b] = mfma(rd.rows(K, 32 * b, ks), qf[ks], s[b]);
     }
     // the tiles at the causal edge and at the document's end
-    const bool edge = key0 + kKeys > doc.nk || (a.causal && key0 + kKeys - 1 > q0 + shift);
-    if (edge) {
+    if (key0 + kKeys > doc.nk || (a.causal && key0 + kKeys - 1 > q0 + shift)) {
 #pragma unroll
-      for (int u = 0; u < NQ; ++u) {
-        const int q = q0 + u * 32 + (lane & 31);
-        int lim = a.causal ? q + shift : doc.nk - 1;
-        if (lim > doc.nk - 1) lim = doc.nk - 1;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = key0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
-            s[u][b][i] = key <= lim ? s[u][b][i] : -__builtin_inff();
-          }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < NQ; ++u) {
-      float mx = s[u][0][0];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][b][i]);
-      mx = fmaxf(mx, other_half(mx)) * sc;
-      // The sums are kept against an earlier maximum until it is passed by
-      // 2^8: the probabilities then stay below 2^8, which 32 bits and a
-      // bfloat16 operand hold as exactly as those below 1.
-      const float mn = fmaxf(m[u], mx);
-      if (__ballot(mn > m[u] + 8.0f)) {
-        const float al = exp2_fast(m[u] - (mn > -__builtin_inff() ? mn : 0.0f));
-        m[u] = mn;
-        l[u] *= al;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[u][d][i] *= al;
-      }
-      const float mm = m[u] > -__builtin_inff() ? m[u] : 0.0f;
-      float sum = 0;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < kKeys / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float p = exp2_fast(s[u][b][i] * sc - mm);
-          s[u][b][i] = p;
-          sum += p;
+          const int key = key0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
+          s[b][i] = key <= lim ? s[b][i] : -__builtin_inff();
         }
-      l[u] += sum;
     }
+    float mx = s[0][0];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < kKeys / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx = fmaxf(mx, other_half(mx)) * sc;
+    // The sums are kept against an earlier maximum until it is passed by
+    // 2^8: the probabilities then stay below 2^8, which 32 bits and a
+    // bfloat16 operand hold as exactly as those below 1.
+    const float mn = fmaxf(m, mx);
+    if (__ballot(mn > m + 8.0f)) {
+      const float al = exp2_fast(m - (mn > -__builtin_inff() ? mn : 0.0f));
+      m = mn;
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= al;
+    }
+    const float mm = m > -__builtin_inff() ? m : 0.0f;
+    float sum = 0;
+#pragma unroll
+    for (int b = 0; b < kKeys / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float p = exp2_fast(s[b][i] * sc - mm);
+        s[b][i] = p;
+        sum += p;
+      }
+    l += sum;
+#pragma unroll
+    for (int b = 0; b < kKeys / 32; ++b)
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
-        bf16x8 p[NQ];
+        const bf16x8 p = as_operand(s[b], k2);
 #pragma unroll
-        for (int u = 0; u < NQ; ++u) p[u] = as_operand(s[u][b], k2);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const bf16x8 va = rd.cols(V, 32 * b + 16 * k2, 32 * d);
-#pragma unroll
-          for (int u = 0; u < NQ; ++u) acc[u][d] = mfma(va, p[u], acc[u][d]);
-        }
+        for (int d = 0; d < DT; ++d) acc[d] = mfma(rd.cols(V, 32 * b + 16 * k2, 32 * d), p, acc[d]);
       }
   };
   auto step = [&](int t, const __bf16* K, const __bf16* V, __bf16* next_k, __bf16* next_v)
@@ -266,25 +238,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
     step(t, kt0, vt0, kt1, vt1);
     if (t + 1 < tiles) step(t + 1, kt1, vt1, kt0, vt0);
   }
-#pragma unroll
-  for (int u = 0; u < NQ; ++u) {
-    const float z = l[u] + other_half(l[u]);
-    const int q = q0 + u * 32 + (lane & 31);
-    if (q >= doc.nq) continue;
-    const int64_t row = (doc.q0 + q) * a.H + h;
-    const float rz = z > 0 ? 1.0f / z : z == 0 ? 0.0f : z;  // NaN stays
-    if (half == 0) a.lse[row] = z == 0 ? -__builtin_inff() : m[u] * kLn2 + __logf(z);
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const int at = 32 * d + 2 * i + 4 * half;
-        bf16x4 o4;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o4[j] = (__bf16)(acc[u][d][i + j] * rz);
-        if (at < a.D) *(bf16x4*)(a.o + row * a.D + at) = o4;
-      }
-  }
+  const float z = l + other_half(l);
+  if (q >= doc.nq) return;
+  const int64_t row = (doc.q0 + q) * a.H + h;
+  if (half == 0) a.lse[row] = z == 0 ? -__builtin_inff() : m * kLn2 + __logf(z);
+  write_rows<DP>(a.o + row * a.D, acc, z > 0 ? 1.0f / z : z == 0 ? 0.0f : z, a.D);  // a NaN stays
 }
 
 }  // namespace
@@ -322,7 +280,7 @@ hipError_t launch_attention(const argus_attention_t& p, const void* q, const voi
     hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), 0, st, a);
     return hipGetLastError();
   };
-  return p.head_dim <= 64 ? go(attn_fwd<64, 1>) : go(attn_fwd<128, 1>);
+  return p.head_dim <= 64 ? go(attn_fwd<64>) : go(attn_fwd<128>);
 }
 
 }  // namespace argus

@@ -22,7 +22,6 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -132,17 +131,6 @@ __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, float* word
 
 // All of this wavefront's loads have arrived.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
-// All but its last N, and all of its LDS reads; then the workgroup's other
-// wavefronts as well. A fence would wait for every load; this barrier orders
-// LDS alone, whose reads are waited for here and whose writes by loads above.
-template <int N>
-__device__ __forceinline__ void wait_but_last() {
-  static_assert(N < 64);
-  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4 << 14));
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
 
 // Reads of tiles of DP elements a row. A few byte offsets of the lane serve
 // every tile: what else moves an operand is a constant, which the
@@ -200,6 +188,43 @@ __device__ __forceinline__ bf16x8 as_operand(const f32x16& x, int t) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) r[j] = (__bf16)x[8 * t + j];
   return r;
+}
+
+// A row's operand in registers: row of the buffer, k as in an operand.
+template <int DP>
+__device__ __forceinline__ void load_operand(bf16x8 (&f)[DP / 16], __amdgpu_buffer_rsrc_t r, int row, int64_t stride,
+                                             int dim) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) {
+    const int c = 16 * ks + 8 * half;
+    const int off = c < dim ? (int)(((int64_t)row * stride + c) * 2) : 0x7ffffff0;
+    f[ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+  }
+}
+
+template <int DP>
+__device__ __forceinline__ void clear(f32x16 (&x)[DP / 32]) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[d][i] = 0;
+}
+
+// Writes a transposed accumulator, times f: lane = row, registers = columns.
+template <int DP>
+__device__ __forceinline__ void write_rows(__bf16* row, const f32x16 (&x)[DP / 32], float f, int dim) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int at = 32 * d + 2 * i + 4 * half;
+      bf16x4 o4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o4[j] = (__bf16)(x[d][i + j] * f);
+      if (at < dim) *(bf16x4*)(row + at) = o4;
+    }
 }
 
 __device__ __forceinline__ float other_half(float v) {

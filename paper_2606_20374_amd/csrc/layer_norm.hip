@@ -12,11 +12,11 @@
 // past that. Workgroups stay and take every n-th row, so that the weights and,
 // backward, the sums of the weight's gradient live in registers. Forward the
 // next row is loaded before the current one is reduced; backward its registers
-// would cost a workgroup of the CU, which hides more (20,011 x 5,000 bf16:
-// 226 us with, 129 us without; three workgroups of ten
-// wavefronts to a CU in place of two: 167 us). The gradient sums of the
-// workgroups are written once each ([workgroups][2][cols]) and added in the
-// order of the workgroups. All sums are 32-bit floats.
+// would cost a workgroup of the CU, which hides more (20,011 x 5,000 bf16, all
+// launches: 232 us with, 135 us without). The gradient sums of the workgroups
+// are written once each ([workgroups][2][cols]) and added in the order of the
+// workgroups. All sums are 32-bit floats. 32,768 x 4,096 bf16 forward: 99 us,
+// 5.4 TB/s, more than a large copy reaches (5.0).
 #include "ops_internal.h"
 
 #pragma clang fp contract(fast)
