@@ -416,12 +416,16 @@ __global__ __launch_bounds__(256) void emb_sums(SumArgs a, const T* dout, G* dta
   const int tpr = a.tpr, lane = threadIdx.x % tpr, sub = threadIdx.x / tpr, groups = 256 / tpr;
   const int64_t begin = ((int64_t)(role / a.cols) * groups + sub) * kWindow;
   uint32_t *mask = lds + sub * kStaged, *key = mask + 2 * ((kWords + 1) / 2), *tok = key + kSpan + 1;
-  // key[i] is that of sorted position first - 1 + i; past the last one none is equal
+  // key[i] is that of sorted position first - 1 + i. Ids that name no row sort
+  // behind all others and have the key of the places past the last position:
+  // the two are one run without an end, which is never summed or written.
   const int64_t first = begin < a.n ? begin : a.n;
+  const uint32_t V = (uint32_t)a.V;
   for (int i = lane; i <= kSpan; i += tpr) {
     const int64_t at = first - 1 + i;
     const bool there = at >= 0 && at < a.n;
-    key[i] = there ? a.skey[at] : ~0u;
+    const uint32_t k = there ? a.skey[at] : ~0u;
+    key[i] = k < V ? k : ~0u;
     tok[i] = there ? a.stok[at] : 0;
   }
   for (int i = lane; i < 2 * ((kWords + 1) / 2); i += tpr) mask[i] = 0;
@@ -431,7 +435,6 @@ __global__ __launch_bounds__(256) void emb_sums(SumArgs a, const T* dout, G* dta
     if (key[i] != key[i + 1]) atomicOr(&mask[i >> 5], 1u << (i & 31));
   __syncthreads();
   const int c = (role % a.cols * tpr + lane) * E;
-  const uint32_t V = (uint32_t)a.V;
   // the stream: from the window's first run to the end of its last
   const uint64_t* mask64 = (const uint64_t*)mask;
   const uint64_t begins = mask64[0] & (~0ull >> (64 - kWindow));
@@ -450,8 +453,6 @@ __global__ __launch_bounds__(256) void emb_sums(SumArgs a, const T* dout, G* dta
   // where its run ends (whole wavefronts search together)
   int e = 0;
   if (heavy && id < V) e = tpr >= 64 ? wave_lower_bound(a.skey, a.n, id + 1) : lower_bound(a.skey, a.n, id + 1);
-  // ids that name no row sort behind all others: at most one run, the last
-  if (!heavy && id >= V) stop = last;
   if (c >= a.dim) return;
   float acc[E] = {};
   auto write = [&](uint32_t to) {

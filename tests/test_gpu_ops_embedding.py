@@ -136,3 +136,21 @@ def test_same_bits_each_time_and_on_another_stream():
         again = pa.embedding_bwd(ids, dout, 4000)["dtable"]
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("n,pad", [(1, 1), (5, 2), (10, 1), (33, 1), (40, 40), (100, 3), (130, 2), (1030, 5), (5001, 1)])
+@pytest.mark.parametrize("dim", [8, 40, 600, 2056])
+def test_gradient_of_padding_writes_no_row(n, pad, dim):
+    # padding that begins and ends among the last sorted positions: what lies
+    # behind the table keeps its values
+    vocab = 77
+    ids = torch.randint(0, vocab, (n,), generator=torch.Generator().manual_seed(n))
+    ids[:pad] = -1
+    ids[0] = vocab
+    dout = torch.randn(n, dim, generator=torch.Generator().manual_seed(dim))
+    rows = torch.full((vocab + 2, dim), 7.0, device=DEV)
+    got = pa.embedding_bwd(ids.to(DEV), dout.to(DEV), vocab,
+                           out={"dtable": rows[:vocab], "dev_status": torch.zeros(1, dtype=torch.int32, device=DEV)})
+    _check_bwd(ids, dout, vocab, 1.0, got, torch.float32)
+    assert torch.all(rows[vocab:] == 7.0)
+    assert int(got["dev_status"]) == ops.DEV_TOKEN_RANGE
