@@ -436,7 +436,8 @@ __global__ __launch_bounds__(256) void bal_bwd(BalBwdArgs a) {
     for (int i = 0; i < NI; ++i) {
       Vec<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.e[j] = from_f32<T>(p[i * V + j] * (g[i * V + j] - s));
+      for (int j = 0; j < V; ++j)  // the choice matters where dloss is no number
+        o.e[j] = from_f32<T>(ok ? p[i * V + j] * (g[i * V + j] - s) : 0.0f);
       stream_row<V>(out + t * E, (i * 16 + lane) * V, E, o);
     }
   }

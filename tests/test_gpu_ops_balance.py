@@ -177,6 +177,16 @@ def test_gradient_against_differences():
     assert abs(near - want) <= abs(wide - near) + rounding, (near, want, wide, rounding)
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_gradient_of_a_loss_that_is_no_number_spares_masked_tokens(bad):
+    x = _logits(50, 24, torch.float32, "normal").to(DEV)
+    mask = torch.ones(50, dtype=torch.uint8, device=DEV)
+    mask[::3] = 0
+    f = pa.balance(x, 2, mask=mask)
+    d = pa.balance_bwd(x, f["lse"], f["expert"], f["count"], f["n_valid"], torch.full((1,), bad, device=DEV))["dlogits"]
+    assert torch.all(d[mask == 0] == 0) and not torch.isfinite(d[mask == 1]).any()
+
+
 def test_same_bits_each_time():
     x = _logits(20_000, 128, torch.bfloat16, "normal").to(DEV)
     a, b = pa.balance(x, 8), pa.balance(x, 8)
