@@ -181,8 +181,10 @@ int argus_balance_bwd(const argus_balance_t* p, const void* logits, const float*
  * is raised and every query is taken to see no key.
  *
  * A value row of a document that holds a NaN or an infinity may reach those
- * of its queries that do not see it under the causal mask; nothing passes
- * from one document to another.
+ * of its queries that do not see it under the causal mask. Backward, such a
+ * key or value row may reach their dq, and such a row of q, o or d_o the dk
+ * and dv of keys that the query does not see. Nothing passes from one
+ * document to another.
  */
 typedef struct argus_attention {
   int32_t n_docs;      /* >= 1 */
