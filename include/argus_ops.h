@@ -183,7 +183,8 @@ int argus_balance_bwd(const argus_balance_t* p, const void* logits, const float*
  * A value row of a document that holds a NaN or an infinity may reach those
  * of its queries that do not see it under the causal mask. Backward, such a
  * key or value row may reach their dq, and such a row of q, o or d_o the dk
- * and dv of keys that the query does not see. Nothing passes from one
+ * and dv of keys that the query does not see. Nothing reaches the outputs of
+ * a query that sees no key, nor passes from its row to a key, nor from one
  * document to another.
  */
 typedef struct argus_attention {

@@ -240,6 +240,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd(FwdArgs a) {
   }
   const float z = l + other_half(l);
   if (q >= doc.nq) return;
+  if (lim < 0) clear<DP>(acc);  // no key seen: 0 times what the hidden values hold may be NaN
   const int64_t row = (doc.q0 + q) * a.H + h;
   if (half == 0) a.lse[row] = z == 0 ? -__builtin_inff() : m * kLn2 + __logf(z);
   write_rows<DP>(a.o + row * a.D, acc, z > 0 ? 1.0f / z : z == 0 ? 0.0f : z, a.D);  // a NaN stays

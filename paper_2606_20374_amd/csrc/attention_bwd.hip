@@ -148,9 +148,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv(BwdArgs a) {
   f32x16 dk[DT], dv[DT];
   clear<DP>(dk);
   clear<DP>(dv);
-  // queries from the first that sees a key of the workgroup on
+  // queries from the first that sees a key of the workgroup on, so none that
+  // sees no key at all, whatever its rows hold
   int first = 0;
-  if (a.causal && row0 > shift) first = (row0 - shift) / kQ * kQ;
+  if (a.causal && row0 > shift) first = row0 - shift;
   const int per = first < doc.nq ? (doc.nq - first + kQ - 1) / kQ : 0;
   // this part's steps, of all heads' one after the other
   const int begin = (int)((int64_t)per * G * part / a.parts), end = (int)((int64_t)per * G * (part + 1) / a.parts);
@@ -333,6 +334,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq(BwdArgs a) {
     if (t + 1 < tiles) step(t + 1, kt1, vt1, kt0, vt0);
   }
   if (q < doc.nq) {
+    if (lim < 0) clear<DP>(acc);  // no key seen: no gradient, whatever its row and the hidden ones hold
     const int64_t row = ((doc.q0 + q) * a.H + h) * a.D;
     if (a.parts == 1) write_rows<DP>(a.dq + row, acc, a.scale, a.D);
     else write_sums<DP>(a.sums + part * a.d.n_q * a.H * a.D + row, acc, a.D);

@@ -297,3 +297,33 @@ def test_same_bits_each_time_and_on_another_stream():
         again = pa.attention_bwd(do, q, k, v, f2["o"], f2["lse"], q_off=off)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(f["o"], f2["o"]) and all(torch.equal(first[n], again[n]) for n in ("dq", "dk", "dv"))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nq,nk", [(100, 30), (300, 100), (1300, 1100)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_queries_that_see_nothing_whatever_their_rows_hold(bad, nq, nk, D):
+    # causal, more queries than keys: the first nq - nk see none. Their own
+    # rows, and the keys and values hidden from them, hold no number
+    q, k, v, do = (t.to(DEV) for t in _make([nq, 40], [nk, 40], 4, 2, D, 7))
+    off = dict(q_off=_off([nq, 40]).to(DEV), k_off=_off([nk, 40]).to(DEV))
+    blind = nq - nk
+
+    def both(q, k, v, do):
+        f = pa.attention(q, k, v, **off)
+        return f, pa.attention_bwd(do, q, k, v, f["o"], f["lse"], **off)
+
+    _, clean = both(q, k, v, do)
+    q2, do2 = q.clone(), do.clone()
+    q2[:blind], do2[:blind] = bad, bad
+    f, b = both(q2, k, v, do2)
+    assert torch.all(f["o"][:blind] == 0) and torch.all(f["lse"][:blind] == -math.inf)
+    assert torch.all(b["dq"][:blind] == 0)
+    for n in ("dk", "dv"):
+        assert torch.equal(b[n], clean[n]), n
+    k2, v2 = k.clone(), v.clone()
+    k2[0], k2[nk // 2], v2[1], v2[nk - 1] = bad, bad, bad, bad
+    for kk, vv in ((k2, v), (k, v2), (k2, v2)):
+        f, b = both(q, kk, vv, do)
+        assert torch.all(f["o"][:blind] == 0) and torch.all(f["lse"][:blind] == -math.inf)
+        assert torch.all(b["dq"][:blind] == 0)
