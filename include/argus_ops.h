@@ -180,10 +180,12 @@ int argus_balance_bwd(const argus_balance_t* p, const void* logits, const float*
  * off[n_docs] is the number of tokens, for both sides, ARGUS_DEV_BAD_SEGMENT
  * is raised and every query is taken to see no key.
  *
+ * A query or key row that holds a NaN makes lse, o and dq of the queries that
+ * see it NaN, and by them dk and dv of all keys these see.
  * A value row of a document that holds a NaN or an infinity may reach those
  * of its queries that do not see it under the causal mask. Backward, such a
- * key or value row may reach their dq, and such a row of q, o or d_o the dk
- * and dv of keys that the query does not see. Nothing reaches the outputs of
+ * key or value row may reach their dq, and such a row of q, o, d_o or lse the
+ * dk and dv of keys that the query does not see. Nothing reaches the outputs of
  * a query that sees no key, nor passes from its row to a key, nor from one
  * document to another.
  */

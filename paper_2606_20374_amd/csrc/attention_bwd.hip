@@ -70,8 +70,9 @@ __global__ __launch_bounds__(256) void attn_prep(BwdArgs a) {
     if (lane == 0) {
       const int64_t t = i / a.H, at = (i - t * a.H) * a.d.n_q + t;
       const float l = a.lse[i];
-      // a query that sees nothing: exp2(s - infinity) = 0 for every key
-      *(float2*)(a.stat + 2 * at) = make_float2(l > -__builtin_inff() ? l * kLog2e : __builtin_inff(), s);
+      // a query that sees nothing: exp2(s - infinity) = 0 for every key (a NaN
+      // stays one: every key it sees shares its sum)
+      *(float2*)(a.stat + 2 * at) = make_float2(l == -__builtin_inff() ? __builtin_inff() : l * kLog2e, s);
     }
   }
 }

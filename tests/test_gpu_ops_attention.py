@@ -327,3 +327,24 @@ def test_queries_that_see_nothing_whatever_their_rows_hold(bad, nq, nk, D):
         f, b = both(q, kk, vv, do)
         assert torch.all(f["o"][:blind] == 0) and torch.all(f["lse"][:blind] == -math.inf)
         assert torch.all(b["dq"][:blind] == 0)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_key_that_is_no_number_reaches_all_it_is_normalised_with(D, causal):
+    # P of a query that sees the key is no number for any of its keys, and the
+    # last query of the document sees all of them
+    lens = [70, 150]
+    q, k, v, do = (t.to(DEV) for t in _make(lens, lens, 4, 2, D, 9))
+    off = _off(lens).to(DEV)
+    k2 = k.clone()
+    k2[100] = float("nan")
+    f, f2 = (pa.attention(q, x, v, q_off=off, causal=causal) for x in (k, k2))
+    b, b2 = (pa.attention_bwd(do, q, x, v, g["o"], g["lse"], q_off=off, causal=causal) for x, g in ((k, f), (k2, f2)))
+    sees = 100 if causal else 70
+    assert torch.isnan(f2["lse"][sees:]).all()
+    assert torch.isnan(b2["dq"][sees:]).all()
+    for n in ("dk", "dv"):
+        assert torch.isnan(b2[n][70:]).all(), n
+        assert torch.equal(b2[n][:70], b[n][:70]), n
+    assert torch.equal(b2["dq"][:70], b["dq"][:70])
