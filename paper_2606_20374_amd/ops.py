@@ -287,8 +287,8 @@ def _heads(t: torch.Tensor, what: str):
         raise ArgusError(f"{what} of {t.dtype}: attention takes bfloat16")
     assert t.stride(2) == 1, "the last dimension has to be contiguous"
     n, h, d = t.shape
-    head = t.stride(1) if h > 1 else d
-    return t.data_ptr(), t.stride(0) if n > 1 else h * max(head, d), head
+    # a dimension of one has no use for its stride, which may lie outside the limits
+    return t.data_ptr(), t.stride(0) if n > 1 else d, t.stride(1) if h > 1 else d
 
 
 def _attention(q, k, v, q_off, k_off, causal, scale, status):

@@ -348,3 +348,21 @@ def test_a_key_that_is_no_number_reaches_all_it_is_normalised_with(D, causal):
         assert torch.isnan(b2[n][70:]).all(), n
         assert torch.equal(b2[n][:70], b[n][:70]), n
     assert torch.equal(b2["dq"][:70], b["dq"][:70])
+
+
+def test_single_tokens_of_head_major_tensors():
+    # a view of one token: the stride to the next one is not used, the heads
+    # are far apart
+    H, N, D, T = 32, 8, 128, 1024
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q, k, v = (torch.randn(h, T, D, generator=g, device=DEV).to(torch.bfloat16).transpose(0, 1) for h in (H, N, N))
+    for a, b in ((slice(500, 501), slice(0, 501)), (slice(0, 300), slice(7, 8)), (slice(9, 10), slice(9, 10))):
+        x = q[a], k[b], v[b]
+        y = tuple(t.contiguous() for t in x)
+        do = torch.randn(y[0].shape, generator=g, device=DEV).to(torch.bfloat16)
+        f, want = (pa.attention(*t, causal=False) for t in (x, y))
+        d, d_want = (pa.attention_bwd(do, *t, want["o"], want["lse"], causal=False) for t in (x, y))
+        for n in ("o", "lse"):
+            assert torch.equal(f[n], want[n]), n
+        for n in ("dq", "dk", "dv"):
+            assert torch.equal(d[n], d_want[n]), n
