@@ -20,6 +20,7 @@ bool bad_embedding(const argus_embedding_t* p) {
     return true;
   if (bad_dtype(p->dtype) || p->row_stride < 0 || !std::isfinite(p->scale)) return true;
   if (p->ids_64 != 0 && p->ids_64 != 1) return true;
+  if (misaligned(p->dev_status, 4)) return true;
   return p->n_tokens > 0 && (!p->ids || misaligned(p->ids, p->ids_64 ? 8 : 4));
 }
 
@@ -49,7 +50,7 @@ bool bad_attention(const argus_attention_t* p) {
   if (!(p->scale >= 0.0f) || !std::isfinite(p->scale)) return true;
   if (p->n_q < 0 || p->n_q > (1 << 30) || p->n_k < 0 || p->n_k > (1 << 30)) return true;
   if ((p->q_off == nullptr) != (p->k_off == nullptr) || (!p->q_off && p->n_docs != 1)) return true;
-  if (misaligned(p->q_off, 8) || misaligned(p->k_off, 8)) return true;
+  if (misaligned(p->q_off, 8) || misaligned(p->k_off, 8) || misaligned(p->dev_status, 4)) return true;
   // one launch takes all tiles of all heads
   if ((p->n_q / 128 + p->n_docs) * p->n_heads >= (1 << 23) || (p->n_k / 128 + p->n_docs) * p->n_kv_heads >= (1 << 23))
     return true;
@@ -139,6 +140,9 @@ int argus_balance(const argus_balance_t* p, const void* logits, const uint8_t* m
   if (!o.count || !o.prob || !o.n_valid || !o.loss) return ARGUS_EINVAL;
   if (p->n_tokens > 0 && (!logits || !o.expert || !o.gate || !o.lse)) return ARGUS_EINVAL;
   if (misaligned(logits, size_of(p->dtype))) return ARGUS_EINVAL;
+  const void* ptrs[8] = {o.expert, o.gate, o.lse, o.count, o.prob, o.n_valid, o.loss, o.dev_status};
+  for (const void* x : ptrs)
+    if (misaligned(x, 4)) return ARGUS_EINVAL;
   if (bad_workspace(workspace, workspace_bytes, argus_balance_workspace(p))) return ARGUS_EINVAL;
   const int rc = check_device();
   if (rc != ARGUS_OK) return rc;
@@ -151,6 +155,9 @@ int argus_balance_bwd(const argus_balance_t* p, const void* logits, const float*
   if (bad_balance(p) || !count || !n_valid || !dloss) return ARGUS_EINVAL;
   if (p->n_tokens > 0 && (!logits || !lse || !dlogits || (dgate && !expert))) return ARGUS_EINVAL;
   if (misaligned(logits, size_of(p->dtype)) || misaligned(dlogits, size_of(p->dtype))) return ARGUS_EINVAL;
+  const void* ptrs[6] = {lse, expert, count, n_valid, dloss, dgate};
+  for (const void* x : ptrs)
+    if (misaligned(x, 4)) return ARGUS_EINVAL;
   const int rc = check_device();
   if (rc != ARGUS_OK) return rc;
   return status_of(launch_balance_bwd(*p, logits, lse, expert, count, n_valid, dloss, dgate, dlogits,

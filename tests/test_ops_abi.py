@@ -162,3 +162,21 @@ def test_binding_refuses_other_types_and_shapes():
         ops._need(x, (4, 9), torch.float32, "x")
     with pytest.raises(pa.ArgusError):
         ops._need(x, (4, 8), torch.bfloat16, "x")
+
+
+def test_refuses_misaligned_outputs_statistics_and_status():
+    need = lambda fn, p: getattr(ops._lib(), fn)(ctypes.byref(p))  # noqa: E731
+    p = ops.Balance(10, 64, 8, 0, 0.01, 64)
+    ws = need("argus_balance_workspace", p)
+    for f in ops.BALANCE_FIELDS:
+        o = ops.BalanceOut(*([P] * 8))
+        setattr(o, f, P + 2)
+        assert _call("argus_balance", p, P, None, ctypes.byref(o), P, ws, None) == A.EINVAL, f
+    for i in range(8):  # logits, lse, expert, count, n_valid, dloss, dgate, dlogits
+        assert _call("argus_balance_bwd", p, *[P + 2 if j == i else P for j in range(8)], None) == A.EINVAL, i
+    p = _embedding(dev_status=P + 2)
+    assert _call("argus_embedding", p, P, P, None) == A.EINVAL
+    assert _call("argus_embedding_bwd", p, P, P, P, need("argus_embedding_bwd_workspace", p), None) == A.EINVAL
+    p = _attention(dev_status=P + 1)
+    assert _call("argus_attention", p, *[P] * 7, 1 << 40, None) == A.EINVAL
+    assert _call("argus_attention_bwd", p, *[P] * 11, 1 << 40, None) == A.EINVAL
