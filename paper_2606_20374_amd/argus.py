@@ -165,7 +165,8 @@ def _check(rc: int, what: str):
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous(), "libargus takes contiguous device tensors"
+    if not (t.is_cuda and t.is_contiguous()):  # no assert: -O would let a host address through
+        raise AssertionError("libargus takes contiguous device tensors")
     return t.data_ptr()
 
 

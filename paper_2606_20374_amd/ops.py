@@ -87,8 +87,10 @@ def _dtype(t: torch.Tensor) -> int:
 
 def _row(t: torch.Tensor):
     """(address, row stride) of a 2-D device tensor with contiguous rows."""
-    assert t.is_cuda and t.dim() == 2, "libargus takes 2-D device tensors of rows"
-    assert t.stride(1) == 1 or t.shape[1] <= 1, "the last dimension has to be contiguous"
+    if not (t.is_cuda and t.dim() == 2):
+        raise AssertionError("libargus takes 2-D device tensors of rows")
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise AssertionError("the last dimension has to be contiguous")
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
@@ -282,10 +284,12 @@ def balance_bwd(logits: torch.Tensor, lse: torch.Tensor, expert: torch.Tensor, c
 # ------------------------------------------------------------------ attention
 def _heads(t: torch.Tensor, what: str):
     """(address, token stride, head stride) of a [tokens, heads, dim] tensor."""
-    assert t.is_cuda and t.dim() == 3, "libargus takes [tokens, heads, dim] device tensors"
+    if not (t.is_cuda and t.dim() == 3):
+        raise AssertionError("libargus takes [tokens, heads, dim] device tensors")
     if t.dtype != torch.bfloat16:
         raise ArgusError(f"{what} of {t.dtype}: attention takes bfloat16")
-    assert t.stride(2) == 1, "the last dimension has to be contiguous"
+    if t.stride(2) != 1:
+        raise AssertionError("the last dimension has to be contiguous")
     n, h, d = t.shape
     # a dimension of one has no use for its stride, which may lie outside the limits
     return t.data_ptr(), t.stride(0) if n > 1 else d, t.stride(1) if h > 1 else d

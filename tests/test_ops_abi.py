@@ -1,6 +1,9 @@
 """The step operators' host side: what they refuse before any launch, and
 their workspaces (no GPU needed)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -180,3 +183,20 @@ def test_refuses_misaligned_outputs_statistics_and_status():
     p = _attention(dev_status=P + 1)
     assert _call("argus_attention", p, *[P] * 7, 1 << 40, None) == A.EINVAL
     assert _call("argus_attention_bwd", p, *[P] * 11, 1 << 40, None) == A.EINVAL
+
+
+def test_host_tensors_are_refused_also_without_assertions():
+    # python -O leaves assert statements out; a host address must not get to a kernel
+    code = """if True:
+        import torch
+        from paper_2606_20374_amd import argus, ops
+        x = torch.zeros(4, 2, 8, dtype=torch.bfloat16)
+        for call in (lambda: argus._ptr(x), lambda: ops._row(x[0]), lambda: ops._heads(x, "q")):
+            try:
+                call()
+            except AssertionError:
+                continue
+            raise SystemExit(3)
+    """
+    root = os.path.dirname(os.path.dirname(os.path.abspath(pa.__file__)))
+    assert subprocess.run([sys.executable, "-O", "-c", code], cwd=root).returncode == 0
