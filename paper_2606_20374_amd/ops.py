@@ -103,10 +103,16 @@ def _empty(shape, dtype, device):
     return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _stream(device) -> int:
-    # the current stream's handle alone: a torch Stream object costs more than
-    # a small operator's launches
-    return torch._C._cuda_getCurrentRawStream(device.index)
+def _call(name: str, device, *args):
+    """Calls an entry point on the device's current stream, with the device
+    current: its null stream is another device's otherwise."""
+    fn = getattr(_lib(), name)
+    if device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return _call(name, device, *args)
+    # the stream's handle alone: a torch Stream object costs more than a small
+    # operator's launches
+    _check(fn(*args, torch._C._cuda_getCurrentRawStream(device.index)), name)
 
 
 def _space(out: dict, need: int, device):
@@ -140,7 +146,7 @@ def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: O
     dt = _dtype(table)
     _need(out["out"], (n, dim), table.dtype, "embedding: out")
     p = _embedding(ids, table.shape[0], dim, dt, dt, scale, stride, out.get("dev_status"))
-    _check(_lib().argus_embedding(ctypes.byref(p), at, _ptr(out["out"]), _stream(table.device)), "argus_embedding")
+    _call("argus_embedding", table.device, ctypes.byref(p), at, _ptr(out["out"]))
     return out
 
 
@@ -160,8 +166,7 @@ def embedding_bwd(ids: torch.Tensor, dout: torch.Tensor, n_vocab: int, scale: fl
     _need(out["dtable"], (n_vocab, dim), out["dtable"].dtype, "embedding_bwd: dtable")
     p = _embedding(ids, n_vocab, dim, _dtype(dout), _dtype(out["dtable"]), scale, stride, out.get("dev_status"))
     ws = _space(out, _lib().argus_embedding_bwd_workspace(ctypes.byref(p)), dout.device)
-    _check(_lib().argus_embedding_bwd(ctypes.byref(p), at, _ptr(out["dtable"]), _ptr(ws), ws.numel(),
-                                      _stream(dout.device)), "argus_embedding_bwd")
+    _call("argus_embedding_bwd", dout.device, ctypes.byref(p), at, _ptr(out["dtable"]), _ptr(ws), ws.numel())
     return out
 
 
@@ -186,8 +191,8 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     _need(out["mean"], (rows,), torch.float32, "layer_norm: mean")
     _need(out["rstd"], (rows,), torch.float32, "layer_norm: rstd")
     p = LayerNorm(rows, cols, _dtype(x), _dtype(weight), eps, stride, 0)
-    _check(_lib().argus_layer_norm(ctypes.byref(p), at, _ptr(weight), _ptr(bias), _ptr(out["y"]), _ptr(out["mean"]),
-                                   _ptr(out["rstd"]), _stream(x.device)), "argus_layer_norm")
+    _call("argus_layer_norm", x.device, ctypes.byref(p), at, _ptr(weight), _ptr(bias), _ptr(out["y"]),
+          _ptr(out["mean"]), _ptr(out["rstd"]))
     return out
 
 
@@ -217,9 +222,8 @@ def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: 
         _need(out["dbias"], (cols,), weight.dtype, "layer_norm_bwd: dbias")
     p = LayerNorm(rows, cols, _dtype(x), _dtype(weight), 0.0, stride, dstride)
     ws = _space(out, _lib().argus_layer_norm_bwd_workspace(ctypes.byref(p)), x.device)
-    _check(_lib().argus_layer_norm_bwd(ctypes.byref(p), dat, at, _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(out["dx"]),
-                                       _ptr(out["dweight"]), _ptr(out["dbias"]) if bias else None, _ptr(ws),
-                                       ws.numel(), _stream(x.device)), "argus_layer_norm_bwd")
+    _call("argus_layer_norm_bwd", x.device, ctypes.byref(p), dat, at, _ptr(mean), _ptr(rstd), _ptr(weight),
+          _ptr(out["dx"]), _ptr(out["dweight"]), _ptr(out["dbias"]) if bias else None, _ptr(ws), ws.numel())
     return out
 
 
@@ -250,8 +254,7 @@ def balance(logits: torch.Tensor, top_k: int, mask: Optional[torch.Tensor] = Non
     p = Balance(n, E, top_k, _dtype(logits), alpha, stride)
     o = BalanceOut(*[_ptr(out.get(f)) for f in BALANCE_FIELDS])
     ws = _space(out, _lib().argus_balance_workspace(ctypes.byref(p)), logits.device)
-    _check(_lib().argus_balance(ctypes.byref(p), at, _ptr(mask), ctypes.byref(o), _ptr(ws), ws.numel(),
-                                _stream(logits.device)), "argus_balance")
+    _call("argus_balance", logits.device, ctypes.byref(p), at, _ptr(mask), ctypes.byref(o), _ptr(ws), ws.numel())
     return out
 
 
@@ -275,9 +278,8 @@ def balance_bwd(logits: torch.Tensor, lse: torch.Tensor, expert: torch.Tensor, c
         _need(dgate, (n, top_k), torch.float32, "balance_bwd: dgate")
     _need(out["dlogits"], (n, E), logits.dtype, "balance_bwd: dlogits")
     p = Balance(n, E, top_k, _dtype(logits), alpha, stride)
-    _check(_lib().argus_balance_bwd(ctypes.byref(p), at, _ptr(lse), _ptr(expert), _ptr(count), _ptr(n_valid),
-                                    _ptr(dloss), _ptr(dgate), _ptr(out["dlogits"]), _stream(logits.device)),
-           "argus_balance_bwd")
+    _call("argus_balance_bwd", logits.device, ctypes.byref(p), at, _ptr(lse), _ptr(expert), _ptr(count),
+          _ptr(n_valid), _ptr(dloss), _ptr(dgate), _ptr(out["dlogits"]))
     return out
 
 
@@ -331,8 +333,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_off: Optional
     _need(out["lse"], q.shape[:2], torch.float32, "attention: lse")
     p, qa, ka, va = _attention(q, k, v, q_off, k_off, causal, scale, out.get("dev_status"))
     ws = _space(out, _lib().argus_attention_workspace(ctypes.byref(p)), q.device)
-    _check(_lib().argus_attention(ctypes.byref(p), qa, ka, va, _ptr(out["o"]), _ptr(out["lse"]), _ptr(ws), ws.numel(),
-                                  _stream(q.device)), "argus_attention")
+    _call("argus_attention", q.device, ctypes.byref(p), qa, ka, va, _ptr(out["o"]), _ptr(out["lse"]), _ptr(ws),
+          ws.numel())
     return out
 
 
@@ -357,7 +359,6 @@ def attention_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.T
     _need(lse, q.shape[:2], torch.float32, "attention_bwd: lse")
     p, qa, ka, va = _attention(q, k, v, q_off, k_off, causal, scale, out.get("dev_status"))
     ws = _space(out, _lib().argus_attention_bwd_workspace(ctypes.byref(p)), q.device)
-    _check(_lib().argus_attention_bwd(ctypes.byref(p), _ptr(do), qa, ka, va, _ptr(o), _ptr(lse), _ptr(out["dq"]),
-                                      _ptr(out["dk"]), _ptr(out["dv"]), _ptr(ws), ws.numel(), _stream(q.device)),
-           "argus_attention_bwd")
+    _call("argus_attention_bwd", q.device, ctypes.byref(p), _ptr(do), qa, ka, va, _ptr(o), _ptr(lse), _ptr(out["dq"]),
+          _ptr(out["dk"]), _ptr(out["dv"]), _ptr(ws), ws.numel())
     return out

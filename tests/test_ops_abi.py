@@ -200,3 +200,47 @@ def test_host_tensors_are_refused_also_without_assertions():
     """
     root = os.path.dirname(os.path.dirname(os.path.abspath(pa.__file__)))
     assert subprocess.run([sys.executable, "-O", "-c", code], cwd=root).returncode == 0
+
+
+def test_launches_go_to_the_tensors_device(monkeypatch):
+    # device 0 is current and the tensors lie on device 1: its null stream is
+    # only its own while it is current
+    now, seen = [0], []
+
+    class Guard:
+        def __init__(self, device):
+            self.to = device.index
+
+        def __enter__(self):
+            self.back, now[0] = now[0], self.to
+
+        def __exit__(self, *exc):
+            now[0] = self.back
+
+    class Tensor:
+        """Enough of a [4, 8] float tensor on device 1."""
+        device, is_cuda, dtype, shape = torch.device("cuda", 1), True, torch.float32, (4, 8)
+
+        def __init__(self, *shape, dtype=torch.float32):
+            self.shape, self.dtype = shape, dtype
+
+        dim = lambda self: len(self.shape)  # noqa: E731
+        data_ptr = lambda self: P  # noqa: E731
+        stride = lambda self, i: self.shape[1] if i == 0 else 1  # noqa: E731
+        is_contiguous = lambda self: True  # noqa: E731
+
+    class Lib:
+        @staticmethod
+        def argus_layer_norm(*args):
+            seen.append((now[0], args[-1]))
+            return A.OK
+
+    monkeypatch.setattr(ops, "_lib", lambda: Lib)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 70 + i, raising=False)
+    out = {"y": Tensor(4, 8), "mean": Tensor(4), "rstd": Tensor(4)}
+    for now[0] in (0, 1):
+        before = now[0]
+        pa.layer_norm(Tensor(4, 8), Tensor(8), out=out)
+        assert seen.pop() == (1, 71) and now[0] == before
