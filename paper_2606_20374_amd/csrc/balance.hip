@@ -383,6 +383,15 @@ struct BalBwdArgs {
   void* dlogits;
 };
 
+// Whether another of a row's 16 lanes holds the same value: rotations by one
+// to eight places meet every pair. All lanes take part in each.
+__device__ __forceinline__ bool repeated(int e) {
+  constexpr int kRotate = 0x120;
+  return (dpp_i32<kRotate + 1>(e) == e) | (dpp_i32<kRotate + 2>(e) == e) | (dpp_i32<kRotate + 3>(e) == e) |
+         (dpp_i32<kRotate + 4>(e) == e) | (dpp_i32<kRotate + 5>(e) == e) | (dpp_i32<kRotate + 6>(e) == e) |
+         (dpp_i32<kRotate + 7>(e) == e) | (dpp_i32<kRotate + 8>(e) == e);
+}
+
 template <typename T, int NI>
 __global__ __launch_bounds__(256) void bal_bwd(BalBwdArgs a) {
   constexpr int V = kVec<T>, N = NI * V;
@@ -406,16 +415,34 @@ __global__ __launch_bounds__(256) void bal_bwd(BalBwdArgs a) {
     Vec<T, V> v[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) v[i] = load_row<V>(logits + t * a.stride, (i * 16 + lane) * V, E);
-    int e = -1;
-    if (a.dgate && lane < a.K) {
-      e = a.expert[t * a.K + lane];
-      if (e >= 0 && e < E) atomicAdd(&row[e], a.dgate[t * a.K + lane]);
-      else e = -1;
-    }
+    int e = -1 - lane;  // no choice: unlike every other lane's
     // the token's row is this wavefront's own: LDS keeps its order
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    auto settle = [] {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    };
+    if (a.dgate) {
+      float dg = 0;
+      if (lane < a.K) {
+        const int at = a.expert[t * a.K + lane];
+        if (at >= 0 && at < E) {
+          e = at;
+          dg = a.dgate[t * a.K + lane];
+        }
+      }
+      // the router's choices are distinct; repeated ones of a caller's own list
+      // are added one after the other, so that their order is fixed
+      if (!__ballot(repeated(e))) {
+        if (e >= 0) row[e] = dg;
+      } else {
+        for (int k = 0; k < a.K; ++k) {
+          if (lane == k && e >= 0) row[e] += dg;
+          settle();
+        }
+      }
+    }
+    settle();
     float p[N], g[N], s = 0;
 #pragma unroll
     for (int i = 0; i < NI; ++i)

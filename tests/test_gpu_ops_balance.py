@@ -192,3 +192,36 @@ def test_same_bits_each_time():
     a, b = pa.balance(x, 8), pa.balance(x, 8)
     for k in ("expert", "gate", "lse", "count", "prob", "loss"):
         assert torch.equal(a[k], b[k])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradient_of_repeated_choices_adds_them_in_order(dtype):
+    # 2^27 + 1 - 2^27 + 1 from the left is 1 in 32 bits, and 0 or 2 in other
+    # orders; tokens of distinct choices beside them, and choices of no expert
+    T, E, K = 64, 40, 4
+    x = _logits(T, E, dtype, "normal")
+    f = pa.balance(x.to(DEV), K, alpha=0.0)
+    expert = f["expert"].clone()
+    dgate = torch.full((T, K), 0.5)
+    expert[::2] = 7
+    dgate[::2] = torch.tensor([2.0**27, 1.0, -(2.0**27), 1.0])
+    expert[4] = torch.tensor([3, 9, 3, -1])
+    dgate[4] = torch.tensor([1.0, 2.0, 4.0, float("nan")])
+    got = pa.balance_bwd(x.to(DEV), f["lse"], expert, f["count"], f["n_valid"], torch.ones(1, device=DEV),
+                         dgate=dgate.to(DEV), alpha=0.0)["dlogits"].cpu().double()
+    p = torch.exp(x.double() - f["lse"].cpu().double()[:, None])
+    gr = torch.zeros(T, E).double()
+    at = expert.cpu().long()
+    for t in range(T):
+        if t == 4:
+            gr[t, 3], gr[t, 9] = 5.0, 2.0
+        elif t % 2 == 0:
+            gr[t, 7] = 1.0
+        else:
+            gr[t, at[t]] = 0.5
+    s = (gr * p).sum(1, keepdim=True)
+    ref = p * (gr - s)
+    # p is off by 2^-16 of itself at most (the file's bound for these logits),
+    # the sums by less
+    tol = p * 2.0**-15 * (gr + s) + UNIT[dtype] * ref.abs() + TINY[dtype]
+    assert torch.all((got - ref).abs() <= tol)
