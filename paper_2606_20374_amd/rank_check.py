@@ -139,7 +139,10 @@ class RankCheck:
             mark(None)  # the step's begin
             self.step(mark)
         torch.cuda.synchronize(self.device)
-        at = [round(begin.elapsed_time(e) * 1e6) for _, e in marks]
+        # a difference of events is a 32-bit number of milliseconds: each is taken
+        # from its neighbour, which keeps the nanoseconds however long the trace
+        events = [begin, *(e for _, e in marks)]
+        at = np.cumsum([round(a.elapsed_time(b) * 1e6) for a, b in zip(events, events[1:])], dtype=np.int64)
         kid = np.array([NAMES.index(name) for name, _ in marks if name], dtype=np.int32)
         start = np.array([at[i - 1] for i, (name, _) in enumerate(marks) if name], dtype=np.int64)
         end = np.array([at[i] for i, (name, _) in enumerate(marks) if name], dtype=np.int64)
