@@ -175,6 +175,8 @@ def expert_load(count: torch.Tensor, expert_ranks: int) -> torch.Tensor:
     """Tokens of each expert-parallel rank, in permille of the even share: a
     rank's slow expert kernels at 1300 are no sign of a slow machine. Experts
     are spread over the ranks in equal, consecutive parts."""
+    if expert_ranks < 1 or len(count) % expert_ranks:
+        raise argus.ArgusError(f"rank_check: {len(count)} experts do not spread evenly over {expert_ranks} ranks")
     c = count.to(torch.int64).view(expert_ranks, -1).sum(1)
     return c * (1000 * expert_ranks) // c.sum().clamp(min=1)
 
@@ -195,16 +197,18 @@ def main(argv: Optional[Sequence[str]] = None) -> int:
             print(f"{f}: score {r['score_pm'][i].tolist()} permille, straggler in {int(r['straggler'][i].sum())} of "
                   f"{len(r['straggler'][i])} segments, degraded operators: {', '.join(slow) or 'none'}")
         return 0
+    if a.expert_ranks < 1 or Config.experts % a.expert_ranks:
+        ap.error(f"--expert-ranks has to divide the step's {Config.experts} experts")
     check = RankCheck()
     t = check.trace(a.steps, a.window)
+    if a.save:
+        np.savez(a.save, **t)
     took = (t["end_ns"] - t["start_ns"]) / 1e3
     for k, name in enumerate(NAMES):
         d = took[t["kernel_id"] == k]
         print(f"{name:20s} median {np.median(d):9.1f} us   p99 {np.quantile(d, 0.99):9.1f} us")
     load = expert_load(check.step()["count"], a.expert_ranks)
     print(f"tokens of {a.expert_ranks} expert-parallel ranks, permille of the even share: {load.tolist()}")
-    if a.save:
-        np.savez(a.save, **t)
     return 0
 
 

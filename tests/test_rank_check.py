@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2606_20374_amd import argus
 from paper_2606_20374_amd import rank_check as rc
 
 
@@ -52,3 +53,16 @@ def test_durations_of_a_long_trace(monkeypatch):
     assert (np.abs(took - want) <= 1 + want * 2.0**-23).all()
     # one operator begins where the one before it ended
     assert (t["start_ns"][1:] == t["end_ns"][:-1]).all()
+
+
+@pytest.mark.parametrize("ranks", ["7", "0", "-8", "256"])
+def test_expert_ranks_that_do_not_divide_the_experts_are_refused_before_the_run(monkeypatch, ranks):
+    def none(*args):
+        raise AssertionError("the step was run")
+
+    monkeypatch.setattr(rc, "RankCheck", none)
+    with pytest.raises(SystemExit) as e:
+        rc.main(["--expert-ranks", ranks])
+    assert e.value.code == 2
+    with pytest.raises(argus.ArgusError):
+        rc.expert_load(torch.ones(128, dtype=torch.int32), int(ranks))
