@@ -3,9 +3,10 @@
  *
  * argus_cross_rank and argus_l2 name ranks and (rank, kernel) pairs that are
  * slow. Whether the machine is slow or its work was larger is answered by
- * running a step with known outputs on it and comparing its times with its
- * peers' through the same summaries, and by the per-expert token counts of
- * the step's router. The operators each bound another part of the GPU:
+ * running the same seeded step on it and on its peers, and comparing their
+ * times through the same summaries and the bits of their outputs, and by the
+ * per-expert token counts that argus_balance gives for the job's own router.
+ * The operators each bound another part of the GPU:
  *
  *   argus_embedding    token lookup with scaling (gather), and the table's
  *                      gradient by sorted tokens (sort, segmented sums)

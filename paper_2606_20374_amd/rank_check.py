@@ -5,10 +5,13 @@ slow. To tell a slow machine from one that had more work, every rank of
 interest runs the same seeded step here: token embedding, layer norm,
 attention over packed documents, the top-k router with its balance loss, and
 their gradients, with the library's matrix products between them. The
-operators' durations become one rank's kernel events, `compare` puts the
-events of several ranks through argus_summarize, argus_cross_rank and
-argus_iter_windows, and `expert_load` says how uneven the router's tokens are
-over expert-parallel ranks.
+operators' durations become one rank's kernel events, and the bits of the
+step's outputs, the same on every sound machine, a digest beside them.
+`compare` puts the events of several ranks through argus_summarize,
+argus_cross_rank and argus_iter_windows, and names the ranks whose outputs
+differ from the others'. `expert_load` says how uneven a router's tokens are
+over expert-parallel ranks, from the counts that argus_balance gives: the
+job's own, where its expert kernels are in question.
 
     python -m paper_2606_20374_amd.rank_check --save rank0.npz
     python -m paper_2606_20374_amd.rank_check --compare rank0.npz rank1.npz rank2.npz
@@ -17,6 +20,7 @@ from __future__ import annotations
 
 import argparse
 import dataclasses
+import hashlib
 from typing import Optional, Sequence
 
 import numpy as np
@@ -28,6 +32,10 @@ from . import argus, ops
 NAMES = ("embedding", "norm1", "qkv_product", "attention", "out_product", "norm2", "router_product", "balance",
          "balance_bwd", "router_product_bwd", "norm2_bwd", "out_product_bwd", "attention_bwd", "qkv_product_bwd",
          "norm1_bwd", "embedding_bwd")
+
+
+# what a step returns
+OUTPUTS = ("h", "expert", "gate", "count", "loss", "d_table", "d_norm1", "d_norm2", "d_qkv", "d_out", "d_router")
 
 
 @dataclasses.dataclass(frozen=True)
@@ -122,9 +130,11 @@ class RankCheck:
 
     def trace(self, steps: int = 6, window: int = 10, warmup: int = 3) -> dict:
         """One rank's kernel events over `steps` segments of `window` runs
-        each: the arrays of argus_summarize with seg_off, on the host."""
+        each: the arrays of argus_summarize with seg_off, on the host, and the
+        digest of the last run's outputs."""
         for _ in range(warmup):
             self.step()
+        last = {}
         stream = torch.cuda.current_stream(self.device)
         begin, marks = torch.cuda.Event(enable_timing=True), []
 
@@ -137,7 +147,8 @@ class RankCheck:
         begin.record(stream)
         for _ in range(steps * window):
             mark(None)  # the step's begin
-            self.step(mark)
+            last = {}  # the run before's memory serves this one
+            last = self.step(mark)
         torch.cuda.synchronize(self.device)
         # a difference of events is a 32-bit number of milliseconds: each is taken
         # from its neighbour, which keeps the nanoseconds however long the trace
@@ -147,14 +158,37 @@ class RankCheck:
         start = np.array([at[i - 1] for i, (name, _) in enumerate(marks) if name], dtype=np.int64)
         end = np.array([at[i] for i, (name, _) in enumerate(marks) if name], dtype=np.int64)
         seg = np.arange(steps + 1, dtype=np.int64) * window * len(NAMES)
-        return {"kernel_id": kid, "stream": np.zeros_like(kid), "start_ns": start, "end_ns": end, "seg_off": seg}
+        return {"kernel_id": kid, "stream": np.zeros_like(kid), "start_ns": start, "end_ns": end, "seg_off": seg,
+                "digest": digest(last)}
+
+
+def digest(outputs: dict) -> np.ndarray:
+    """64 bits of the SHA-256 of each output's bits, in the dict's order."""
+    d = []
+    for v in outputs.values():
+        h = hashlib.sha256()
+        for t in v if isinstance(v, tuple) else (v,):
+            h.update(t.detach().contiguous().view(torch.uint8).cpu().numpy())
+        d.append(int.from_bytes(h.digest()[:8], "little"))
+    return np.array(d, dtype=np.uint64)
+
+
+def outputs_differ(digests: Sequence[np.ndarray]) -> np.ndarray:
+    """[ranks][outputs]: whether a rank's output is another than most ranks
+    have; where no value has a majority, every rank's is taken to differ."""
+    if any(len(d) != len(digests[0]) for d in digests):
+        raise argus.ArgusError("rank_check: the traces have different numbers of outputs")
+    a = np.stack(digests)
+    same = (a[:, None] == a[None]).sum(1)  # ranks that agree with each, itself among them
+    return 2 * same <= len(a)
 
 
 def compare(traces: Sequence[dict], device="cuda", **params) -> dict:
     """The events of several ranks (as RankCheck.trace gives them, equally many
     segments each) through summarize, cross-rank and iteration windows. Keys:
     `summary`, `cross_rank`, `windows`, and per rank `score_pm` and `straggler`
-    [ranks][steps], per (rank, operator) `degraded` (any step)."""
+    [ranks][steps], per (rank, operator) `degraded` (any step), and where all
+    traces have their digests `outputs_differ` [ranks][OUTPUTS]."""
     R, S, K = len(traces), len(traces[0]["seg_off"]) - 1, len(NAMES)
     if any(len(t["seg_off"]) - 1 != S for t in traces):
         raise argus.ArgusError("rank_check: the traces have different numbers of segments")
@@ -167,8 +201,11 @@ def compare(traces: Sequence[dict], device="cuda", **params) -> dict:
     x = argus.cross_rank(s["count"], s["sum_ns"], R, S, K, **params)
     w = argus.iter_windows(s["step_ns"], R, S)
     flags = x["flags"].view(R, S, K)
-    return {"summary": s, "cross_rank": x, "windows": w, "score_pm": x["score_pm"].view(R, S).cpu(),
-            "straggler": x["straggler"].view(R, S).cpu(), "degraded": (flags & 8).ne(0).any(1).cpu()}
+    r = {"summary": s, "cross_rank": x, "windows": w, "score_pm": x["score_pm"].view(R, S).cpu(),
+         "straggler": x["straggler"].view(R, S).cpu(), "degraded": (flags & 8).ne(0).any(1).cpu()}
+    if all("digest" in t for t in traces):
+        r["outputs_differ"] = outputs_differ([t["digest"] for t in traces])
+    return r
 
 
 def expert_load(count: torch.Tensor, expert_ranks: int) -> torch.Tensor:
@@ -194,8 +231,12 @@ def main(argv: Optional[Sequence[str]] = None) -> int:
         r = compare(traces)
         for i, f in enumerate(a.compare):
             slow = [NAMES[k] for k in range(len(NAMES)) if r["degraded"][i, k]]
+            other = ""
+            if "outputs_differ" in r:
+                names = [n for n, x in zip(OUTPUTS, r["outputs_differ"][i]) if x]
+                other = f"; OUTPUTS DIFFER: {', '.join(names)}" if names else "; outputs as the others'"
             print(f"{f}: score {r['score_pm'][i].tolist()} permille, straggler in {int(r['straggler'][i].sum())} of "
-                  f"{len(r['straggler'][i])} segments, degraded operators: {', '.join(slow) or 'none'}")
+                  f"{len(r['straggler'][i])} segments, degraded operators: {', '.join(slow) or 'none'}{other}")
         return 0
     if a.expert_ranks < 1 or Config.experts % a.expert_ranks:
         ap.error(f"--expert-ranks has to divide the step's {Config.experts} experts")
@@ -208,7 +249,8 @@ def main(argv: Optional[Sequence[str]] = None) -> int:
         d = took[t["kernel_id"] == k]
         print(f"{name:20s} median {np.median(d):9.1f} us   p99 {np.quantile(d, 0.99):9.1f} us")
     load = expert_load(check.step()["count"], a.expert_ranks)
-    print(f"tokens of {a.expert_ranks} expert-parallel ranks, permille of the even share: {load.tolist()}")
+    print(f"tokens of the step's router on {a.expert_ranks} expert-parallel ranks, permille of the even share: "
+          f"{load.tolist()}")
     return 0
 
 

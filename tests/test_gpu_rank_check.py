@@ -155,3 +155,32 @@ def test_graph_replays():
             for n, t in o.items():
                 if n != "_workspace":
                     assert torch.equal(got[m][n], t), (i, m, n)
+
+
+def test_outputs_of_a_machine_that_computes_wrongly_are_named(tmp_path, capsys, monkeypatch):
+    good = [rc.RankCheck(SMALL).trace(steps=2, window=8) for _ in range(3)]
+    assert tuple(rc.RankCheck(SMALL).step()) == rc.OUTPUTS
+    right = pa.ops.balance_bwd
+
+    def wrong(*args, **kw):  # one bit of one logit's gradient
+        out = right(*args, **kw)
+        out["dlogits"].view(torch.int16)[5, 2] ^= 1 << 12
+        return out
+
+    monkeypatch.setattr(pa.ops, "balance_bwd", wrong)
+    bad = rc.RankCheck(SMALL).trace(steps=2, window=8)
+    d = rc.compare([*good, bad])["outputs_differ"]
+    assert not d[:3].any()
+    named = {n for n, x in zip(rc.OUTPUTS, d[3]) if x}
+    assert "d_router" in named and not named & {"h", "expert", "gate", "count", "loss"}
+    files = [str(tmp_path / f"r{i}.npz") for i in range(4)]
+    for f, t in zip(files, [*good, bad]):
+        np.savez(f, **t)
+    assert rc.main(["--compare", *files]) == 0
+    lines = capsys.readouterr().out.splitlines()
+    assert all("outputs as the others'" in x for x in lines[:3]) and "OUTPUTS DIFFER" in lines[3] and "d_router" in lines[3]
+    # events saved without their outputs are still compared by their times
+    for f, t in zip(files, [*good, bad]):
+        np.savez(f, **{k: v for k, v in t.items() if k != "digest"})
+    assert rc.main(["--compare", *files]) == 0
+    assert all(x.rpartition("operators: ")[2].count(";") == 0 for x in capsys.readouterr().out.splitlines())

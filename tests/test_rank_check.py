@@ -66,3 +66,22 @@ def test_expert_ranks_that_do_not_divide_the_experts_are_refused_before_the_run(
     assert e.value.code == 2
     with pytest.raises(argus.ArgusError):
         rc.expert_load(torch.ones(128, dtype=torch.int32), int(ranks))
+
+
+def test_ranks_whose_outputs_differ():
+    # four ranks of three outputs: one rank alone with its first, two pairs
+    # with their second (no majority: all are named), all alike in the third
+    d = np.array([[1, 5, 9], [1, 5, 9], [2, 6, 9], [1, 6, 9]], dtype=np.uint64)
+    want = [[False, True, False], [False, True, False], [True, True, False], [False, True, False]]
+    assert rc.outputs_differ(list(d)).tolist() == want
+    assert rc.outputs_differ([d[0]]).tolist() == [[False] * 3]
+    with pytest.raises(argus.ArgusError):
+        rc.outputs_differ([d[0], d[0][:2]])
+
+
+def test_digest_tells_bits():
+    a = {"x": torch.tensor([1.0, 0.0]), "y": (torch.ones(3, dtype=torch.bfloat16), torch.zeros(2))}
+    b = {"x": torch.tensor([1.0, -0.0]), "y": (torch.ones(3, dtype=torch.bfloat16), torch.zeros(2))}
+    c = {"x": torch.tensor([1.0, 0.0]), "y": (torch.ones(3, dtype=torch.bfloat16), torch.zeros(2) + 1e-40)}
+    da, db, dc = (rc.digest(x) for x in (a, b, c))
+    assert (da == rc.digest(a)).all() and (da != db).tolist() == [True, False] and (da != dc).tolist() == [False, True]
