@@ -10,6 +10,7 @@ of sum |q k| scale, below 2^-15 for the values here):
   dq  dS is rounded as an operand, dq once: scale (u + w) sum P (|dP| + |delta|)
       |k| + u |dq|;  dk likewise over its queries
   lse 2^-20 (1 + |lse|) + w 2^-6"""
+import ctypes
 import math
 
 import pytest
@@ -17,6 +18,7 @@ import torch
 
 import paper_2606_20374_amd as pa
 from paper_2606_20374_amd import argus as A
+from paper_2606_20374_amd import ops
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -366,3 +368,25 @@ def test_single_tokens_of_head_major_tensors():
             assert torch.equal(f[n], want[n]), n
         for n in ("dq", "dk", "dv"):
             assert torch.equal(d[n], d_want[n]), n
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lens,H,N", [([1300, 700], 8, 1), ([900, 1400], 6, 2), ([2100], 3, 1)])
+def test_shared_tiles(lens, H, N, causal, D):
+    # few tiles and heads: several workgroups share a tile of keys, their parts
+    # begin inside a query head, and (long keys) a tile of queries
+    T = sum(lens)
+    p = ops.Attention(len(lens), H, N, D, int(causal), 1, 1.0, T, T, 0x1000, 0x1000, H * D, D, N * D, D, N * D, D, None)
+    up = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    unshared = 256 + 2 * up(8 * (T // 128 + len(lens))) + up(8 * T * H)
+    # at least two workgroups' 32-bit sums of dk and dv
+    assert ops._lib().argus_attention_bwd_workspace(ctypes.byref(p)) >= unshared + 2 * 2 * T * N * D * 4
+    _run(lens, lens, H, N, D, causal)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_shared_tiles_of_uneven_sides(causal):
+    # dk and dv: one document has more queries than keys, one fewer
+    _run([2500, 300], [700, 1100], 4, 1, 64, causal)
+    _run([600, 900], [2300, 100], 4, 2, 128, causal)
