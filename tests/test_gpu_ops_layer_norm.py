@@ -6,10 +6,13 @@ sum of magnitudes. So the mean is off by dm = G mean|x|, the deviations'
 square root by (G + 2^-22) of itself plus dm, and a normalised value by
 e = rstd dm (1 + |xhat|) + (G + 2^-21) |xhat|, twice that covering second
 order; sums over r rows add at most r 2^-24 of their terms' magnitudes."""
+import ctypes
+
 import pytest
 import torch
 
 import paper_2606_20374_amd as pa
+from paper_2606_20374_amd import ops
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -153,3 +156,16 @@ def test_backward_against_differences():
     rounding = (dy.double().abs() * (f["y"].cpu().double().abs() + 1) * (G + 2.0**-20)).sum() / 2.0**-4
     assert abs(near - want) <= abs(wide - near) + rounding, (near, want, wide)
     assert rounding < 0.05 * abs(want) + 1  # the bound says something
+
+
+@pytest.mark.parametrize("dtype,wdtype", [(torch.float32, torch.float32), (torch.bfloat16, torch.float32),
+                                          (torch.float16, torch.float16)])
+@pytest.mark.parametrize("rows,cols", [(20_001, 24), (17_000, 200), (2_501, 2_048), (1_700, 5_000), (1_300, 8_192)])
+def test_rows_that_follow_one_another_in_a_workgroup(rows, cols, dtype, wdtype):
+    # more rows than all workgroups take at once: each takes two or more
+    test_forward(rows, cols, dtype, wdtype)
+    test_backward(rows, cols, dtype, wdtype)
+    p = ops.LayerNorm(rows, cols, ops.DTYPES[dtype], ops.DTYPES[wdtype], 1e-5, cols, cols)
+    groups = ops._lib().argus_layer_norm_bwd_workspace(ctypes.byref(p)) // (8 * cols)
+    narrow = cols <= (512 if dtype == torch.float32 else 1024)  # four rows to a workgroup
+    assert rows > groups * (4 if narrow else 1)
