@@ -225,3 +225,26 @@ def test_gradient_of_repeated_choices_adds_them_in_order(dtype):
     # the sums by less
     tol = p * 2.0**-15 * (gr + s) + UNIT[dtype] * ref.abs() + TINY[dtype]
     assert torch.all((got - ref).abs() <= tol)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,E,K", [(1500, 24, 3), (6000, 8, 2), (20_000, 8, 2), (20_011, 40, 9), (34_000, 160, 4),
+                                   (20_000, 384, 8)])
+def test_tokens_that_share_a_workgroup(T, E, K, dtype):
+    # several wavefronts to a workgroup, and past 16,384 tokens (or fewer, of
+    # many experts) several tokens to each group of lanes
+    x = _logits(T, E, dtype, "ties" if T % 2 else "normal")
+    g = torch.Generator().manual_seed(8)
+    mask = (torch.rand(T, generator=g) < 0.9).to(torch.uint8)
+    x[mask == 0] = float("nan")
+    got = pa.balance(x.to(DEV), K, mask=mask.to(DEV), alpha=0.02)
+    _check(got, _reference(x, K, mask, 0.02), x, T)
+    assert int(got["dev_status"]) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,E,K", [(33_000, 24, 3), (70_003, 12, 5), (100_000, 160, 16)])
+def test_gradient_of_tokens_that_share_a_row(T, E, K, dtype):
+    # past 32,768 tokens each group of lanes takes several, one after the
+    # other, and clears its row of gate gradients between them
+    test_gradient(T, E, K, 0, dtype)
