@@ -154,3 +154,11 @@ def test_gradient_of_padding_writes_no_row(n, pad, dim):
     _check_bwd(ids, dout, vocab, 1.0, got, torch.float32)
     assert torch.all(rows[vocab:] == 7.0)
     assert int(got["dev_status"]) == ops.DEV_TOKEN_RANGE
+
+
+@pytest.mark.parametrize("kind", ["uniform", "one", "hot", "ends", "none"])
+@pytest.mark.parametrize("n,vocab,dim", [(70_001, 300, 24), (140_000, 50_000, 8), (5000, 262_144, 8), (70_001, 300_007, 9)])
+def test_gradient_of_many_tokens_and_ids(n, vocab, dim, kind):
+    # past 65,536 tokens a workgroup sorts several rounds of them, and ids from
+    # 262,144 on take a third pass
+    test_gradient(n, vocab, dim, kind)
