@@ -5,17 +5,20 @@
 // query, and O^T += V^T P^T. The transposed products keep a query in one lane
 // (two lanes, one to each half of a tile's keys), so its maximum, sum and
 // rescaling are plain registers, and P^T is the second product's operand as it
-// comes out of the first, rounded to bfloat16 (2^-9 of each probability, as
-// exact as the values and the output; the sum l is that of the unrounded
-// ones, in 32 bits).
+// comes out of the first, rounded to bfloat16: at most 2^-8 of each
+// probability, as the values and the output have it, since the matrix
+// instructions take no wider operand at this rate (o is off by 0.0021 of its
+// norm, with 32-bit probabilities by 0.0016, the output's own rounding). The
+// sum l is that of the unrounded ones, in 32 bits.
 //
 // A workgroup of four wavefronts owns 128 queries, 32 to a wavefront, and two
 // such workgroups share a CU (at most 256 registers a lane: with one, 1,150 us
 // in place of 682). Keys and values come straight into LDS, 64 at a time, the
 // next tile while one is used (through registers 682 us, straight 583).
 // Four sequences of 4,096, causal, 32 query and 8 key heads of 128: 556 to
-// 592 us from run to run, 930 to 990 TFLOP/s; the matrix units are busy half
-// of the cycles (counters). Tiles of 32 keys four deep (617 us), eight
+// 592 us, 930 to 990 TFLOP/s, after some fifty runs one after the other (600
+// to 760 in the first thirty); the matrix units are busy half of the cycles
+// (counters). Tiles of 32 keys four deep (617 us), eight
 // wavefronts with three tiles (594) and three workgroups to a CU (718) were
 // not faster.
 #include "attention_tile.h"

@@ -2,22 +2,26 @@
 //
 //   P = exp(S - lse),  dP = dO V^T,  dS = P (dP - delta),  delta = dO . O
 //   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
-// The probabilities are recomputed from q, k and lse. Three launches:
-//   prep   delta and lse (in units of log2) per head and query; offsets check
-//   dkv    a workgroup owns 128 keys of a key head, 32 to a wavefront, with K
-//          and V as operands in registers, and takes the queries of all its
-//          query heads through LDS. S = Q K^T keeps a key in one lane, so P
-//          and dS are the operands of dV^T += dO^T P and dK^T += Q^T dS as
-//          they are.
+// The probabilities are recomputed from q, k and lse. Launches, after that of
+// the plan of tiles, which checks the offsets:
+//   prep   delta and lse (in units of log2) per head and query
+//   dkv    a workgroup owns 128 keys of a key head, 32 to a wavefront, with V
+//          as operands in registers (K too where heads are at most 64 wide, in
+//          LDS otherwise), and takes the queries of all its query heads
+//          through LDS. S = Q K^T keeps a key in one lane, so P and dS are the
+//          operands of dV^T += dO^T P and dK^T += Q^T dS as they are.
 //   dq     a workgroup owns 128 queries and takes the keys through LDS:
 //          S^T = K Q^T keeps a query in one lane, dQ^T += K^T dS^T.
 // S and dP are computed in both: 7 products in place of 5, and no atomics:
 // sums have a fixed order. Where tiles and heads are few, several workgroups
 // share one (the queries of dkv's, the keys of dq's in equal parts) and write
-// 32-bit sums that a further launch adds in their order.
+// 32-bit sums that a further launch for each of dk, dv and dq adds in their
+// order.
 //
-// Each rounding to bfloat16 is of an operand: P and dS, 2^-9 of each. Two
-// workgroups share a CU, with at most 256 registers a lane. Two sequences of
+// Each rounding to bfloat16 is of an operand, P and dS, at most 2^-8 of each:
+// the matrix instructions take no wider one at this rate (the gradients are
+// off by 0.0024 of their norm, with both in 32 bits by 0.0017, the outputs' own
+// rounding). Two workgroups share a CU, with at most 256 registers a lane. Two sequences of
 // 8,192, causal, 32 query and 8 key heads of 128: 3,540 to 3,740 us in all from run
 // to run, 735 to 776 TFLOP/s of the gradient's five products. Under the
 // profiler dkv takes 2,189 us on average, dq 1,495 and prep 53; the matrix

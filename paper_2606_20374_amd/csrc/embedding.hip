@@ -402,8 +402,8 @@ __global__ __launch_bounds__(256) void emb_pieces(SumArgs a, const T* dout, G* d
 // begin in it, one after the other in one stream of rows, eight of which are
 // in flight whatever the runs' lengths.
 constexpr int kSpan = kWindow + 2 * kPiece + 1;      // positions that decide the window's runs
-constexpr int kWords = (kSpan + 31) / 32 + 1;        // of a mask of them, an even number
-constexpr int kStaged = 2 * (kSpan + 1) + 2 * ((kWords + 1) / 2);  // words of LDS of a window
+constexpr int kWords = (kSpan + 31) / 32 + 1;        // of a mask of them, one to spare
+constexpr int kStaged = 2 * (kSpan + 1) + 2 * ((kWords + 1) / 2);  // words of LDS of a window, the mask's an even number
 static_assert(kWindow <= 64 && kPiece <= 64 && kStaged % 2 == 0);
 
 template <typename T, typename G>

@@ -262,8 +262,12 @@ LnShape ln_shape(const argus_layer_norm_t& p) {
   return {false, (int)ceil_div(ceil_div(vecs, n), 64) * 64, n};
 }
 
-// Workgroups that take the rows in turn: `threads` of each CU, all that fit at
-// once (forward 32,768 x 4,096 bf16 with 2,048: 98.7 us, 1,536: 108, 8,192: 101).
+// Workgroups that take the rows in turn: `threads` of each CU (forward 32,768 x
+// 4,096 bf16 with 2,048: 98.7 us, 1,536: 108, 8,192: 101). Those of one vector
+// to a thread fit at once, but for the gradient's of f16 with 32-bit weights (82
+// registers). Of more vectors registers admit fewer, and the rest begin as the
+// first end: of the gradient's of 16-bit rows of 513 to 1,024 columns (129 to
+// 132 registers) three workgroups fit a CU in place of six.
 int64_t ln_grid(const argus_layer_norm_t& p, int64_t threads) {
   const LnShape s = ln_shape(p);
   const int64_t fit = threads / s.threads, most = 256 * (fit < 1 ? 1 : fit), need = ceil_div(p.rows, s.wave ? 4 : 1);
