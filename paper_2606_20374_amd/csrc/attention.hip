@@ -16,9 +16,9 @@
 // in place of 682). Keys and values come straight into LDS, 64 at a time, the
 // next tile while one is used (through registers 682 us, straight 583).
 // Four sequences of 4,096, causal, 32 query and 8 key heads of 128: 556 to
-// 592 us, 930 to 990 TFLOP/s, after some fifty runs one after the other (600
-// to 760 in the first thirty); the matrix units are busy half of the cycles
-// (counters). Tiles of 32 keys four deep (617 us), eight
+// 592 us, 930 to 990 TFLOP/s, after some fifty runs one after the other; the
+// first thirty take 600 to 760 us and the same cycles, at a lower clock. The
+// matrix units are busy half of the cycles (counters). Tiles of 32 keys four deep (617 us), eight
 // wavefronts with three tiles (594) and three workgroups to a CU (718) were
 // not faster.
 #include "attention_tile.h"

@@ -24,10 +24,10 @@
 // rounding). Two workgroups share a CU, with at most 256 registers a lane. Two sequences of
 // 8,192, causal, 32 query and 8 key heads of 128: 3,540 to 3,740 us in all from run
 // to run, 735 to 776 TFLOP/s of the gradient's five products. Under the
-// profiler dkv takes 2,189 us on average, dq 1,495 and prep 53; the matrix
+// profiler dkv takes 2,047 us, dq 1,391 and prep 50 after forty runs; the matrix
 // units are busy 59% of dkv's cycles and 64% of dq's (counters). 13 packed
 // documents, the longest of 3,812 tokens, 16 heads of 64: 226 to 233 us (dkv
-// 132, dq 96, prep 13 under the profiler).
+// 124, dq 92, prep 13 under the profiler).
 #include "attention_tile.h"
 
 #pragma clang fp contract(fast)

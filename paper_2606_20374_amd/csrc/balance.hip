@@ -17,7 +17,7 @@
 //             LDS row of the token, read back by the lanes that own the
 //             experts, and cleared.
 // Backward is bound by memory (logits read, dlogits written): 262,144 tokens
-// of 128 bf16 logits, top 8: 32.6 us, 30 at a large copy's 5.0 TB/s. Forward is
+// of 128 bf16 logits, top 8: 31 to 34 us, 30 at a large copy's 5.0 TB/s. Forward is
 // bound by the selection's instructions: 131,072 tokens of 256 32-bit logits,
 // top 8: 86 us, 29 at the copy's rate; the vector units are busy 77% of the
 // cycles, 1,011 instructions to four tokens (counters).
