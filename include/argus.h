@@ -103,7 +103,8 @@ enum {
   ARGUS_DEV_SUMMARY_STALLED = 256,  /* argus_summarize: a bounded wait inside the kernel expired in every one of
                                        its redo passes over some segment (never expected: it means a defect in
                                        the library or the device); that segment's cells may be incomplete */
-  ARGUS_DEV_TOKEN_RANGE = 512,     /* argus_embedding: a token id at or above n_vocab (taken as padding) */
+  ARGUS_DEV_TOKEN_RANGE = 512,     /* argus_embedding: a token id at or above n_vocab (taken as padding);
+                                      argus_cross_entropy: a label there (token not learned) */
   ARGUS_DEV_LOGITS = 1024          /* argus_balance: a token with a NaN logit or no finite largest one (left out) */
 };
 

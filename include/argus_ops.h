@@ -17,6 +17,14 @@
  *                      instructions)
  *   argus_balance      top-k router: softmax, chosen experts, per-expert
  *                      counts and the balance loss, and its gradient
+ *   argus_rotary       rotary positions of queries and keys, and their
+ *                      gradient (memory streaming, 64-bit angles)
+ *   argus_gated_ff     gated feed-forward block: two products, activation
+ *                      and gate, and its gradients (matrix instructions;
+ *                      few tokens: memory streaming)
+ *   argus_cross_entropy  the loss over a large vocabulary from the last
+ *                      hidden states, without the logits in memory, and its
+ *                      gradients (matrix instructions)
  *
  * The conventions are those of argus.h: device pointers owned by the caller,
  * a caller workspace where the *_workspace query is not 0 (256-byte aligned,
@@ -30,8 +38,9 @@
  *
  * Strides are counted in elements and are those of the outer dimensions; the
  * innermost dimension is always contiguous. Rows need no alignment beyond
- * their element's (attention: 16 bytes, see there), and rows that are only
- * read may coincide (stride 0, a broadcast input; not attention's). Outputs may not overlap
+ * their element's (attention, gated_ff and cross_entropy: 16 bytes, see
+ * there), and rows that are only read may coincide (stride 0, a broadcast
+ * input; not those three's). Outputs may not overlap
  * inputs or each other, except where noted.
  */
 #ifndef ARGUS_OPS_H
@@ -49,6 +58,11 @@ enum { ARGUS_F32 = 0, ARGUS_BF16 = 1, ARGUS_F16 = 2 }; /* element types */
 #define ARGUS_MAX_EXPERTS 1024     /* argus_balance: experts limit */
 #define ARGUS_MAX_TOP_K 16         /* argus_balance: experts per token limit */
 #define ARGUS_MAX_HEAD_DIM 128     /* argus_attention: head dimension limit */
+#define ARGUS_MAX_ROTARY_DIM 1024  /* argus_rotary: head dimension limit */
+#define ARGUS_MAX_FF_WIDTH 65536   /* argus_gated_ff: width limit */
+#define ARGUS_MAX_FF 131072        /* argus_gated_ff: inner width limit */
+#define ARGUS_MAX_CE_WIDTH 16384   /* argus_cross_entropy: width limit */
+#define ARGUS_MAX_CE_VOCAB 1048576 /* argus_cross_entropy: vocabulary limit */
 
 /* ---------------------------------------------------------------- embedding
  *
@@ -219,6 +233,120 @@ size_t argus_attention_bwd_workspace(const argus_attention_t* p);
 int argus_attention_bwd(const argus_attention_t* p, const void* d_o, const void* q, const void* k, const void* v,
                         const void* o, const float* lse, void* dq, void* dk, void* dv, void* workspace,
                         size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------- rotary
+ *
+ * Pair i of a token's head, i = 0 .. rot_dim / 2 - 1, is (x[i], x[i + rot_dim
+ * / 2]), or with interleaved set (x[2 i], x[2 i + 1]). With the angle a = pos
+ * freq[i], (u, v) becomes scale (u cos a - v sin a, u sin a + v cos a), in 32
+ * bits, rounded once; with inverse set a is taken as -a, which is the
+ * gradient's direction (the map's transpose). Elements from rot_dim on are
+ * copied. pos freq[i] / 2 pi is taken in 64 bits and its fraction alone goes
+ * on: positions up to 2^31 in size turn right to 1e-6 of a radian.
+ */
+typedef struct argus_rotary {
+  int64_t n_tokens;    /* 0 .. 2^28 */
+  int32_t n_heads;     /* 1 .. 65535 */
+  int32_t head_dim;    /* 2 .. ARGUS_MAX_ROTARY_DIM */
+  int32_t rot_dim;     /* even, 2 .. head_dim */
+  int32_t interleaved; /* 0 or 1 */
+  int32_t inverse;     /* 0 or 1 */
+  int32_t dtype;       /* of x, out */
+  float scale;         /* finite */
+  int32_t pos_64;      /* 1: pos is int64 */
+  const void* pos;     /* [n_tokens] int32 or int64, or NULL: 0, 1, 2, .. */
+  const double* freq;  /* [rot_dim / 2] radians a position */
+  int64_t x_tok, x_head;     /* strides of x, >= 0 */
+  int64_t out_tok, out_head; /* strides of out; heads and tokens may not overlap */
+} argus_rotary_t;
+
+/* out may be x with the same strides. */
+int argus_rotary(const argus_rotary_t* p, const void* x, void* out, void* stream);
+
+/* ----------------------------------------------------------------- gated_ff
+ *
+ * g = x wg^T, u = x wu^T, h = act(g) u, with act(g) = g / (1 + exp(-g))
+ * (ARGUS_SILU), g Phi(g) with the normal distribution's Phi (ARGUS_GELU), or
+ * g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 (ARGUS_GELU_TANH). The
+ * products have 32-bit sums, h is made of those and rounded once.
+ * Backward, from the rounded g and u: dg = d_h u act'(g), du = d_h act(g),
+ * both rounded to dtype as operands; dx = dg wg + du wu, dwg = dg^T x,
+ * dwu = du^T x.
+ */
+enum { ARGUS_SILU = 0, ARGUS_GELU = 1, ARGUS_GELU_TANH = 2 };
+
+typedef struct argus_gated_ff {
+  int64_t n_tokens; /* 0 .. 2^20 */
+  int32_t width;    /* a multiple of 8, 8 .. ARGUS_MAX_FF_WIDTH */
+  int32_t ff;       /* a multiple of 8, 8 .. ARGUS_MAX_FF */
+  int32_t dtype;    /* ARGUS_BF16 or ARGUS_F16, of every tensor */
+  int32_t act;
+  /* row strides: multiples of 8, at least the row's length, at most 2^21; all
+   * pointers to tensors are 16-byte aligned */
+  int64_t x_stride, wg_stride, wu_stride;
+  int64_t dh_stride; /* of d_h (argus_gated_ff_bwd) */
+} argus_gated_ff_t;
+
+/* x: [n_tokens][width]; wg, wu: [ff][width]; h: [n_tokens][ff], contiguous;
+ * g, u: like h, or both NULL where no backward pass follows. */
+size_t argus_gated_ff_workspace(const argus_gated_ff_t* p);
+int argus_gated_ff(const argus_gated_ff_t* p, const void* x, const void* wg, const void* wu, void* h, void* g, void* u,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* d_h: [n_tokens][ff]; g, u: the forward's, contiguous; dx: [n_tokens]
+ * [width], dwg, dwu: [ff][width], contiguous. */
+size_t argus_gated_ff_bwd_workspace(const argus_gated_ff_t* p);
+int argus_gated_ff_bwd(const argus_gated_ff_t* p, const void* d_h, const void* x, const void* wg, const void* wu,
+                       const void* g, const void* u, void* dx, void* dwg, void* dwu, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------ cross_entropy
+ *
+ * Per token: z = scale x w^T over the vocabulary, lse = log sum exp(z), loss =
+ * lse - z[label] + z_loss lse^2; mean = sum of loss / n_valid, n_valid the
+ * number of tokens that are learned (mean 0 if none). A token whose label is
+ * below 0 is not learned; one whose label is at or above n_vocab neither, and
+ * raises ARGUS_DEV_TOKEN_RANGE: loss 0, lse -infinity, and no gradient,
+ * whatever their rows of x hold. The logits are not kept.
+ * Backward, with c = dmean / max(n_valid, 1) + dloss[token] for a token that
+ * is learned: dz[v] = c scale (exp(z[v] - lse) (1 + 2 z_loss lse) - [v =
+ * label]), rounded to bfloat16 as an operand; dx = dz w, dw = dz^T x. n_valid
+ * divides dmean alone: with tokens on several ranks it may be their total.
+ */
+typedef struct argus_cross_entropy {
+  const void* labels; /* [n_tokens] int32 or int64 */
+  int64_t n_tokens;   /* 0 .. 2^20; n_tokens n_vocab below 2^38 */
+  int32_t ids_64;     /* 1: labels are int64 */
+  int32_t n_vocab;    /* 1 .. ARGUS_MAX_CE_VOCAB */
+  int32_t width;      /* a multiple of 8, 8 .. ARGUS_MAX_CE_WIDTH */
+  int32_t dtype;      /* ARGUS_BF16, of x, w, dx, dw */
+  float scale;        /* finite */
+  float z_loss;       /* finite, >= 0 */
+  /* row strides: multiples of 8, at least width, at most 2^21; all pointers to
+   * tensors are 16-byte aligned */
+  int64_t x_stride, w_stride;
+} argus_cross_entropy_t;
+
+typedef struct argus_cross_entropy_out {
+  float* loss;         /* [n_tokens] */
+  float* lse;          /* [n_tokens] */
+  float* mean;         /* [1] */
+  uint32_t* n_valid;   /* [1] */
+  int32_t* dev_status; /* optional (may be NULL) */
+} argus_cross_entropy_out_t;
+
+/* x: [n_tokens][width]; w: [n_vocab][width]. */
+size_t argus_cross_entropy_workspace(const argus_cross_entropy_t* p);
+int argus_cross_entropy(const argus_cross_entropy_t* p, const void* x, const void* w,
+                        const argus_cross_entropy_out_t* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* lse: the forward's; dmean: [1], with n_valid [1], or NULL; dloss: [n_tokens]
+ * or NULL; one of the two has to be there. dx: [n_tokens][width], dw: [n_vocab]
+ * [width], contiguous; dev_status: optional. */
+size_t argus_cross_entropy_bwd_workspace(const argus_cross_entropy_t* p);
+int argus_cross_entropy_bwd(const argus_cross_entropy_t* p, const void* x, const void* w, const float* lse,
+                            const uint32_t* n_valid, const float* dmean, const float* dloss, void* dx, void* dw,
+                            int32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

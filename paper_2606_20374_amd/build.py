@@ -8,7 +8,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libargus.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "summarize.hip", "cross_rank.hip", "iter_windows.hip", "kde.hip", "w1.hip", "l2.hip", "compact.hip",
-           "ops_api.hip", "embedding.hip", "layer_norm.hip", "balance.hip", "attention.hip", "attention_bwd.hip"]
+           "ops_api.hip", "embedding.hip", "layer_norm.hip", "balance.hip", "attention.hip", "attention_bwd.hip",
+           "rotary.hip", "gated_ff.hip", "cross_entropy.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HIP_FLAGS = [

@@ -1,0 +1,478 @@
+// Softmax cross entropy over a large vocabulary, straight from the last hidden
+// states: the logits z = scale x w^T live in registers only.
+//
+// Tokens that are learned are numbered first, in order, and their rows of x
+// copied together where some are left out, so that ignored tokens cost no
+// product and whatever their rows hold reaches nothing.
+// Forward: each tile of logits leaves its rows' maximum and sum of
+// exponentials; a further launch joins a row's tiles.
+// Backward: a piece of the vocabulary at a time, the logits again, and
+//   dz = c / C (exp(z - lse) (1 + 2 z_loss lse) - [v = label]),
+// rounded to bfloat16 as the operand of dw = C scale dz^T x, which is final for
+// these ids, and dx += C scale dz w, which is summed over the pieces in 32
+// bits. C is the largest |c|: with a factor that all tokens share in the
+// operand, dz of most labels, -c, would round by the same part of itself, and
+// the sums by as much (0.0029 of their norm for 0.0023).
+#include "product.h"
+
+namespace argus {
+using namespace product;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// The learned tokens, in order.
+struct Tokens {
+  uint32_t* n;      // [1] how many
+  float* most;      // [1] largest |coef| that is finite, 1 if that is 0; backward
+  int32_t* index;   // [n] token
+  int32_t* label;   // [n]
+  int32_t* place;   // [T] number of a token, -1: not learned
+  float *coef, *lse;  // [n], backward
+  bf16_t* x;        // [n][W], where n < T
+};
+
+struct CeArgs {
+  Tokens t;
+  Operand x, w;
+  const void* labels;
+  int32_t ids_64;
+  int64_t T, V;
+  float scale, z_loss;
+};
+
+constexpr int kIndexThreads = 1024, kEach = 8;
+
+struct IndexArgs {
+  float *loss, *lse_out;  // forward: of tokens that are not learned
+  uint32_t* n_valid;
+  const float *lse, *dloss, *dmean;  // backward
+  const uint32_t* divisor;
+  int32_t* status;
+};
+
+__global__ __launch_bounds__(kIndexThreads) void ce_index(CeArgs a, IndexArgs o) {
+  __shared__ uint32_t sums[kIndexThreads / 64];
+  __shared__ float tops[kIndexThreads / 64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if (o.status && threadIdx.x == 0) *o.status = 0;
+  __syncthreads();
+  float mean = 0;
+  if (o.dmean) {
+    const uint32_t d = *o.divisor;
+    mean = *o.dmean / (float)(d ? d : 1);
+  }
+  uint32_t base = 0;
+  float top = 0;
+  bool range = false;
+  for (int64_t t0 = 0; t0 < a.T; t0 += kIndexThreads * kEach) {
+    const int64_t mine = t0 + (int64_t)threadIdx.x * kEach;
+    int64_t id[kEach];
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      id[j] = -1;
+      if (mine + j < a.T) id[j] = a.ids_64 ? ((const int64_t*)a.labels)[mine + j] : ((const int32_t*)a.labels)[mine + j];
+      if (id[j] >= a.V) {
+        range = true;
+        id[j] = -1;
+      }
+      n += id[j] >= 0;
+    }
+    uint32_t before = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t v = __shfl_up(before, d);
+      if (lane >= d) before += v;
+    }
+    if (lane == 63) sums[w] = before;
+    __syncthreads();
+    uint32_t at = base + before - n, all = 0;
+#pragma unroll
+    for (int j = 0; j < kIndexThreads / 64; ++j) {
+      if (j < w) at += sums[j];
+      all += sums[j];
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int64_t t = mine + j;
+      if (t >= a.T) break;
+      if (id[j] >= 0) {
+        a.t.index[at] = (int32_t)t;
+        a.t.label[at] = (int32_t)id[j];
+        if (o.lse) {
+          a.t.lse[at] = o.lse[t];
+          const float c = mean + (o.dloss ? o.dloss[t] : 0.0f);
+          a.t.coef[at] = c;
+          if (fabsf(c) < __builtin_inff()) top = fmaxf(top, fabsf(c));
+        }
+        ++at;
+      } else if (o.loss) {
+        o.loss[t] = 0.0f;
+        o.lse_out[t] = -__builtin_inff();
+      }
+      if (a.t.place) a.t.place[t] = id[j] >= 0 ? (int32_t)at - 1 : -1;
+    }
+    base += all;
+    __syncthreads();
+  }
+  if (range && o.status) atomicOr(o.status, ARGUS_DEV_TOKEN_RANGE);
+  if (a.t.most) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) tops[w] = top;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    *a.t.n = base;
+    if (o.n_valid) *o.n_valid = base;
+    if (a.t.most) {
+      for (int j = 0; j < kIndexThreads / 64; ++j) top = fmaxf(top, tops[j]);
+      *a.t.most = top > 0.0f ? top : 1.0f;
+    }
+  }
+}
+
+// A row to a wavefront.
+__global__ __launch_bounds__(256) void ce_gather(CeArgs a) {
+  const int64_t n = *a.t.n, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (n == a.T || row >= n) return;
+  const bf16_t* from = (const bf16_t*)a.x.p + a.t.index[row] * a.x.stride;
+  bf16_t* to = a.t.x + row * a.x.k;
+  for (int64_t c = (threadIdx.x & 63) * 8; c < a.x.k; c += 512) store_vec<8>(to + c, load_vec<8>(from + c));
+}
+
+__device__ __forceinline__ Operand learned(const CeArgs& a, int64_t n) {
+  if (n == a.T) return a.x;
+  return {a.t.x, n, a.x.k, a.x.k};
+}
+
+__device__ __forceinline__ float other_half(float v) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return __builtin_bit_cast(float, (uint32_t)((threadIdx.x & 32) ? s[0] : s[1]));
+}
+
+template <class TT>
+__global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, float* own, int mt, int nt) {
+  __shared__ float2 join[TT::WN][TT::TM];
+  int m, n;
+  my_tile(mt, nt, m, n);
+  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n), m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
+  if (m0 >= count) return;
+  TT t;
+  const typename TT::LoadA la(learned(a, count), m0);
+  const typename TT::LoadB lb(a.w, n0);
+  t.run(la, lb, 0, (int)a.x.k);
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+  for (int i = 0; i < TT::FM; ++i) {
+    const int at = TT::row_of(i) + (lane & 31);
+    const int64_t label = m0 + at < count ? a.t.label[m0 + at] - n0 : -1;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float z = t.acc[i][j][e] * a.scale;
+        if (n0 + TT::TN > a.V && n0 + TT::col_of(j) + 8 * (e / 4) + 4 * half + e % 4 >= a.V) z = -__builtin_inff();
+        t.acc[i][j][e] = z;
+        top = fmaxf(top, z);
+      }
+    if (__any(label >= 0 && label < TT::TN)) {
+#pragma unroll
+      for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (label == TT::col_of(j) + 8 * (e / 4) + 4 * half + e % 4) own[m0 + at] = t.acc[i][j][e];
+    }
+    top = fmaxf(top, other_half(top));
+    const float from = top == -__builtin_inff() ? 0.0f : top;  // no difference of infinities
+    float sum = 0;
+#pragma unroll
+    for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((t.acc[i][j][e] - from) * kLog2e);
+    sum += other_half(sum);
+    if (half == 0) join[TT::wave() % TT::WN][at] = make_float2(top, sum);
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < TT::TM; r += TT::THREADS) {
+    if (m0 + r >= count) break;
+    float top = -__builtin_inff(), sum = 0;
+#pragma unroll
+    for (int j = 0; j < TT::WN; ++j) top = fmaxf(top, join[j][r].x);
+    const float from = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+    for (int j = 0; j < TT::WN; ++j) sum += join[j][r].y * __builtin_amdgcn_exp2f((join[j][r].x - from) * kLog2e);
+    part[(m0 + r) * nt + n] = make_float2(top, sum);
+  }
+}
+
+// A token to a wavefront.
+__global__ __launch_bounds__(256) void ce_join(CeArgs a, const float2* part, const float* own, int nt, float* loss,
+                                               float* lse) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= *a.t.n) return;
+  const int lane = threadIdx.x & 63;
+  float top = -__builtin_inff(), sum = 0;
+  for (int j = lane; j < nt; j += 64) top = fmaxf(top, part[row * nt + j].x);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float from = top == -__builtin_inff() ? 0.0f : top;
+  for (int j = lane; j < nt; j += 64) {
+    const float2 p = part[row * nt + j];
+    sum += p.y * __builtin_amdgcn_exp2f((p.x - from) * kLog2e);
+  }
+  sum = wave_sum_f32(sum);
+  if (lane == 0) {
+    const float rest = logf(sum), all = from + rest;
+    // the largest logit's distance first: a sure token's loss is what is left of the sum
+    loss[a.t.index[row]] = (from - own[row]) + rest + a.z_loss * all * all;
+    lse[a.t.index[row]] = all;
+  }
+}
+
+__global__ __launch_bounds__(1024) void ce_mean(const float* loss, int64_t T, const uint32_t* n, float* mean) {
+  __shared__ double sums[16];
+  double s = 0;
+  for (int64_t t = threadIdx.x; t < T; t += 1024) s += loss[t];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x) return;
+  s = 0;
+  for (int j = 0; j < 16; ++j) s += sums[j];
+  *mean = (float)(s / (*n ? *n : 1));
+}
+
+// dz of the ids [v0, v0 + cols) of the vocabulary, `cols` a multiple of 64.
+template <class TT>
+__global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64_t v0, int64_t cols, int64_t stride,
+                                                     int mt, int nt) {
+  int m, n;
+  my_tile(mt, nt, m, n);
+  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n), m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
+  if (m0 >= count) return;
+  TT t;
+  const typename TT::LoadA la(learned(a, count), m0);
+  const typename TT::LoadB lb(a.w, v0 + n0);
+  t.run(la, lb, 0, (int)a.x.k);
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+  for (int i = 0; i < TT::FM; ++i) {
+    const int64_t row = m0 + TT::row_of(i) + (lane & 31);
+    if (row >= count) continue;
+    const float lse = a.t.lse[row], f = a.t.coef[row] / *a.t.most, more = 1.0f + 2.0f * a.z_loss * lse;
+    const int64_t label = a.t.label[row] - v0;
+#pragma unroll
+    for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int64_t c = n0 + TT::col_of(j) + 2 * e + 4 * half;
+        if (c >= cols) continue;
+        Vec<bf16_t, 4> o;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float p = __builtin_amdgcn_exp2f((t.acc[i][j][e + u] * a.scale - lse) * kLog2e) * more;
+          if (c + u == label) p -= 1.0f;
+          o.e[u] = (bf16_t)(v0 + c + u < a.V ? f * p : 0.0f);
+        }
+        *(Vec<bf16_t, 4>*)(dz + row * stride + c) = o;
+      }
+  }
+}
+
+// dx of every token from the parts' sums: zeros where it is not learned.
+__global__ __launch_bounds__(256) void ce_dx(Tokens t, const float* sums, int32_t S, int64_t T, int64_t W, float scale,
+                                             bf16_t* dx) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= T * W) return;
+  const int64_t row = i / W, c = i - row * W;
+  const int64_t at = t.place[row];
+  const float f = *t.most * scale;
+  Vec<bf16_t, 8> o;
+  float v[8] = {};
+  if (at >= 0)
+    for (int s = 0; s < S; ++s) {
+      const Vec<float, 8> p = load_vec<8>(sums + ((int64_t)s * T + at) * W + c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += p.e[j];
+    }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) o.e[j] = (bf16_t)(v[j] * f);
+  store_vec<8>(dx + i, o);
+}
+
+__global__ __launch_bounds__(256) void ce_clear(bf16_t* p, int64_t n) {
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048)
+    *(uint4*)(p + i) = make_uint4(0, 0, 0, 0);
+}
+
+struct Space {
+  char* p;
+  size_t at = 0;
+  template <class T>
+  T* take(size_t n) {
+    T* r = (T*)(p + at);
+    at += align256(n * sizeof(T));
+    return r;
+  }
+};
+
+int64_t tiles_n(const argus_cross_entropy_t& p) { return ceil_div(p.n_vocab, is_big(p.n_tokens, p.n_vocab) ? 256 : 128); }
+// Ids of a piece: at most 2^27 values of dz where the tokens allow it.
+int64_t piece_of(const argus_cross_entropy_t& p) {
+  int64_t ids = ((int64_t)1 << 27) / (p.n_tokens > 0 ? p.n_tokens : 1) / 256 * 256;
+  if (ids < 4096) ids = 4096;
+  const int64_t all = ceil_div(p.n_vocab, 64) * 64;
+  return ids < all ? ids : all;
+}
+
+struct Forward {
+  Tokens t;
+  float2* part;
+  float* own;
+  size_t bytes;
+};
+Forward forward_space(const argus_cross_entropy_t& p, void* ws) {
+  Space s{(char*)ws};
+  const size_t T = (size_t)p.n_tokens;
+  Forward f{};
+  f.t.n = s.take<uint32_t>(1);
+  f.t.index = s.take<int32_t>(T);
+  f.t.label = s.take<int32_t>(T);
+  f.t.x = s.take<bf16_t>(T * (size_t)p.width);
+  f.part = s.take<float2>(T * (size_t)tiles_n(p));
+  f.own = s.take<float>(T);
+  f.bytes = s.at;
+  return f;
+}
+
+struct Backward {
+  Tokens t;
+  bf16_t* dz;
+  float *dx, *dw;
+  int64_t piece;
+  int32_t parts;  // of a piece's product for dx
+  size_t bytes;
+};
+Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
+  Space s{(char*)ws};
+  const size_t T = (size_t)p.n_tokens;
+  Backward b{};
+  b.piece = piece_of(p);
+  b.parts = parts_of(p.n_tokens, p.width, b.piece);
+  b.t.n = s.take<uint32_t>(1);
+  b.t.most = s.take<float>(1);
+  b.t.index = s.take<int32_t>(T);
+  b.t.label = s.take<int32_t>(T);
+  b.t.place = s.take<int32_t>(T);
+  b.t.coef = s.take<float>(T);
+  b.t.lse = s.take<float>(T);
+  b.t.x = s.take<bf16_t>(T * (size_t)p.width);
+  b.dz = s.take<bf16_t>(T * (size_t)b.piece);
+  b.dx = s.take<float>((size_t)b.parts * T * (size_t)p.width);
+  b.dw = s.take<float>(sums_bytes(b.piece, p.width, p.n_tokens) / 4);
+  b.bytes = s.at;
+  return b;
+}
+
+CeArgs args_of(const argus_cross_entropy_t& p, const Tokens& t, const void* x, const void* w) {
+  return {t, {x, p.n_tokens, p.width, p.x_stride}, {w, p.n_vocab, p.width, p.w_stride},
+          p.labels, p.ids_64, p.n_tokens, p.n_vocab, p.scale, p.z_loss};
+}
+
+hipError_t launch_tokens(const CeArgs& a, const IndexArgs& o, hipStream_t st) {
+  hipLaunchKernelGGL(ce_index, dim3(1), dim3(kIndexThreads), 0, st, a, o);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.T == 0) return e;
+  hipLaunchKernelGGL(ce_gather, dim3((unsigned)ceil_div(a.T, 4)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t cross_entropy_workspace_bytes(const argus_cross_entropy_t& p) { return forward_space(p, nullptr).bytes; }
+size_t cross_entropy_bwd_workspace_bytes(const argus_cross_entropy_t& p) { return backward_space(p, nullptr).bytes; }
+
+hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, const void* w,
+                                const argus_cross_entropy_out_t& o, void* ws, hipStream_t st) {
+  const Forward f = forward_space(p, ws);
+  const CeArgs a = args_of(p, f.t, x, w);
+  hipError_t e = launch_tokens(a, {o.loss, o.lse, o.n_valid, nullptr, nullptr, nullptr, nullptr, o.dev_status}, st);
+  if (e != hipSuccess) return e;
+  if (p.n_tokens > 0) {
+    auto go = [&](auto tile) {
+      using TT = decltype(tile);
+      const int mt = (int)ceil_div(p.n_tokens, TT::TM), nt = (int)ceil_div(p.n_vocab, TT::TN);
+      hipLaunchKernelGGL(ce_fwd<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, f.part, f.own, mt, nt);
+      return hipGetLastError();
+    };
+    e = is_big(p.n_tokens, p.n_vocab) ? go(Big<bf16_t, true, true>{}) : go(Small<bf16_t, true, true>{});
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(ce_join, dim3((unsigned)ceil_div(p.n_tokens, 4)), dim3(256), 0, st, a, f.part, f.own,
+                       (int)tiles_n(p), o.loss, o.lse);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(ce_mean, dim3(1), dim3(1024), 0, st, o.loss, p.n_tokens, f.t.n, o.mean);
+  return hipGetLastError();
+}
+
+hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* x, const void* w, const float* lse,
+                                    const uint32_t* n_valid, const float* dmean, const float* dloss, void* dx, void* dw,
+                                    int32_t* dev_status, void* ws, hipStream_t st) {
+  const Backward b = backward_space(p, ws);
+  const int64_t T = p.n_tokens, V = p.n_vocab, W = p.width;
+  hipError_t e;
+  if (T == 0) {
+    if (dev_status) {
+      const CeArgs a = args_of(p, b.t, x, w);
+      if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, dev_status}, st)) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(ce_clear, dim3(2048), dim3(256), 0, st, (bf16_t*)dw, V * W);
+    return hipGetLastError();
+  }
+  const CeArgs a = args_of(p, b.t, x, w);
+  if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, lse, dloss, dmean, n_valid, dev_status}, st)) != hipSuccess) return e;
+  for (int64_t v0 = 0; v0 < V; v0 += b.piece) {
+    const int64_t ids = V - v0 < b.piece ? V - v0 : b.piece, cols = ceil_div(ids, 64) * 64;
+    auto go = [&](auto tile) {
+      using TT = decltype(tile);
+      const int mt = (int)ceil_div(T, TT::TM), nt = (int)ceil_div(cols, TT::TN);
+      hipLaunchKernelGGL(ce_dz<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, b.dz, v0, cols, b.piece, mt, nt);
+      return hipGetLastError();
+    };
+    e = is_big(T, cols) ? go(Big<bf16_t, true, true>{}) : go(Small<bf16_t, true, true>{});
+    if (e != hipSuccess) return e;
+    Grad g{};
+    g.a = {b.dz, T, cols, b.piece};
+    g.b = {(const char*)w + v0 * p.w_stride * 2, W, ids, p.w_stride};
+    g.n = b.t.n;
+    g.rows = {nullptr, nullptr, T, T, 0};
+    g.S = b.parts;
+    g.sums = b.dx;
+    g.add = v0 > 0;
+    if ((e = launch_grad<bf16_t, true, false, false>(g, T, st)) != hipSuccess) return e;
+    Grad d{};
+    d.a = {b.dz, cols, T, b.piece};
+    d.b = a.x;
+    d.b1 = {b.t.x, W, T, W};
+    d.b.rows = W;
+    d.b.k = T;
+    d.n = b.t.n;
+    d.f = b.t.most;
+    d.scale = p.scale;
+    d.rows = {(bf16_t*)dw + v0 * W, nullptr, ids, ids, 0};
+    d.S = parts_of(ids, W, T);
+    d.sums = d.S > 1 ? b.dw : nullptr;
+    if ((e = launch_grad<bf16_t, false, false, true>(d, ids, st)) != hipSuccess) return e;
+    if (d.S > 1 && (e = launch_join<bf16_t>(d, ids, st)) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(ce_dx, dim3((unsigned)ceil_div(T * W, 2048)), dim3(256), 0, st, b.t, b.dx, b.parts, T, W, p.scale, (bf16_t*)dx);
+  return hipGetLastError();
+}
+
+}  // namespace argus

@@ -1,0 +1,186 @@
+// Gated feed-forward block, forward and backward.
+//
+// Forward: g = x Wg^T and u = x Wu^T of the same columns are summed in one
+// workgroup's registers, h = act(g) u leaves it.
+// Backward, from the forward's rounded g and u: dg = dh u act'(g) and
+// du = dh act(g), rounded to x's type as the operands that the matrix
+// instructions take (half a step each), lie side by side in the workspace;
+// dx = [dg | du] [Wg; Wu], [dWg; dWu] = [dg | du]^T x.
+#include "product.h"
+
+namespace argus {
+using namespace product;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
+
+// act(g) and its derivative.
+__device__ __forceinline__ float2 activation(float g, int act) {
+  if (act == ARGUS_SILU) {
+    const float s = logistic(g);
+    return make_float2(g * s, s * (1.0f + g * (1.0f - s)));
+  }
+  if (act == ARGUS_GELU) {
+    const float cdf = 0.5f * (1.0f + erff(g * 0.70710678f));
+    return make_float2(g * cdf, cdf + g * 0.39894228f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * g * g));
+  }
+  // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)), y = sqrt(2 / pi) (g + 0.044715 g^3)
+  const float s = logistic(1.5957691f * (g + 0.044715f * g * g * g));
+  return make_float2(g * s, s + g * s * (1.0f - s) * 1.5957691f * (1.0f + 0.134145f * g * g));
+}
+
+struct FfArgs {
+  Operand x, wg, wu;
+  void *h, *g, *u;
+  int32_t act, mt, nt;
+};
+
+template <class TT>
+struct LoadBoth {
+  using Half = LoadRows<TT::TN / 2, TT::THREADS>;
+  Half g, u;
+  __device__ __forceinline__ void load(int k0, typename TT::T* tile, bool whole) const {
+    g.load(k0, tile, whole);
+    u.load(k0, tile + TT::TN / 2 * kStep, whole);
+  }
+};
+
+template <class TT>
+__global__ __launch_bounds__(TT::THREADS) void ff_fwd(FfArgs a) {
+  using T = typename TT::T;
+  int m, n;
+  my_tile(a.mt, a.nt, m, n);
+  const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * (TT::TN / 2), F = a.wg.rows;
+  TT t;
+  const typename TT::LoadA la(a.x, m0);
+  t.run(la, LoadBoth<TT>{{a.wg, n0}, {a.wu, n0}}, 0, (int)a.x.k);
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < TT::FM; ++i) {
+    const int64_t row = m0 + TT::row_of(i) + (lane & 31);
+    if (row >= a.x.rows) continue;
+#pragma unroll
+    for (int j = 0; j < TT::FN / 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int64_t c = n0 + TT::col_of(j) + 2 * e + 4 * (lane >> 5);
+        if (c >= F) continue;  // F is a multiple of 8
+        Vec<T, 4> h, g, u;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float gv = t.acc[i][j][e + v], uv = t.acc[i][j + TT::FN / 2][e + v];
+          h.e[v] = (T)(activation(gv, a.act).x * uv);
+          g.e[v] = (T)gv;
+          u.e[v] = (T)uv;
+        }
+        *(Vec<T, 4>*)((T*)a.h + row * F + c) = h;
+        if (a.g) {
+          *(Vec<T, 4>*)((T*)a.g + row * F + c) = g;
+          *(Vec<T, 4>*)((T*)a.u + row * F + c) = u;
+        }
+      }
+  }
+}
+
+// dg and du of a row, eight columns to a thread: [rows][2][wide], zeros from F on.
+template <class T>
+__global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, const T* g, const T* u, T* to, int64_t rows,
+                                                int32_t F, int32_t wide, int32_t act) {
+  const int per = wide / 8;
+  const int64_t all = rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per;
+    const int c = (int)(i - row * per) * 8;
+    Vec<T, 8> dg, du;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dg.e[j] = du.e[j] = (T)0.0f;
+    if (c < F) {
+      const Vec<T, 8> d = load_vec<8>(dh + row * stride + c), gv = load_vec<8>(g + row * F + c), uv = load_vec<8>(u + row * F + c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float2 f = activation((float)gv.e[j], act);
+        dg.e[j] = (T)((float)d.e[j] * (float)uv.e[j] * f.y);
+        du.e[j] = (T)((float)d.e[j] * f.x);
+      }
+    }
+    store_vec<8>(to + row * 2 * wide + c, dg);
+    store_vec<8>(to + row * 2 * wide + wide + c, du);
+  }
+}
+
+int64_t wide_of(const argus_gated_ff_t& p) { return ceil_div(p.ff, 64) * 64; }
+size_t point_bytes(const argus_gated_ff_t& p) { return align256((size_t)p.n_tokens * 2 * (size_t)wide_of(p) * 2); }
+
+template <class T>
+hipError_t forward(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g, void* u,
+                   hipStream_t st) {
+  FfArgs a{{x, p.n_tokens, p.width, p.x_stride}, {wg, p.ff, p.width, p.wg_stride}, {wu, p.ff, p.width, p.wu_stride},
+           h, g, u, p.act, 0, 0};
+  auto go = [&](auto tile) {
+    using TT = decltype(tile);
+    a.mt = (int32_t)ceil_div(p.n_tokens, TT::TM);
+    a.nt = (int32_t)ceil_div(p.ff, TT::TN / 2);
+    hipLaunchKernelGGL(ff_fwd<TT>, dim3((unsigned)(a.mt * a.nt)), dim3(TT::THREADS), 0, st, a);
+    return hipGetLastError();
+  };
+  return is_big(p.n_tokens, 2 * (int64_t)p.ff) ? go(Big<T, true, true>{}) : go(Small<T, true, true>{});
+}
+
+template <class T>
+hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, const void* wg, const void* wu, const void* g,
+                    const void* u, void* dx, void* dwg, void* dwu, void* ws, hipStream_t st) {
+  const int64_t wide = wide_of(p), W = p.width, F = p.ff, N = p.n_tokens;
+  T* point = (T*)ws;
+  float* sums = (float*)((char*)ws + point_bytes(p));
+  hipError_t e;
+  if (N > 0) {
+    const int64_t need = ceil_div(N * (wide / 8), 256);
+    hipLaunchKernelGGL(ff_point<T>, dim3((unsigned)(need < 16384 ? need : 16384)), dim3(256), 0, st, (const T*)dh,
+                       p.dh_stride, (const T*)g, (const T*)u, point, N, p.ff, (int32_t)wide, p.act);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    Grad d{};
+    d.a = {point, N, 2 * wide, 2 * wide};
+    d.b = {wg, W, F, p.wg_stride};
+    d.b1 = {wu, W, F, p.wu_stride};
+    d.k1 = wide;
+    d.rows = {dx, nullptr, N, N, 0};
+    d.S = parts_of(N, W, 2 * wide);
+    d.sums = d.S > 1 ? sums : nullptr;
+    if ((e = launch_grad<T, true, true, false>(d, N, st)) != hipSuccess) return e;
+    if (d.S > 1 && (e = launch_join<T>(d, N, st)) != hipSuccess) return e;
+  }
+  Grad d{};
+  d.a = {point, 2 * wide, N, 2 * wide};
+  d.b = {x, W, N, p.x_stride};
+  d.rows = {dwg, dwu, F, wide, F};
+  d.S = parts_of(2 * wide, W, N);
+  d.sums = d.S > 1 ? sums : nullptr;
+  if ((e = launch_grad<T, false, false, false>(d, 2 * wide, st)) != hipSuccess) return e;
+  return d.S > 1 ? launch_join<T>(d, wide + F, st) : hipSuccess;
+}
+
+}  // namespace
+
+size_t gated_ff_workspace_bytes(const argus_gated_ff_t&) { return 0; }
+
+size_t gated_ff_bwd_workspace_bytes(const argus_gated_ff_t& p) {
+  const size_t a = sums_bytes(p.n_tokens, p.width, 2 * wide_of(p)), b = sums_bytes(2 * wide_of(p), p.width, p.n_tokens);
+  return point_bytes(p) + (a > b ? a : b);
+}
+
+hipError_t launch_gated_ff(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g,
+                           void* u, void*, hipStream_t st) {
+  if (p.n_tokens == 0) return hipSuccess;
+  return p.dtype == ARGUS_F16 ? forward<f16_t>(p, x, wg, wu, h, g, u, st) : forward<bf16_t>(p, x, wg, wu, h, g, u, st);
+}
+
+hipError_t launch_gated_ff_bwd(const argus_gated_ff_t& p, const void* dh, const void* x, const void* wg, const void* wu,
+                               const void* g, const void* u, void* dx, void* dwg, void* dwu, void* ws, hipStream_t st) {
+  return p.dtype == ARGUS_F16 ? backward<f16_t>(p, dh, x, wg, wu, g, u, dx, dwg, dwu, ws, st)
+                              : backward<bf16_t>(p, dh, x, wg, wu, g, u, dx, dwg, dwu, ws, st);
+}
+
+}  // namespace argus

@@ -62,6 +62,46 @@ bool bad_attention(const argus_attention_t* p) {
   return false;
 }
 
+bool bad_rotary(const argus_rotary_t* p) {
+  if (!p || p->n_tokens < 0 || p->n_tokens > (1 << 28) || p->n_heads < 1 || p->n_heads > 65535) return true;
+  if (p->head_dim < 2 || p->head_dim > ARGUS_MAX_ROTARY_DIM || p->rot_dim < 2 || p->rot_dim > p->head_dim ||
+      p->rot_dim % 2 != 0)
+    return true;
+  for (int32_t flag : {p->interleaved, p->inverse, p->pos_64})
+    if (flag != 0 && flag != 1) return true;
+  if (bad_dtype(p->dtype) || !std::isfinite(p->scale)) return true;
+  if (misaligned(p->pos, p->pos_64 ? 8 : 4) || !p->freq || misaligned(p->freq, 8)) return true;
+  // a written head may not reach into another: heads inside a token, or tokens inside a head
+  if (p->x_tok < 0 || p->x_head < 0 || p->out_tok < 0 || p->out_head < 0) return true;
+  const int64_t T = p->n_tokens, H = p->n_heads, D = p->head_dim;
+  if ((H > 1 && p->out_head < D) || (T > 1 && p->out_tok < D)) return true;
+  const unsigned __int128 heads = (unsigned __int128)(H - 1) * p->out_head + D,
+                          tokens = T > 0 ? (unsigned __int128)(T - 1) * p->out_tok + D : D;
+  return H > 1 && T > 1 && (unsigned __int128)p->out_tok < heads && (unsigned __int128)p->out_head < tokens;
+}
+
+// Rows for the matrix products: strides in elements that 16-byte pieces divide.
+bool bad_rows(int64_t stride, int64_t cols) { return stride < cols || stride % 8 != 0 || stride > (1 << 21); }
+
+bool bad_gated_ff(const argus_gated_ff_t* p) {
+  if (!p || p->n_tokens < 0 || p->n_tokens > (1 << 20)) return true;
+  if (p->width < 8 || p->width > ARGUS_MAX_FF_WIDTH || p->width % 8 != 0) return true;
+  if (p->ff < 8 || p->ff > ARGUS_MAX_FF || p->ff % 8 != 0) return true;
+  if (p->dtype != ARGUS_BF16 && p->dtype != ARGUS_F16) return true;
+  if (p->act < ARGUS_SILU || p->act > ARGUS_GELU_TANH) return true;
+  return bad_rows(p->x_stride, p->width) || bad_rows(p->wg_stride, p->width) || bad_rows(p->wu_stride, p->width);
+}
+
+bool bad_cross_entropy(const argus_cross_entropy_t* p) {
+  if (!p || p->n_tokens < 0 || p->n_tokens > (1 << 20) || p->n_vocab < 1 || p->n_vocab > ARGUS_MAX_CE_VOCAB) return true;
+  if (p->n_tokens * p->n_vocab >= ((int64_t)1 << 38)) return true;
+  if (p->width < 8 || p->width > ARGUS_MAX_CE_WIDTH || p->width % 8 != 0) return true;
+  if (p->dtype != ARGUS_BF16 || (p->ids_64 != 0 && p->ids_64 != 1)) return true;
+  if (!std::isfinite(p->scale) || !std::isfinite(p->z_loss) || p->z_loss < 0.0f) return true;
+  if (p->n_tokens > 0 && (!p->labels || misaligned(p->labels, p->ids_64 ? 8 : 4))) return true;
+  return bad_rows(p->x_stride, p->width) || bad_rows(p->w_stride, p->width);
+}
+
 }  // namespace
 }  // namespace argus
 
@@ -198,6 +238,88 @@ int argus_attention_bwd(const argus_attention_t* p, const void* d_o, const void*
   const int rc = check_device();
   if (rc != ARGUS_OK) return rc;
   return status_of(launch_attention_bwd(*p, d_o, q, k, v, o, lse, dq, dk, dv, workspace, (hipStream_t)stream));
+}
+
+int argus_rotary(const argus_rotary_t* p, const void* x, void* out, void* stream) {
+  if (bad_rotary(p)) return ARGUS_EINVAL;
+  const uintptr_t s = size_of(p->dtype);
+  if (p->n_tokens > 0 && (!x || !out)) return ARGUS_EINVAL;
+  if (misaligned(x, s) || misaligned(out, s)) return ARGUS_EINVAL;
+  if (x == out && (p->x_tok != p->out_tok || p->x_head != p->out_head)) return ARGUS_EINVAL;
+  const int rc = check_device();
+  if (rc != ARGUS_OK) return rc;
+  return status_of(launch_rotary(*p, x, out, (hipStream_t)stream));
+}
+
+size_t argus_gated_ff_workspace(const argus_gated_ff_t* p) { return bad_gated_ff(p) ? 0 : gated_ff_workspace_bytes(*p); }
+
+int argus_gated_ff(const argus_gated_ff_t* p, const void* x, const void* wg, const void* wu, void* h, void* g, void* u,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  if (bad_gated_ff(p) || !wg || !wu || (g == nullptr) != (u == nullptr)) return ARGUS_EINVAL;
+  if (p->n_tokens > 0 && (!x || !h)) return ARGUS_EINVAL;
+  const void* ptrs[6] = {x, wg, wu, h, g, u};
+  for (const void* q : ptrs)
+    if (misaligned(q, 16)) return ARGUS_EINVAL;
+  if (bad_workspace(workspace, workspace_bytes, argus_gated_ff_workspace(p))) return ARGUS_EINVAL;
+  const int rc = check_device();
+  if (rc != ARGUS_OK) return rc;
+  return status_of(launch_gated_ff(*p, x, wg, wu, h, g, u, workspace, (hipStream_t)stream));
+}
+
+size_t argus_gated_ff_bwd_workspace(const argus_gated_ff_t* p) {
+  return bad_gated_ff(p) ? 0 : gated_ff_bwd_workspace_bytes(*p);
+}
+
+int argus_gated_ff_bwd(const argus_gated_ff_t* p, const void* d_h, const void* x, const void* wg, const void* wu,
+                       const void* g, const void* u, void* dx, void* dwg, void* dwu, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  if (bad_gated_ff(p) || bad_rows(p->dh_stride, p->ff) || !wg || !wu || !dwg || !dwu) return ARGUS_EINVAL;
+  if (p->n_tokens > 0 && (!d_h || !x || !g || !u || !dx)) return ARGUS_EINVAL;
+  const void* ptrs[9] = {d_h, x, wg, wu, g, u, dx, dwg, dwu};
+  for (const void* q : ptrs)
+    if (misaligned(q, 16)) return ARGUS_EINVAL;
+  if (bad_workspace(workspace, workspace_bytes, argus_gated_ff_bwd_workspace(p))) return ARGUS_EINVAL;
+  const int rc = check_device();
+  if (rc != ARGUS_OK) return rc;
+  return status_of(launch_gated_ff_bwd(*p, d_h, x, wg, wu, g, u, dx, dwg, dwu, workspace, (hipStream_t)stream));
+}
+
+size_t argus_cross_entropy_workspace(const argus_cross_entropy_t* p) {
+  return bad_cross_entropy(p) ? 0 : cross_entropy_workspace_bytes(*p);
+}
+
+int argus_cross_entropy(const argus_cross_entropy_t* p, const void* x, const void* w,
+                        const argus_cross_entropy_out_t* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (bad_cross_entropy(p) || !w || !out || !out->mean || !out->n_valid) return ARGUS_EINVAL;
+  if (p->n_tokens > 0 && (!x || !out->loss || !out->lse)) return ARGUS_EINVAL;
+  if (misaligned(x, 16) || misaligned(w, 16)) return ARGUS_EINVAL;
+  const void* ptrs[5] = {out->loss, out->lse, out->mean, out->n_valid, out->dev_status};
+  for (const void* q : ptrs)
+    if (misaligned(q, 4)) return ARGUS_EINVAL;
+  if (bad_workspace(workspace, workspace_bytes, argus_cross_entropy_workspace(p))) return ARGUS_EINVAL;
+  const int rc = check_device();
+  if (rc != ARGUS_OK) return rc;
+  return status_of(launch_cross_entropy(*p, x, w, *out, workspace, (hipStream_t)stream));
+}
+
+size_t argus_cross_entropy_bwd_workspace(const argus_cross_entropy_t* p) {
+  return bad_cross_entropy(p) ? 0 : cross_entropy_bwd_workspace_bytes(*p);
+}
+
+int argus_cross_entropy_bwd(const argus_cross_entropy_t* p, const void* x, const void* w, const float* lse,
+                            const uint32_t* n_valid, const float* dmean, const float* dloss, void* dx, void* dw,
+                            int32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream) {
+  if (bad_cross_entropy(p) || !w || !dw || (!dmean && !dloss) || (dmean && !n_valid)) return ARGUS_EINVAL;
+  if (p->n_tokens > 0 && (!x || !lse || !dx)) return ARGUS_EINVAL;
+  for (const void* q : {x, w, (const void*)dx, (const void*)dw})
+    if (misaligned(q, 16)) return ARGUS_EINVAL;
+  for (const void* q : {(const void*)lse, (const void*)n_valid, (const void*)dmean, (const void*)dloss, (const void*)dev_status})
+    if (misaligned(q, 4)) return ARGUS_EINVAL;
+  if (bad_workspace(workspace, workspace_bytes, argus_cross_entropy_bwd_workspace(p))) return ARGUS_EINVAL;
+  const int rc = check_device();
+  if (rc != ARGUS_OK) return rc;
+  return status_of(launch_cross_entropy_bwd(*p, x, w, lse, n_valid, dmean, dloss, dx, dw, dev_status, workspace,
+                                            (hipStream_t)stream));
 }
 
 }  // extern "C"

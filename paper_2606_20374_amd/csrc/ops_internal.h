@@ -1,5 +1,5 @@
 // Shared by the step operators' kernels (embedding, layer norm, balance,
-// attention): element types, unaligned vectors, lane reductions, and the
+// attention, rotary, gated feed-forward, cross entropy): element types, unaligned vectors, lane reductions, and the
 // launch-side entry points. See include/argus_ops.h for the contract.
 #pragma once
 
@@ -139,5 +139,22 @@ size_t attention_bwd_workspace_bytes(const argus_attention_t& p);
 hipError_t launch_attention_bwd(const argus_attention_t& p, const void* d_o, const void* q, const void* k,
                                 const void* v, const void* o, const float* lse, void* dq, void* dk, void* dv,
                                 void* ws, hipStream_t st);
+
+hipError_t launch_rotary(const argus_rotary_t& p, const void* x, void* out, hipStream_t st);
+
+size_t gated_ff_workspace_bytes(const argus_gated_ff_t& p);
+hipError_t launch_gated_ff(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g,
+                           void* u, void* ws, hipStream_t st);
+size_t gated_ff_bwd_workspace_bytes(const argus_gated_ff_t& p);
+hipError_t launch_gated_ff_bwd(const argus_gated_ff_t& p, const void* dh, const void* x, const void* wg, const void* wu,
+                               const void* g, const void* u, void* dx, void* dwg, void* dwu, void* ws, hipStream_t st);
+
+size_t cross_entropy_workspace_bytes(const argus_cross_entropy_t& p);
+hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, const void* w,
+                                const argus_cross_entropy_out_t& o, void* ws, hipStream_t st);
+size_t cross_entropy_bwd_workspace_bytes(const argus_cross_entropy_t& p);
+hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* x, const void* w, const float* lse,
+                                    const uint32_t* n_valid, const float* dmean, const float* dloss, void* dx, void* dw,
+                                    int32_t* dev_status, void* ws, hipStream_t st);
 
 }  // namespace argus

@@ -51,6 +51,31 @@ class Attention(ctypes.Structure):
                 ("dev_status", V)]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [("n_tokens", I64), ("n_heads", I32), ("head_dim", I32), ("rot_dim", I32), ("interleaved", I32),
+                ("inverse", I32), ("dtype", I32), ("scale", F32), ("pos_64", I32), ("pos", V), ("freq", V),
+                ("x_tok", I64), ("x_head", I64), ("out_tok", I64), ("out_head", I64)]
+
+
+class GatedFf(ctypes.Structure):
+    _fields_ = [("n_tokens", I64), ("width", I32), ("ff", I32), ("dtype", I32), ("act", I32), ("x_stride", I64),
+                ("wg_stride", I64), ("wu_stride", I64), ("dh_stride", I64)]
+
+
+class CrossEntropy(ctypes.Structure):
+    _fields_ = [("labels", V), ("n_tokens", I64), ("ids_64", I32), ("n_vocab", I32), ("width", I32), ("dtype", I32),
+                ("scale", F32), ("z_loss", F32), ("x_stride", I64), ("w_stride", I64)]
+
+
+CROSS_ENTROPY_FIELDS = ["loss", "lse", "mean", "n_valid", "dev_status"]
+
+
+class CrossEntropyOut(ctypes.Structure):
+    _fields_ = [(f, V) for f in CROSS_ENTROPY_FIELDS]
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
 _bound = None
 
 
@@ -69,11 +94,18 @@ def _lib():
             "argus_balance_bwd": [P(Balance), V, V, V, V, V, V, V, V, V],
             "argus_attention": [P(Attention), V, V, V, V, V, V, S, V],
             "argus_attention_bwd": [P(Attention), V, V, V, V, V, V, V, V, V, V, S, V],
+            "argus_rotary": [P(Rotary), V, V, V],
+            "argus_gated_ff": [P(GatedFf), V, V, V, V, V, V, V, S, V],
+            "argus_gated_ff_bwd": [P(GatedFf), V, V, V, V, V, V, V, V, V, V, S, V],
+            "argus_cross_entropy": [P(CrossEntropy), V, V, P(CrossEntropyOut), V, S, V],
+            "argus_cross_entropy_bwd": [P(CrossEntropy), V, V, V, V, V, V, V, V, V, V, S, V],
         }.items():
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         for name, arg in {"argus_embedding_bwd_workspace": Embedding, "argus_layer_norm_bwd_workspace": LayerNorm,
                           "argus_balance_workspace": Balance, "argus_attention_workspace": Attention,
-                          "argus_attention_bwd_workspace": Attention}.items():
+                          "argus_attention_bwd_workspace": Attention, "argus_gated_ff_workspace": GatedFf,
+                          "argus_gated_ff_bwd_workspace": GatedFf, "argus_cross_entropy_workspace": CrossEntropy,
+                          "argus_cross_entropy_bwd_workspace": CrossEntropy}.items():
             getattr(L, name).argtypes, getattr(L, name).restype = [P(arg)], S
         _bound = L
     return _bound
@@ -361,4 +393,197 @@ def attention_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.T
     ws = _space(out, _lib().argus_attention_bwd_workspace(ctypes.byref(p)), q.device)
     _call("argus_attention_bwd", q.device, ctypes.byref(p), _ptr(do), qa, ka, va, _ptr(o), _ptr(lse), _ptr(out["dq"]),
           _ptr(out["dk"]), _ptr(out["dv"]), _ptr(ws), ws.numel())
+    return out
+
+
+# --------------------------------------------------------------------- rotary
+def rotary_freq(rot_dim: int, base: float = 10_000.0, factor: float = 1.0, how: str = "linear", context: int = 4096,
+                slow: float = 1.0, fast: float = 32.0, device="cuda"):
+    """Frequencies [rot_dim / 2] (float64, radians a position) for `rotary`,
+    base^(-2 i / rot_dim), and the scale that goes with them. A context made
+    longer by `factor`: "linear" divides all of them by it; "base" raises the
+    base so that the slowest is divided by it; "parts" divides those that turn
+    less than `slow` times over the original context, leaves those that turn
+    more than `fast` times, mixes between, and scales by 1 + 0.1 ln factor."""
+    if rot_dim < 2 or rot_dim % 2 or not base > 0 or not factor >= 1:
+        raise ArgusError("rotary_freq: an even rot_dim, a positive base and a factor of at least 1 expected")
+    if how not in ("linear", "base", "parts") or not fast > slow:
+        raise ArgusError("rotary_freq: linear, base or parts, with fast > slow, expected")
+    scale = 1.0
+    if how == "base" and rot_dim > 2:
+        base *= factor ** (rot_dim / (rot_dim - 2))
+    f = base ** -(torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    if how == "linear":
+        f /= factor
+    elif how == "parts":
+        keep = ((context * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / factor)
+        scale = 1.0 + 0.1 * math.log(factor)
+    return f.to(device), scale
+
+
+def _turned(t: torch.Tensor, what: str):
+    """(address, token stride, head stride) of a [tokens, heads, dim] tensor."""
+    if not (t.is_cuda and t.dim() == 3):
+        raise AssertionError("libargus takes [tokens, heads, dim] device tensors")
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise AssertionError(f"{what}: the last dimension has to be contiguous")
+    n, h, d = t.shape
+    return t.data_ptr(), t.stride(0) if n > 1 else h * d, t.stride(1) if h > 1 else d
+
+
+def _rotary(x, freq, pos, interleaved, scale, inverse, out, name):
+    n, heads, dim = x.shape
+    if freq.dtype != torch.float64 or freq.dim() != 1:
+        raise ArgusError("rotary: frequencies are float64 [rot_dim / 2]")
+    if pos is not None and pos.dtype not in (torch.int32, torch.int64):
+        raise ArgusError(f"rotary: positions of {pos.dtype}: int32 or int64 expected")
+    if pos is not None:
+        _need(pos, (n,), pos.dtype, "rotary: pos")
+    _need(out, x.shape, x.dtype, "rotary: " + name)
+    (xa, xt, xh), (oa, ot, oh) = _turned(x, "x"), _turned(out, name)
+    p = Rotary(n, heads, dim, 2 * freq.numel(), int(bool(interleaved)), int(inverse), _dtype(x), scale,
+               int(pos is not None and pos.dtype == torch.int64), _ptr(pos), _ptr(freq), xt, xh, ot, oh)
+    _call("argus_rotary", x.device, ctypes.byref(p), xa, oa)
+
+
+def rotary(x: torch.Tensor, freq: torch.Tensor, pos: Optional[torch.Tensor] = None, interleaved: bool = False,
+           scale: float = 1.0, out: Optional[dict] = None) -> dict:
+    """argus_rotary: the first 2 len(freq) elements of each head of x [tokens,
+    heads, dim] turned by the token's position (int32 or int64; none: 0, 1,
+    ..). freq and scale: of rotary_freq. out={"out": x} turns x in place."""
+    if out is None:
+        out = {"out": _empty(x.shape, x.dtype, x.device)}
+    _rotary(x, freq, pos, interleaved, scale, False, out["out"], "out")
+    return out
+
+
+def rotary_bwd(dout: torch.Tensor, freq: torch.Tensor, pos: Optional[torch.Tensor] = None, interleaved: bool = False,
+               scale: float = 1.0, out: Optional[dict] = None) -> dict:
+    """argus_rotary with inverse set: dx of rotary's x from dout."""
+    if out is None:
+        out = {"dx": _empty(dout.shape, dout.dtype, dout.device)}
+    _rotary(dout, freq, pos, interleaved, scale, True, out["dx"], "dx")
+    return out
+
+
+# ------------------------------------------------------------------- gated_ff
+def _gated_ff(x, wg, wu, act, dh_stride=0):
+    if act not in ACTIVATIONS:
+        raise ArgusError(f"gated_ff: activation {act!r}: one of {', '.join(ACTIVATIONS)} expected")
+    (xa, xs), (ga, gs), (ua, us) = _row(x), _row(wg), _row(wu)
+    _need(wg, (wg.shape[0], x.shape[1]), x.dtype, "gated_ff: wg")
+    _need(wu, wg.shape, x.dtype, "gated_ff: wu")
+    return GatedFf(x.shape[0], x.shape[1], wg.shape[0], _dtype(x), ACTIVATIONS[act], xs, gs, us, dh_stride), xa, ga, ua
+
+
+def alloc_gated_ff(n_tokens: int, ff: int, dtype, save: bool = False, device="cuda") -> dict:
+    return {f: _empty((n_tokens, ff), dtype, device) for f in (("h", "g", "u") if save else ("h",))}
+
+
+def gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "silu", save: bool = False,
+             out: Optional[dict] = None) -> dict:
+    """argus_gated_ff: h = act(x wg^T) (x wu^T) of x [tokens, width] and
+    weights [ff, width], bfloat16 or float16; with save, g and u for the
+    backward pass. act: silu, gelu or gelu_tanh."""
+    if out is None:
+        out = alloc_gated_ff(x.shape[0], wg.shape[0], x.dtype, save, x.device)
+    p, xa, ga, ua = _gated_ff(x, wg, wu, act)
+    for f in ("h", "g", "u") if save else ("h",):
+        _need(out[f], (x.shape[0], wg.shape[0]), x.dtype, "gated_ff: " + f)
+    need = _lib().argus_gated_ff_workspace(ctypes.byref(p))
+    ws = _space(out, need, x.device) if need else None
+    _call("argus_gated_ff", x.device, ctypes.byref(p), xa, ga, ua, _ptr(out["h"]), _ptr(out["g"]) if save else None,
+          _ptr(out["u"]) if save else None, _ptr(ws), ws.numel() if need else 0)
+    return out
+
+
+def alloc_gated_ff_bwd(n_tokens: int, width: int, ff: int, dtype, device="cuda") -> dict:
+    return {"dx": _empty((n_tokens, width), dtype, device), "dwg": _empty((ff, width), dtype, device),
+            "dwu": _empty((ff, width), dtype, device)}
+
+
+def gated_ff_bwd(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, g: torch.Tensor,
+                 u: torch.Tensor, act: str = "silu", out: Optional[dict] = None) -> dict:
+    """argus_gated_ff_bwd: dx, dwg and dwu from dh and the forward's x, weights,
+    g and u."""
+    n, width, ff = x.shape[0], x.shape[1], wg.shape[0]
+    if out is None:
+        out = alloc_gated_ff_bwd(n, width, ff, x.dtype, x.device)
+    da, ds = _row(dh)
+    p, xa, ga, ua = _gated_ff(x, wg, wu, act, ds)
+    for t, what in ((dh, "dh"), (g, "g"), (u, "u")):
+        _need(t, (n, ff), x.dtype, "gated_ff_bwd: " + what)
+    for f, shape in (("dx", (n, width)), ("dwg", (ff, width)), ("dwu", (ff, width))):
+        _need(out[f], shape, x.dtype, "gated_ff_bwd: " + f)
+    ws = _space(out, _lib().argus_gated_ff_bwd_workspace(ctypes.byref(p)), x.device)
+    _call("argus_gated_ff_bwd", x.device, ctypes.byref(p), da, xa, ga, ua, _ptr(g), _ptr(u), _ptr(out["dx"]),
+          _ptr(out["dwg"]), _ptr(out["dwu"]), _ptr(ws), ws.numel())
+    return out
+
+
+# -------------------------------------------------------------- cross_entropy
+def _cross_entropy(x, w, labels, scale, z_loss):
+    if labels.dtype not in (torch.int32, torch.int64):
+        raise ArgusError(f"labels of {labels.dtype}: int32 or int64 expected")
+    (xa, xs), (wa, ws) = _row(x), _row(w)
+    _need(labels, (x.shape[0],), labels.dtype, "cross_entropy: labels")
+    _need(w, (w.shape[0], x.shape[1]), x.dtype, "cross_entropy: w")
+    return CrossEntropy(_ptr(labels), x.shape[0], int(labels.dtype == torch.int64), w.shape[0], x.shape[1], _dtype(x),
+                        scale, z_loss, xs, ws), xa, wa
+
+
+def alloc_cross_entropy(n_tokens: int, device="cuda") -> dict:
+    loss, lse, mean = _empty(2 * n_tokens + 1, torch.float32, device).split([n_tokens, n_tokens, 1])
+    n_valid, status = _empty(2, torch.int32, device).split([1, 1])
+    return {"loss": loss, "lse": lse, "mean": mean, "n_valid": n_valid, "dev_status": status}
+
+
+def cross_entropy(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, scale: float = 1.0, z_loss: float = 0.0,
+                  out: Optional[dict] = None) -> dict:
+    """argus_cross_entropy: the loss of each token of x [tokens, width] over
+    the vocabulary w [ids, width], bfloat16, its lse, their mean and n_valid. A
+    label below 0 leaves a token out; one past the vocabulary too, and raises
+    DEV_TOKEN_RANGE in dev_status."""
+    n = x.shape[0]
+    if out is None:
+        out = alloc_cross_entropy(n, x.device)
+    p, xa, wa = _cross_entropy(x, w, labels, scale, z_loss)
+    for f, shape, dt in (("loss", (n,), torch.float32), ("lse", (n,), torch.float32), ("mean", (1,), torch.float32),
+                         ("n_valid", (1,), torch.int32)):
+        _need(out[f], shape, dt, "cross_entropy: " + f)
+    o = CrossEntropyOut(*[_ptr(out.get(f)) for f in CROSS_ENTROPY_FIELDS])
+    ws = _space(out, _lib().argus_cross_entropy_workspace(ctypes.byref(p)), x.device)
+    _call("argus_cross_entropy", x.device, ctypes.byref(p), xa, wa, ctypes.byref(o), _ptr(ws), ws.numel())
+    return out
+
+
+def alloc_cross_entropy_bwd(n_tokens: int, n_vocab: int, width: int, device="cuda") -> dict:
+    return {"dx": _empty((n_tokens, width), torch.bfloat16, device), "dw": _empty((n_vocab, width), torch.bfloat16, device),
+            "dev_status": _empty(1, torch.int32, device)}
+
+
+def cross_entropy_bwd(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor,
+                      n_valid: Optional[torch.Tensor] = None, dmean: Optional[torch.Tensor] = None,
+                      dloss: Optional[torch.Tensor] = None, scale: float = 1.0, z_loss: float = 0.0,
+                      out: Optional[dict] = None) -> dict:
+    """argus_cross_entropy_bwd: dx and dw from the forward's inputs and lse, and
+    the gradient dmean [1] of the mean (with n_valid, which divides it) or
+    dloss [tokens] of the losses, or both."""
+    n, width = x.shape
+    if out is None:
+        out = alloc_cross_entropy_bwd(n, w.shape[0], width, x.device)
+    p, xa, wa = _cross_entropy(x, w, labels, scale, z_loss)
+    _need(lse, (n,), torch.float32, "cross_entropy_bwd: lse")
+    if n_valid is not None:
+        _need(n_valid, (1,), torch.int32, "cross_entropy_bwd: n_valid")
+    if dmean is not None:
+        _need(dmean, (1,), torch.float32, "cross_entropy_bwd: dmean")
+    if dloss is not None:
+        _need(dloss, (n,), torch.float32, "cross_entropy_bwd: dloss")
+    _need(out["dx"], (n, width), x.dtype, "cross_entropy_bwd: dx")
+    _need(out["dw"], w.shape, x.dtype, "cross_entropy_bwd: dw")
+    ws = _space(out, _lib().argus_cross_entropy_bwd_workspace(ctypes.byref(p)), x.device)
+    _call("argus_cross_entropy_bwd", x.device, ctypes.byref(p), xa, wa, _ptr(lse), _ptr(n_valid), _ptr(dmean),
+          _ptr(dloss), _ptr(out["dx"]), _ptr(out["dw"]), _ptr(out.get("dev_status")), _ptr(ws), ws.numel())
     return out
