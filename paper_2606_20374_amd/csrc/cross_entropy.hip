@@ -148,10 +148,12 @@ __device__ __forceinline__ Operand learned(const CeArgs& a, int64_t n) {
   return {a.t.x, n, a.x.k, a.x.k};
 }
 
-__device__ __forceinline__ float other_half(float v) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, v);
-  auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return __builtin_bit_cast(float, (uint32_t)((threadIdx.x & 32) ? s[0] : s[1]));
+// Maximum over the four rows of a wavefront, lane by lane, in every row.
+__device__ __forceinline__ float rows_max(float v) {
+  auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  v = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
 }
 
 template <class TT>
@@ -165,18 +167,18 @@ __global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, fl
   const typename TT::LoadA la(learned(a, count), m0);
   const typename TT::LoadB lb(a.w, n0);
   t.run(la, lb, 0, (int)a.x.k);
-  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int lane = threadIdx.x & 63, q = lane >> 4;
 #pragma unroll
   for (int i = 0; i < TT::FM; ++i) {
-    const int at = TT::row_of(i) + (lane & 31);
+    const int at = TT::row_of(i) + (lane & 15);
     const int64_t label = m0 + at < count ? a.t.label[m0 + at] - n0 : -1;
     float top = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < TT::FN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
+      for (int e = 0; e < 4; ++e) {
         float z = t.acc[i][j][e] * a.scale;
-        if (n0 + TT::TN > a.V && n0 + TT::col_of(j) + 8 * (e / 4) + 4 * half + e % 4 >= a.V) z = -__builtin_inff();
+        if (n0 + TT::TN > a.V && n0 + TT::col_of(j) + 4 * q + e >= a.V) z = -__builtin_inff();
         t.acc[i][j][e] = z;
         top = fmaxf(top, z);
       }
@@ -184,18 +186,18 @@ __global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, fl
 #pragma unroll
       for (int j = 0; j < TT::FN; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (label == TT::col_of(j) + 8 * (e / 4) + 4 * half + e % 4) own[m0 + at] = t.acc[i][j][e];
+        for (int e = 0; e < 4; ++e)
+          if (label == TT::col_of(j) + 4 * q + e) own[m0 + at] = t.acc[i][j][e];
     }
-    top = fmaxf(top, other_half(top));
+    top = rows_max(top);
     const float from = top == -__builtin_inff() ? 0.0f : top;  // no difference of infinities
     float sum = 0;
 #pragma unroll
     for (int j = 0; j < TT::FN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((t.acc[i][j][e] - from) * kLog2e);
-    sum += other_half(sum);
-    if (half == 0) join[TT::wave() % TT::WN][at] = make_float2(top, sum);
+      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((t.acc[i][j][e] - from) * kLog2e);
+    sum = rows_sum(sum);
+    if (q == 0) join[TT::wave() % TT::WN][at] = make_float2(top, sum);
   }
   __syncthreads();
   for (int r = threadIdx.x; r < TT::TM; r += TT::THREADS) {
@@ -260,28 +262,21 @@ __global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64
   const typename TT::LoadA la(learned(a, count), m0);
   const typename TT::LoadB lb(a.w, v0 + n0);
   t.run(la, lb, 0, (int)a.x.k);
-  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int lane = threadIdx.x & 63, q = lane >> 4;
 #pragma unroll
   for (int i = 0; i < TT::FM; ++i) {
-    const int64_t row = m0 + TT::row_of(i) + (lane & 31);
-    if (row >= count) continue;
+    int64_t row = m0 + TT::row_of(i) + (lane & 15);
+    if (row >= count) row = count - 1;  // computed and not written
     const float lse = a.t.lse[row], f = a.t.coef[row] / *a.t.most, more = 1.0f + 2.0f * a.z_loss * lse;
     const int64_t label = a.t.label[row] - v0;
 #pragma unroll
-    for (int j = 0; j < TT::FN; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int64_t c = n0 + TT::col_of(j) + 2 * e + 4 * half;
-        if (c >= cols) continue;
-        Vec<bf16_t, 4> o;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          float p = __builtin_amdgcn_exp2f((t.acc[i][j][e + u] * a.scale - lse) * kLog2e) * more;
-          if (c + u == label) p -= 1.0f;
-          o.e[u] = (bf16_t)(v0 + c + u < a.V ? f * p : 0.0f);
-        }
-        *(Vec<bf16_t, 4>*)(dz + row * stride + c) = o;
-      }
+    for (int h = 0; h < 2; ++h)
+      t.write(i, h, cols - n0, [&](int j, int e) {
+        const int64_t c = n0 + TT::col_of(j) + 4 * q + e;
+        float p = __builtin_amdgcn_exp2f((t.acc[i][j][e] * a.scale - lse) * kLog2e) * more;
+        if (c == label) p -= 1.0f;
+        return v0 + c < a.V ? f * p : 0.0f;
+      }, [&](int r) { return m0 + r < count ? dz + (m0 + r) * stride + n0 : nullptr; });
   }
 }
 

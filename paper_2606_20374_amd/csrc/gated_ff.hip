@@ -39,16 +39,6 @@ struct FfArgs {
 };
 
 template <class TT>
-struct LoadBoth {
-  using Half = LoadRows<TT::TN / 2, TT::THREADS>;
-  Half g, u;
-  __device__ __forceinline__ void load(int k0, typename TT::T* tile, bool whole) const {
-    g.load(k0, tile, whole);
-    u.load(k0, tile + TT::TN / 2 * kStep, whole);
-  }
-};
-
-template <class TT>
 __global__ __launch_bounds__(TT::THREADS) void ff_fwd(FfArgs a) {
   using T = typename TT::T;
   int m, n;
@@ -56,32 +46,18 @@ __global__ __launch_bounds__(TT::THREADS) void ff_fwd(FfArgs a) {
   const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * (TT::TN / 2), F = a.wg.rows;
   TT t;
   const typename TT::LoadA la(a.x, m0);
-  t.run(la, LoadBoth<TT>{{a.wg, n0}, {a.wu, n0}}, 0, (int)a.x.k);
-  const int lane = threadIdx.x & 63;
+  const typename TT::LoadB lb(a.wg, n0, a.wu, n0);
+  t.run(la, lb, 0, (int)a.x.k);
 #pragma unroll
   for (int i = 0; i < TT::FM; ++i) {
-    const int64_t row = m0 + TT::row_of(i) + (lane & 31);
-    if (row >= a.x.rows) continue;
-#pragma unroll
-    for (int j = 0; j < TT::FN / 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int64_t c = n0 + TT::col_of(j) + 2 * e + 4 * (lane >> 5);
-        if (c >= F) continue;  // F is a multiple of 8
-        Vec<T, 4> h, g, u;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const float gv = t.acc[i][j][e + v], uv = t.acc[i][j + TT::FN / 2][e + v];
-          h.e[v] = (T)(activation(gv, a.act).x * uv);
-          g.e[v] = (T)gv;
-          u.e[v] = (T)uv;
-        }
-        *(Vec<T, 4>*)((T*)a.h + row * F + c) = h;
-        if (a.g) {
-          *(Vec<T, 4>*)((T*)a.g + row * F + c) = g;
-          *(Vec<T, 4>*)((T*)a.u + row * F + c) = u;
-        }
-      }
+    auto to = [&](void* p) {
+      return [=](int r) { return m0 + r < a.x.rows ? (T*)p + (m0 + r) * F + n0 : nullptr; };
+    };
+    t.write(i, 0, F - n0, [&](int j, int e) { return activation(t.acc[i][j][e], a.act).x * t.acc[i][j + TT::HN][e]; }, to(a.h));
+    if (a.g) {
+      t.write(i, 0, F - n0, [&](int j, int e) { return t.acc[i][j][e]; }, to(a.g));
+      t.write(i, 0, F - n0, [&](int j, int e) { return t.acc[i][j + TT::HN][e]; }, to(a.u));
+    }
   }
 }
 

@@ -5,14 +5,19 @@
 //
 // Either operand is stored with k innermost ("rows": x, weights in a forward
 // product) or with k as the outer dimension ("columns": weights and inputs in
-// gradients). A workgroup owns TM x TN of C and takes k in steps of 32 through
-// kBuffers pairs of LDS tiles, loaded straight from memory.
+// gradients). A workgroup owns TM x TN of C and takes k in steps of 64 through
+// two pairs of LDS tiles, loaded straight from memory.
 //
-// All products are v_mfma_f32_32x32x16 with B's rows as the instruction's
-// first operand, so that a lane holds one m (its column) and groups of four
-// consecutive n: with c = lane % 32 and h = lane / 32, register i of a block
-// is n = 8 (i / 4) + 4 h + i % 4, m = c, and of both operands a lane holds
-// k = 8 h + j, j = 0 .. 7.
+// All products are v_mfma_f32_16x16x32 with B's rows as the instruction's
+// first operand, so that a lane holds one m (its column) and four consecutive
+// n: with c = lane % 16 and q = lane / 16, register e of a block is n = 4 q + e,
+// m = c, and of both operands a lane holds k = 8 q + j, j = 0 .. 7.
+//
+// Bound by power: products of 8,192^3 run at 1,460 TFLOP/s (both operands with k
+// innermost), 1,426 and 1,377 (one, none), at 1.6 to 1.9 GHz with the matrix units
+// busy 78%, 71% and 66% of the cycles. The 32x32x16 instruction, which moves
+// twice as much through the accumulators, took 6 to 8% longer in the same loop;
+// steps of 32 k, which ask for half lines, 13% (k innermost) and 4%.
 #pragma once
 
 #include <type_traits>
@@ -22,19 +27,19 @@
 namespace argus {
 namespace product {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kStep = 32;  // k of a tile
+constexpr int kStep = 64;  // k of a tile
 
-__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c, bf16_t) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+__device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, bf16_t) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c, f16_t) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+__device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16_t) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 // Past every buffer's end: reads as zeros.
@@ -59,115 +64,129 @@ struct Operand {
   int64_t rows, k, stride;
 };
 
-// Loads of tiles of ROWS rows by 32 k with k innermost: 64 bytes a row, four
-// pieces of 16 bytes. Piece c of row r lies at place c ^ (r >> 2 & 3), so that
+// Loads of both halves of tiles of 2 ROWS rows by 64 k with k innermost: 128
+// bytes a row (requests of 64 bytes leave half of each L2 line unused), eight
+// pieces of 16 bytes. Piece c of row r lies at place c ^ (r >> 1 & 7), so that
 // the 16 rows of one cycle's read take all 64 banks; a wavefront's lanes write
 // consecutive places, so the exchange is made on the global side.
 template <int ROWS, int THREADS>
 struct LoadRows {
-  static constexpr int N = ROWS * 4 / THREADS;
-  static_assert(N >= 1 && ROWS * 4 % THREADS == 0);
-  __amdgpu_buffer_rsrc_t r;
-  int off[N], at, k;
-  __device__ __forceinline__ LoadRows(const Operand& o, int64_t row0) {
-    const int row = threadIdx.x >> 2, c = (threadIdx.x & 3) ^ ((threadIdx.x >> 4) & 3);
-    r = buffer((const char*)o.p + row0 * o.stride * 2, ((o.rows - row0 - 1) * o.stride + o.k) * 2);
-    at = c * 8;
-    k = (int)o.k;
+  static constexpr int N = ROWS * 8 / THREADS;
+  static_assert(N >= 1 && ROWS * 8 % THREADS == 0 && THREADS % 128 == 0);
+  __amdgpu_buffer_rsrc_t r[2];
+  int off[2][N], at;  // the same in both halves where they are of one operand
+  __device__ __forceinline__ LoadRows(const Operand& o, int64_t row0) : LoadRows(o, row0, o, row0 + ROWS) {}
+  // halves of their own
+  __device__ __forceinline__ LoadRows(const Operand& o, int64_t row0, const Operand& p, int64_t row1) {
+    const int row = threadIdx.x >> 3;
+    at = ((threadIdx.x & 7) ^ ((threadIdx.x >> 4) & 7)) * 8;
+    r[0] = buffer((const char*)o.p + row0 * o.stride * 2, ((o.rows - row0 - 1) * o.stride + o.k) * 2);
+    r[1] = buffer((const char*)p.p + row1 * p.stride * 2, ((p.rows - row1 - 1) * p.stride + p.k) * 2);
 #pragma unroll
-    for (int i = 0; i < N; ++i) off[i] = (int)(((row + i * (THREADS / 4)) * o.stride + c * 8) * 2);
+    for (int i = 0; i < N; ++i) {
+      off[0][i] = (int)(((row + i * (THREADS / 8)) * o.stride + at) * 2);
+      off[1][i] = (int)(((row + i * (THREADS / 8)) * p.stride + at) * 2);
+    }
   }
-  // Tile of k = k0 .. k0 + 31. With whole set, all of them exist.
+  // Half of the tile of k = k0 .. k0 + 63, zeros from k_end on.
   template <class T>
-  __device__ __forceinline__ void load(int k0, T* tile, bool whole) const {
+  __device__ __forceinline__ void load(int half, int k0, int k_end, T* tile) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      load_lds(r, tile + (i * THREADS + wave * 64) * 8, whole || k0 + at < k ? off[i] : kNowhere, k0 * 2);
+      load_lds(r[half], tile + (i * THREADS + wave * 64) * 8, k0 + at < k_end ? off[half][i] : kNowhere, k0 * 2);
   }
 };
 
-// Loads of tiles of 32 k by COLS columns with k as the outer dimension. Piece
-// c of row k lies at place c ^ 4 (k & 3): a transposed read takes, of 32 lanes
-// at a time, four neighbouring pieces of four rows, which are all 64 banks.
+// Place of piece c of row k of a half tile with k as the outer dimension, as an
+// exchange c ^ swap: a transposed read takes, of 32 lanes at a time, two
+// neighbouring pieces of rows k .. k + 3 and k + 8 .. k + 11, which are then all
+// 64 banks. Rows of eight pieces lie two to the banks' width.
+template <int PIECES>
+__device__ __forceinline__ constexpr int swap_cols(int k) {
+  static_assert(PIECES == 8 || PIECES == 16);
+  return PIECES == 16 ? ((k & 3) << 2) ^ ((k >> 2) & 2) : ((k & 2) << 1) ^ ((k >> 2) & 2);
+}
+
+// The same with k as the outer dimension: 64 k by COLS columns.
 template <int COLS, int THREADS>
 struct LoadCols {
   static constexpr int PIECES = COLS / 8, N = kStep * PIECES / THREADS;
   static_assert(N >= 1 && kStep * PIECES % THREADS == 0);
   const char* p;
   int64_t k, stride;
-  int off[N], cols;
+  int off[2][N], cols;
   __device__ __forceinline__ LoadCols(const Operand& o, int64_t col0) {
     p = (const char*)o.p + col0 * 2;
     k = o.k;
     stride = o.stride;
-    cols = (int)(o.rows - col0 < COLS ? o.rows - col0 : COLS);
+    cols = (int)(o.rows - col0 < 2 * COLS ? o.rows - col0 : 2 * COLS);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = i * THREADS + threadIdx.x, row = at / PIECES, c = (at % PIECES) ^ ((row & 3) << 2);
-      off[i] = c * 8 < cols ? (int)((row * stride + c * 8) * 2) : kNowhere;
-    }
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int at = i * THREADS + threadIdx.x, row = at / PIECES;
+        const int c = h * COLS + ((at % PIECES) ^ swap_cols<PIECES>(row)) * 8;
+        off[h][i] = c < cols ? (int)((row * stride + c) * 2) : kNowhere;
+      }
   }
   template <class T>
-  __device__ __forceinline__ void load(int k0, T* tile, bool) const {
+  __device__ __forceinline__ void load(int half, int k0, int k_end, T* tile) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const auto r = buffer(p + k0 * stride * 2, ((k - k0 - 1) * stride + cols) * 2);
+    const int64_t left = k < k_end ? k - k0 : (int64_t)k_end - k0;
+    const auto r = buffer(p + k0 * stride * 2, left > 0 ? ((left - 1) * stride + cols) * 2 : 0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) load_lds(r, tile + (i * THREADS + wave * 64) * 8, off[i], 0);
+    for (int i = 0; i < N; ++i) load_lds(r, tile + (i * THREADS + wave * 64) * 8, off[half][i], 0);
   }
 };
 
-// Reads of blocks of 32 rows (or columns) by 16 k as operands. BLOCKS of them,
-// at rows first(0), first(1), .. of the tile.
+// Reads of blocks of 16 rows (or columns) by 32 k as operands, from row
+// `first` of a half tile on.
 template <bool ROWS, int WIDTH, int BLOCKS>
 struct Read;
 template <int WIDTH, int BLOCKS>
 struct Read<true, WIDTH, BLOCKS> {
   uint32_t at[2];
-  uint32_t row[BLOCKS];
-  template <class F>
-  __device__ __forceinline__ explicit Read(F first) {
+  __device__ __forceinline__ explicit Read(int first) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-      at[ks] = (first(0) + (lane & 31)) * 64 + ((2 * ks + (lane >> 5)) ^ ((lane >> 2) & 3)) * 16;
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) row[b] = (first(b) - first(0)) * 64;  // constants
+    for (int s = 0; s < 2; ++s) at[s] = (first + (lane & 15)) * 128 + ((4 * s + (lane >> 4)) ^ ((lane >> 1) & 7)) * 16;
   }
   template <class T>
-  __device__ __forceinline__ s16x8 get(const T* tile, int b, int ks) const {
+  __device__ __forceinline__ s16x8 get(const T* tile, int b, int s) const {
     typedef __attribute__((address_space(3))) const char* lds_ptr;
     const lds_ptr p = (lds_ptr)(__attribute__((address_space(3))) const void*)tile;
-    return *(__attribute__((address_space(3))) const s16x8*)(p + at[ks] + row[b]);
+    return *(__attribute__((address_space(3))) const s16x8*)(p + at[s] + b * 16 * 128);
   }
 };
 template <int WIDTH, int BLOCKS>
 struct Read<false, WIDTH, BLOCKS> {
   uint32_t at[BLOCKS];
-  template <class F>
-  __device__ __forceinline__ explicit Read(F first) {
-    const int lane = threadIdx.x & 63, i = lane & 15;
+  __device__ __forceinline__ explicit Read(int first) {
+    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b)
-      at[b] = ((lane >> 5) * 8 + (i >> 2)) * WIDTH * 2 + (((first(b) / 32) ^ (i >> 2)) * 4 + (lane & 16) / 8) * 16 + (i & 3) * 8;
+      at[b] = (8 * q + (i >> 2)) * WIDTH * 2 +
+              (((first + 16 * b) / 8 + (i & 3) / 2) ^ swap_cols<WIDTH / 8>(8 * q + (i >> 2))) * 16 + (i & 1) * 8;
   }
   // Sixteen lanes read four rows of sixteen columns and each gets one column.
   template <class T>
-  __device__ __forceinline__ s16x8 get(const T* tile, int b, int ks) const {
+  __device__ __forceinline__ s16x8 get(const T* tile, int b, int s) const {
     typedef __attribute__((address_space(3))) const char* lds_ptr;
     typedef __attribute__((address_space(3))) s16x4* tr_ptr;
     const lds_ptr p = (lds_ptr)(__attribute__((address_space(3))) const void*)tile;
-    const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + at[b] + (16 * ks) * WIDTH * 2));
-    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + at[b] + (16 * ks + 4) * WIDTH * 2));
+    const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + at[b] + (32 * s) * WIDTH * 2));
+    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + at[b] + (32 * s + 4) * WIDTH * 2));
     return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
 
-// Loads issued by this wavefront that may still be under way: at most n.
+// At most n of the loads that this wavefront issued are still under way, and
+// none of its reads from LDS.
 template <int n>
 __device__ __forceinline__ void wait_loads() {
   static_assert(n < 64);
-  __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | ((n >> 4) << 14));
+  __builtin_amdgcn_s_waitcnt(0x0070 | (n & 15) | ((n >> 4) << 14));
 }
 // All wavefronts are here; nothing is waited for.
 __device__ __forceinline__ void meet() {
@@ -176,110 +195,160 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
-// The tile of a workgroup. Wavefronts lie WM by WN over it; in n each takes a
-// share of both halves of the tile, the same columns of each: a feed-forward
-// tile holds gate columns in the one and up columns in the other.
+// The tile of a workgroup, in two halves of its rows and two of its columns.
+// Wavefronts lie WM by WN over it, each with the same share of both halves, so
+// that it takes the tile's quarters one after the other; a feed-forward tile
+// holds gate columns in one half and up columns in the other.
 template <class T_, int TM_, int TN_, int WM_, int WN_, bool ROWS_A, bool ROWS_B>
 struct Tile {
   using T = T_;
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, THREADS = 64 * WM * WN;
-  static constexpr int FM = TM / WM / 32, FN = TN / WN / 32;
-  static_assert(FM >= 1 && FN >= 2 && FN % 2 == 0);
-  using LoadA = std::conditional_t<ROWS_A, LoadRows<TM, THREADS>, LoadCols<TM, THREADS>>;
-  using LoadB = std::conditional_t<ROWS_B, LoadRows<TN, THREADS>, LoadCols<TN, THREADS>>;
-  static constexpr int kLoads = LoadA::N + LoadB::N;
+  static constexpr int FM = TM / WM / 16, FN = TN / WN / 16, HM = FM / 2, HN = FN / 2;
+  static_assert(HM >= 1 && HN >= 1 && FM % 2 == 0 && FN % 2 == 0);
+  using LoadA = std::conditional_t<ROWS_A, LoadRows<TM / 2, THREADS>, LoadCols<TM / 2, THREADS>>;
+  using LoadB = std::conditional_t<ROWS_B, LoadRows<TN / 2, THREADS>, LoadCols<TN / 2, THREADS>>;
+  static constexpr int kLoads = LoadA::N + LoadB::N;  // of one half of each
 
-  f32x16 acc[FM][FN];
+  f32x4 acc[FM][FN];
+  T* stage;  // LDS that run leaves free
 
   static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-  static __device__ __forceinline__ int row_of(int b) { return wave() / WN * (FM * 32) + 32 * b; }
-  static __device__ __forceinline__ int col_of(int b) {
-    return b / (FN / 2) * (TN / 2) + wave() % WN * (FN / 2 * 32) + b % (FN / 2) * 32;
+  static __device__ __forceinline__ int row_of(int b) { return b / HM * (TM / 2) + wave() / WN * (HM * 16) + b % HM * 16; }
+  static __device__ __forceinline__ int col_of(int b) { return b / HN * (TN / 2) + wave() % WN * (HN * 16) + b % HN * 16; }
+
+  // A half tile. Each is an array of its own: reads of one do not wait for loads
+  // into another.
+  template <int WHICH, int SIZE>
+  static __device__ __forceinline__ T* lds() {
+    __shared__ __align__(16) T half[SIZE / 2 * kStep];
+    return half;
   }
 
-  // Order of a half step's instructions: its reads from LDS (of the next half
-  // step's operands) and its loads one by one between the products.
-  template <int LOADS>
+  // Order of a quarter's instructions: its reads from LDS and its loads one by
+  // one between the products.
+  template <int LOADS, int READS>
   static __device__ __forceinline__ void interleave() {
-    constexpr int kReads = FM * (ROWS_A ? 1 : 2) + FN * (ROWS_B ? 1 : 2), kProducts = FM * FN;
-    constexpr int kEach = (kReads + LOADS + kProducts - 1) / kProducts;  // to a product
+    constexpr int kProducts = 2 * HM * HN, kAll = READS + LOADS;
 #pragma unroll
     for (int i = 0; i < kProducts; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int n = i * kEach + j;
-        if (n < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        else if (n < kReads + LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      for (int j = i * kAll / kProducts; j < (i + 1) * kAll / kProducts; ++j) {
+        if (j < READS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        else __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  // Adds the products of k = k_begin .. k_end - 1 (k_begin a multiple of 32).
-  // load_b(k0, tile, whole) loads a tile of B. Four tiles deep: at the barrier
-  // of a step the tiles of this one and the next have arrived, those of the
-  // one after are under way, and the step before has left its buffers, which
-  // the loads of the third go to.
-  template <class LB>
-  __device__ __forceinline__ void run(const LoadA& la, const LB& lb, int k_begin, int k_end) {
-    __shared__ __align__(16) T a0[TM * kStep], a1[TM * kStep], a2[TM * kStep], a3[TM * kStep];
-    __shared__ __align__(16) T b0[TN * kStep], b1[TN * kStep], b2[TN * kStep], b3[TN * kStep];
-    const Read<ROWS_A, TM, FM> ra([](int b) { return row_of(b); });
-    const Read<ROWS_B, TN, FN> rb([](int b) { return col_of(b); });
+  // Rounds the values v(j, e) of row block i and of the columns of half h to T
+  // and writes them by way of LDS: 64 bytes of a row together, where a lane of
+  // the result holds 8. row(r) is the tile's row r in memory, or null; columns
+  // from `cols` on (a multiple of 8) are left out.
+  template <class V, class R>
+  __device__ __forceinline__ void write(int i, int h, int64_t cols, V v, R row) {
+    constexpr int W = HN * 16 + 8;  // 16 bytes more: rows in other banks
+    static_assert(HN == 2 && 16 * W * WM * WN <= TM / 2 * kStep);
+    const int lane = threadIdx.x & 63;
+    T* s = stage + wave() * 16 * W;
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int j = 0; j < HN; ++j) {
+      Vec<T, 4> o;
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    if (k_begin >= k_end) return;
-    const int last = k_begin + ((k_end - k_begin - 1) / kStep) * kStep;  // k of the last tile
-    auto load = [&](int k0, T* A, T* B) __attribute__((always_inline)) {
-      // past the last tile the same one again, into a buffer that is read no
-      // more: the count of loads under way stays the same
-      const int k = k0 < last ? k0 : last;
-      la.load(k, A, k + kStep <= k_end);
-      lb.load(k, B, k + kStep <= k_end);
-    };
-    s16x8 fa[2][FM], fb[2][FN];
-    auto read = [&](int to, const T* A, const T* B, int ks) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < FM; ++i) fa[to][i] = ra.get(A, i, ks);
-#pragma unroll
-      for (int j = 0; j < FN; ++j) fb[to][j] = rb.get(B, j, ks);
-    };
-    auto multiply = [&](int of) __attribute__((always_inline)) {
+      for (int e = 0; e < 4; ++e) o.e[e] = (T)v(h * HN + j, e);
+      *(uint2*)(s + (lane & 15) * W + j * 16 + 4 * (lane >> 4)) = __builtin_bit_cast(uint2, o);
+    }
+    asm volatile("" ::: "memory");  // one wavefront: LDS takes its instructions in order
+    const int c = (lane & 3) * 8;
+    const uint4 x = *(const uint4*)(s + (lane >> 2) * W + c);
+    asm volatile("" ::: "memory");
+    T* to = row(row_of(i) + (lane >> 2));
+    if (to && col_of(h * HN) + c < cols) *(uint4*)(to + col_of(h * HN) + c) = x;
+  }
+
+  // Adds the products of k = k_begin .. k_end - 1 (k_begin a multiple of kStep).
+  //
+  // Two tiles deep, by halves. A step of 64 k takes the quarters (A0, B0), (A0,
+  // B1), (A1, B1), (A1, B0), and during each reads the half that the next one
+  // but one (A0, B0: of the next step) needs. At its first barrier the step's
+  // A0 and B0 have been read by all, and their places get those of the step
+  // after the next; at the second, before (A1, B1), A1 and B1. So each load has
+  // one and a half steps, and two barriers a step are enough.
+  template <bool MORE = false>  // to what is there
+  __device__ __forceinline__ void run(const LoadA& la, const LoadB& lb, int k_begin, int k_end) {
+    T *a00 = lds<0, TM>(), *a01 = lds<1, TM>(), *a10 = lds<2, TM>(), *a11 = lds<3, TM>();
+    T *b00 = lds<4, TN>(), *b01 = lds<5, TN>(), *b10 = lds<6, TN>(), *b11 = lds<7, TN>();
+    const Read<ROWS_A, TM / 2, HM> ra(wave() / WN * (HM * 16));
+    const Read<ROWS_B, TN / 2, HN> rb(wave() % WN * (HN * 16));
+    if constexpr (!MORE)
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mfma(fb[of][j], fa[of][i], acc[i][j], T{});
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    stage = a00;
+    if (k_begin >= k_end) return;
+    constexpr int RA = 2 * HM * (ROWS_A ? 1 : 2), RB = 2 * HN * (ROWS_B ? 1 : 2);
+    s16x8 fa[2][2][HM], fb[2][2][HN];
+    auto read_a = [&](int to, const T* A) __attribute__((always_inline)) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < HM; ++i) fa[to][s][i] = ra.get(A, i, s);
+    };
+    auto read_b = [&](int to, const T* B) __attribute__((always_inline)) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < HN; ++j) fb[to][s][j] = rb.get(B, j, s);
+    };
+    // quarter (i, j), the operands of B in fb[of]
+    auto multiply = [&](int hi, int hj, int of) __attribute__((always_inline)) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < HM; ++i)
+#pragma unroll
+          for (int j = 0; j < HN; ++j)
+            acc[hi * HM + i][hj * HN + j] = mfma(fb[of][s][j], fa[hi][s][i], acc[hi * HM + i][hj * HN + j], T{});
+    };
+    auto load = [&](int half, int k0, T* A, T* B) __attribute__((always_inline)) {
+      la.load(half, k0, k_end, A);
+      lb.load(half, k0, k_end, B);
     };
     int k = k_begin;
-    load(k, a0, b0);
-    load(k + kStep, a1, b1);
-    load(k + 2 * kStep, a2, b2);
-    wait_loads<2 * kLoads>();
+    load(0, k, a00, b00);
+    load(1, k, a01, b01);
+    load(0, k + kStep, a10, b10);
+    load(1, k + kStep, a11, b11);
+    wait_loads<3 * kLoads>();
     meet();
-    read(0, a0, b0, 0);
-    auto step = [&](T* A, T* B, T* nextA, T* nextB, T* freeA, T* freeB) __attribute__((always_inline)) {
-      wait_loads<kLoads>();
+    read_a(0, a00);
+    read_b(0, b00);
+    auto step = [&](int x, T* A0, T* A1, T* B0, T* B1, const T* nextA, const T* nextB) __attribute__((always_inline)) {
+      wait_loads<2 * kLoads>();
       meet();
-      load(k + 3 * kStep, freeA, freeB);
-      read(1, A, B, 1);
-      multiply(0);
-      interleave<kLoads>();
-      read(0, nextA, nextB, 0);
-      multiply(1);
-      interleave<0>();
+      load(0, k + 2 * kStep, A0, B0);
+      read_b(x ^ 1, B1);
+      multiply(0, 0, x);
+      interleave<kLoads, RB>();
+      read_a(1, A1);
+      multiply(0, 1, x ^ 1);
+      interleave<0, RA>();
+      wait_loads<2 * kLoads>();
+      meet();
+      load(1, k + 2 * kStep, A1, B1);
+      read_a(0, nextA);
+      multiply(1, 1, x ^ 1);
+      interleave<kLoads, RA>();
+      read_b(x ^ 1, nextB);
+      multiply(1, 0, x);
+      interleave<0, RB>();
       k += kStep;
-      return k <= last;
+      return k < k_end;
     };
     while (true) {
-      if (!step(a0, b0, a1, b1, a3, b3)) break;
-      if (!step(a1, b1, a2, b2, a0, b0)) break;
-      if (!step(a2, b2, a3, b3, a1, b1)) break;
-      if (!step(a3, b3, a0, b0, a2, b2)) break;
+      if (!step(0, a00, a01, b00, b01, a10, b10)) break;
+      if (!step(1, a10, a11, b10, b11, a00, b00)) break;
     }
     wait_loads<0>();  // none may write into LDS that another use has taken
     meet();
@@ -358,43 +427,50 @@ __global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
   my_part(g.a.k, blockIdx.y, g.S, begin, end);
   TT t;
   const typename TT::LoadA la(g.a, m0);
-  const typename TT::LoadB lb(g.b, n0), lb1(TWO ? g.b1 : g.b, n0);
-  auto load_b = [&](int k0, T* tile, bool whole) __attribute__((always_inline)) {
-    if (TWO && k0 >= g.k1) lb1.load(k0 - (int)g.k1, tile, whole);
-    else lb.load(k0, tile, whole);
-  };
-  struct B {
-    decltype(load_b)& f;
-    __device__ __forceinline__ void load(int k0, T* tile, bool whole) const { f(k0, tile, whole); }
-  };
-  t.run(la, B{load_b}, begin, end);
+  const typename TT::LoadB lb(g.b, n0);
+  if constexpr (TWO) {
+    // one loop after the other: a choice between them at each load breaks the
+    // order of the loop's instructions (gradients of 16,384 tokens, 4,096 wide
+    // with 12,288 inside: 8,492 us in place of 5,406)
+    const int k1 = (int)g.k1;
+    t.run(la, lb, begin, end < k1 ? end : k1);
+    g.b1.p = (const char*)g.b1.p - g.k1 * g.b1.stride * 2;  // its k count from k1 on
+    g.b1.k += g.k1;
+    t.template run<true>(la, typename TT::LoadB(g.b1, n0), begin > k1 ? begin : k1, end);
+  } else {
+    t.run(la, lb, begin, end);
+  }
   const int lane = threadIdx.x & 63;
   const int64_t cols = g.b.rows;
-  const float f = factor_of(g);
+  if (!g.sums) {
+    const float f = factor_of(g);
+#pragma unroll
+    for (int i = 0; i < TT::FM; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        t.write(i, h, cols - n0, [&](int j, int e) { return t.acc[i][j][e] * f; },
+                [&](int r) {
+                  T* row = m0 + r < g.a.rows ? row_at<T>(g.rows, m0 + r, cols) : nullptr;
+                  return row ? row + n0 : nullptr;
+                });
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < TT::FM; ++i) {
-    const int64_t row = m0 + TT::row_of(i) + (lane & 31);
-    T* out = row < g.a.rows ? row_at<T>(g.rows, row, cols) : nullptr;
-    float* sum = row < g.a.rows && row < kept ? g.sums + ((int64_t)blockIdx.y * kept + row) * cols : nullptr;
+    const int64_t row = m0 + TT::row_of(i) + (lane & 15);
+    if (row >= g.a.rows || row >= kept) continue;
+    float* sum = g.sums + ((int64_t)blockIdx.y * kept + row) * cols;
 #pragma unroll
-    for (int j = 0; j < TT::FN; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int64_t c = n0 + TT::col_of(j) + 2 * e + 4 * (lane >> 5);
-        if (c >= cols) continue;  // cols is a multiple of 8
-        float4 v = make_float4(t.acc[i][j][e], t.acc[i][j][e + 1], t.acc[i][j][e + 2], t.acc[i][j][e + 3]);
-        if (g.sums) {
-          if (!sum) continue;
-          if (g.add) {
-            const float4 o = *(const float4*)(sum + c);
-            v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
-          }
-          *(float4*)(sum + c) = v;
-        } else if (out) {
-          Vec<T, 4> o{{(T)(v.x * f), (T)(v.y * f), (T)(v.z * f), (T)(v.w * f)}};
-          *(Vec<T, 4>*)(out + c) = o;
-        }
+    for (int j = 0; j < TT::FN; ++j) {
+      const int64_t c = n0 + TT::col_of(j) + 4 * (lane >> 4);
+      if (c >= cols) continue;  // cols is a multiple of 8
+      float4 v = make_float4(t.acc[i][j][0], t.acc[i][j][1], t.acc[i][j][2], t.acc[i][j][3]);
+      if (g.add) {
+        const float4 o = *(const float4*)(sum + c);
+        v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
       }
+      *(float4*)(sum + c) = v;
+    }
   }
 }
 

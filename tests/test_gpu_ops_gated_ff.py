@@ -127,6 +127,17 @@ def test_backward(T, W, F, dtype):
     _check_backward(got, dh, x, wg, wu, f["g"], f["u"], act)
 
 
+@pytest.mark.parametrize("T", [7, 200, 3_130])
+def test_every_tensor_has_its_own_stride(T):
+    W, F = 72, 2_056
+    x, wg, wu, dh = _data(T, W, F, torch.bfloat16)
+    own = lambda t, pad: torch.nn.functional.pad(t, (0, pad), value=math.nan)[:, :t.shape[1]]  # noqa: E731
+    x, wg, wu, dh = own(x, 8), own(wg, 40), own(wu, 16), own(dh, 24)
+    f = pa.gated_ff(x, wg, wu, save=True)
+    _check_forward(f, x, wg, wu, "silu")
+    _check_backward(pa.gated_ff_bwd(dh, x, wg, wu, f["g"], f["u"]), dh, x, wg, wu, f["g"], f["u"], "silu")
+
+
 def test_many_tokens_of_a_narrow_block():
     # the weights' gradients sum over a long axis by parts
     x, wg, wu, dh = _data(40_011, 40, 72, torch.bfloat16)
