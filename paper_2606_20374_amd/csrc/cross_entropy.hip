@@ -24,13 +24,13 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // The learned tokens, in order.
 struct Tokens {
-  uint32_t* n;      // [1] how many
-  float* most;      // [1] largest |coef| that is finite, 1 if that is 0; backward
-  int32_t* index;   // [n] token
-  int32_t* label;   // [n]
-  int32_t* place;   // [T] number of a token, -1: not learned
-  float *coef, *lse;  // [n], backward
-  bf16_t* x;        // [n][W], where n < T
+  uint32_t* n;     // [1] how many
+  float* most;     // [1] largest |c| that is finite, 1 if that is 0; backward
+  int32_t* index;  // [n] token
+  int32_t* label;  // [n] forward
+  int32_t* place;  // [T] number of a token, -1: not learned; backward
+  float4* row;     // [n] backward: -lse in units of log2, c, c (1 + 2 z_loss lse), label
+  bf16_t* x;       // [n][W], where n < T
 };
 
 struct CeArgs {
@@ -100,11 +100,11 @@ __global__ __launch_bounds__(kIndexThreads) void ce_index(CeArgs a, IndexArgs o)
       if (t >= a.T) break;
       if (id[j] >= 0) {
         a.t.index[at] = (int32_t)t;
-        a.t.label[at] = (int32_t)id[j];
-        if (o.lse) {
-          a.t.lse[at] = o.lse[t];
-          const float c = mean + (o.dloss ? o.dloss[t] : 0.0f);
-          a.t.coef[at] = c;
+        if (!a.t.row) {
+          a.t.label[at] = (int32_t)id[j];
+        } else {
+          const float lse = o.lse[t], c = mean + (o.dloss ? o.dloss[t] : 0.0f);
+          a.t.row[at] = make_float4(-lse * kLog2e, c, c * (1.0f + 2.0f * a.z_loss * lse), __int_as_float((int32_t)id[j]));
           if (fabsf(c) < __builtin_inff()) top = fmaxf(top, fabsf(c));
         }
         ++at;
@@ -159,10 +159,12 @@ __device__ __forceinline__ float rows_max(float v) {
 template <class TT>
 __global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, float* own, int mt, int nt) {
   __shared__ float2 join[TT::WN][TT::TM];
+  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n);
+  mt = (int)((count + TT::TM - 1) / TT::TM);
+  if (blockIdx.x >= (unsigned)mt * nt) return;
   int m, n;
-  my_tile(mt, nt, m, n);
-  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n), m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
-  if (m0 >= count) return;
+  tile_at(blockIdx.x, mt, nt, m, n);
+  const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
   TT t;
   const typename TT::LoadA la(learned(a, count), m0);
   const typename TT::LoadB lb(a.w, n0);
@@ -254,50 +256,66 @@ __global__ __launch_bounds__(1024) void ce_mean(const float* loss, int64_t T, co
 template <class TT>
 __global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64_t v0, int64_t cols, int64_t stride,
                                                      int mt, int nt) {
+  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n);
+  mt = (int)((count + TT::TM - 1) / TT::TM);
+  if (blockIdx.x >= (unsigned)mt * nt) return;
   int m, n;
-  my_tile(mt, nt, m, n);
-  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n), m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
-  if (m0 >= count) return;
+  tile_at(blockIdx.x, mt, nt, m, n);
+  const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
   TT t;
   const typename TT::LoadA la(learned(a, count), m0);
   const typename TT::LoadB lb(a.w, v0 + n0);
   t.run(la, lb, 0, (int)a.x.k);
   const int lane = threadIdx.x & 63, q = lane >> 4;
+  const float sc = a.scale * kLog2e, inv = 1.0f / *a.t.most;
+  float4 rows[TT::FM];
 #pragma unroll
   for (int i = 0; i < TT::FM; ++i) {
-    int64_t row = m0 + TT::row_of(i) + (lane & 15);
-    if (row >= count) row = count - 1;  // computed and not written
-    const float lse = a.t.lse[row], f = a.t.coef[row] / *a.t.most, more = 1.0f + 2.0f * a.z_loss * lse;
-    const int64_t label = a.t.label[row] - v0;
+    const int64_t row = m0 + TT::row_of(i) + (lane & 15);
+    rows[i] = a.t.row[row < count ? row : count - 1];  // computed and not written
+  }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      t.write(i, h, cols - n0, [&](int j, int e) {
-        const int64_t c = n0 + TT::col_of(j) + 4 * q + e;
-        float p = __builtin_amdgcn_exp2f((t.acc[i][j][e] * a.scale - lse) * kLog2e) * more;
-        if (c == label) p -= 1.0f;
-        return v0 + c < a.V ? f * p : 0.0f;
-      }, [&](int r) { return m0 + r < count ? dz + (m0 + r) * stride + n0 : nullptr; });
+  for (int i = 0; i < TT::FM; ++i) {
+    const float less = rows[i].x, f = rows[i].y * inv, more = rows[i].z * inv;
+    const int64_t label = __float_as_int(rows[i].w) - v0 - n0;
+#pragma unroll
+    for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t.acc[i][j][e] = more * __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], sc, less));
+    // few tiles hold a label of their rows, or the vocabulary's end
+    if (__any(label >= 0 && label < TT::TN)) {
+#pragma unroll
+      for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (label == TT::col_of(j) + 4 * q + e) t.acc[i][j][e] -= f;
+    }
+    if (v0 + n0 + TT::TN > a.V) {
+#pragma unroll
+      for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v0 + n0 + TT::col_of(j) + 4 * q + e >= a.V) t.acc[i][j][e] = 0.0f;
+    }
+    t.template write<0, 2>(i, cols - n0, [&](int j, int e) { return t.acc[i][j][e]; },
+                           [&](int r) { return m0 + r < count ? dz + (m0 + r) * stride + n0 : nullptr; });
   }
 }
 
 // dx of every token from the parts' sums: zeros where it is not learned.
-__global__ __launch_bounds__(256) void ce_dx(Tokens t, const float* sums, int32_t S, int64_t T, int64_t W, float scale,
-                                             bf16_t* dx) {
+__global__ __launch_bounds__(256) void ce_dx(Tokens t, Grad g, int64_t T, int64_t W, bf16_t* dx) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= T * W) return;
-  const int64_t row = i / W, c = i - row * W;
-  const int64_t at = t.place[row];
-  const float f = *t.most * scale;
+  const int64_t row = i / W, at = t.place[row];
   Vec<bf16_t, 8> o;
-  float v[8] = {};
-  if (at >= 0)
-    for (int s = 0; s < S; ++s) {
-      const Vec<float, 8> p = load_vec<8>(sums + ((int64_t)s * T + at) * W + c);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += p.e[j];
-    }
+  for (int j = 0; j < 8; ++j) o.e[j] = (bf16_t)0.0f;
+  if (at >= 0) {
+    const float f = factor_of(g);
+    const Vec<float, 8> v = sum_parts(g.sums, counted(g.grid, *t.n, g.tile), g.tile, at, W, i - row * W);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o.e[j] = (bf16_t)(v[j] * f);
+    for (int j = 0; j < 8; ++j) o.e[j] = (bf16_t)(v.e[j] * f);
+  }
   store_vec<8>(dx + i, o);
 }
 
@@ -351,7 +369,7 @@ struct Backward {
   bf16_t* dz;
   float *dx, *dw;
   int64_t piece;
-  int32_t parts;  // of a piece's product for dx
+  Grid to_dx;  // of a piece's product
   size_t bytes;
 };
 Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
@@ -359,18 +377,23 @@ Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
   const size_t T = (size_t)p.n_tokens;
   Backward b{};
   b.piece = piece_of(p);
-  b.parts = parts_of(p.n_tokens, p.width, b.piece);
+  b.to_dx = grid_of(p.n_tokens > 0 ? p.n_tokens : 1, p.width, b.piece);
   b.t.n = s.take<uint32_t>(1);
   b.t.most = s.take<float>(1);
   b.t.index = s.take<int32_t>(T);
-  b.t.label = s.take<int32_t>(T);
   b.t.place = s.take<int32_t>(T);
-  b.t.coef = s.take<float>(T);
-  b.t.lse = s.take<float>(T);
+  b.t.row = s.take<float4>(T);
   b.t.x = s.take<bf16_t>(T * (size_t)p.width);
   b.dz = s.take<bf16_t>(T * (size_t)b.piece);
-  b.dx = s.take<float>((size_t)b.parts * T * (size_t)p.width);
-  b.dw = s.take<float>(sums_bytes(b.piece, p.width, p.n_tokens) / 4);
+  b.dx = s.take<float>(sums_bytes(b.to_dx, is_big(p.n_tokens, p.width), p.width) / 4);
+  size_t dw = 0;  // the last piece may be in more parts than the others
+  for (int64_t ids : {b.piece < p.n_vocab ? b.piece : (int64_t)p.n_vocab, p.n_vocab % b.piece}) {
+    if (ids == 0) continue;
+    const Grid g = grid_of(ids, p.width, p.n_tokens);
+    const size_t need = g.S > 1 ? sums_bytes(g, is_big(ids, p.width), p.width) : 0;
+    if (need > dw) dw = need;
+  }
+  b.dw = s.take<float>(dw / 4);
   b.bytes = s.at;
   return b;
 }
@@ -432,6 +455,7 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
   }
   const CeArgs a = args_of(p, b.t, x, w);
   if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, lse, dloss, dmean, n_valid, dev_status}, st)) != hipSuccess) return e;
+  Grad g{};
   for (int64_t v0 = 0; v0 < V; v0 += b.piece) {
     const int64_t ids = V - v0 < b.piece ? V - v0 : b.piece, cols = ceil_div(ids, 64) * 64;
     auto go = [&](auto tile) {
@@ -442,31 +466,30 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     };
     e = is_big(T, cols) ? go(Big<bf16_t, true, true>{}) : go(Small<bf16_t, true, true>{});
     if (e != hipSuccess) return e;
-    Grad g{};
+    g = Grad{};
     g.a = {b.dz, T, cols, b.piece};
     g.b = {(const char*)w + v0 * p.w_stride * 2, W, ids, p.w_stride};
     g.n = b.t.n;
-    g.rows = {nullptr, nullptr, T, T, 0};
-    g.S = b.parts;
+    g.f = b.t.most;
+    g.scale = p.scale;
+    g.grid = b.to_dx;
     g.sums = b.dx;
     g.add = v0 > 0;
     if ((e = launch_grad<bf16_t, true, false, false>(g, T, st)) != hipSuccess) return e;
     Grad d{};
     d.a = {b.dz, cols, T, b.piece};
-    d.b = a.x;
+    d.b = {x, W, T, p.x_stride};
     d.b1 = {b.t.x, W, T, W};
-    d.b.rows = W;
-    d.b.k = T;
     d.n = b.t.n;
     d.f = b.t.most;
     d.scale = p.scale;
     d.rows = {(bf16_t*)dw + v0 * W, nullptr, ids, ids, 0};
-    d.S = parts_of(ids, W, T);
-    d.sums = d.S > 1 ? b.dw : nullptr;
+    d.grid = grid_of(ids, W, T);
+    d.sums = d.grid.S > 1 ? b.dw : nullptr;
     if ((e = launch_grad<bf16_t, false, false, true>(d, ids, st)) != hipSuccess) return e;
-    if (d.S > 1 && (e = launch_join<bf16_t>(d, ids, st)) != hipSuccess) return e;
+    if (d.sums && (e = launch_join<bf16_t>(d, ids, st)) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(ce_dx, dim3((unsigned)ceil_div(T * W, 2048)), dim3(256), 0, st, b.t, b.dx, b.parts, T, W, p.scale, (bf16_t*)dx);
+  hipLaunchKernelGGL(ce_dx, dim3((unsigned)ceil_div(T * W, 2048)), dim3(256), 0, st, b.t, g, T, W, (bf16_t*)dx);
   return hipGetLastError();
 }
 

@@ -42,7 +42,7 @@ template <class TT>
 __global__ __launch_bounds__(TT::THREADS) void ff_fwd(FfArgs a) {
   using T = typename TT::T;
   int m, n;
-  my_tile(a.mt, a.nt, m, n);
+  tile_at(blockIdx.x, a.mt, a.nt, m, n);
   const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * (TT::TN / 2), F = a.wg.rows;
   TT t;
   const typename TT::LoadA la(a.x, m0);
@@ -53,10 +53,10 @@ __global__ __launch_bounds__(TT::THREADS) void ff_fwd(FfArgs a) {
     auto to = [&](void* p) {
       return [=](int r) { return m0 + r < a.x.rows ? (T*)p + (m0 + r) * F + n0 : nullptr; };
     };
-    t.write(i, 0, F - n0, [&](int j, int e) { return activation(t.acc[i][j][e], a.act).x * t.acc[i][j + TT::HN][e]; }, to(a.h));
+    t.template write<0, 1>(i, F - n0, [&](int j, int e) { return activation(t.acc[i][j][e], a.act).x * t.acc[i][j + TT::HN][e]; }, to(a.h));
     if (a.g) {
-      t.write(i, 0, F - n0, [&](int j, int e) { return t.acc[i][j][e]; }, to(a.g));
-      t.write(i, 0, F - n0, [&](int j, int e) { return t.acc[i][j + TT::HN][e]; }, to(a.u));
+      t.template write<0, 1>(i, F - n0, [&](int j, int e) { return t.acc[i][j][e]; }, to(a.g));
+      t.template write<0, 1>(i, F - n0, [&](int j, int e) { return t.acc[i][j + TT::HN][e]; }, to(a.u));
     }
   }
 }
@@ -123,19 +123,19 @@ hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, co
     d.b1 = {wu, W, F, p.wu_stride};
     d.k1 = wide;
     d.rows = {dx, nullptr, N, N, 0};
-    d.S = parts_of(N, W, 2 * wide);
-    d.sums = d.S > 1 ? sums : nullptr;
+    d.grid = grid_of(N, W, 2 * wide);
+    d.sums = d.grid.S > 1 ? sums : nullptr;
     if ((e = launch_grad<T, true, true, false>(d, N, st)) != hipSuccess) return e;
-    if (d.S > 1 && (e = launch_join<T>(d, N, st)) != hipSuccess) return e;
+    if (d.sums && (e = launch_join<T>(d, N, st)) != hipSuccess) return e;
   }
   Grad d{};
   d.a = {point, 2 * wide, N, 2 * wide};
   d.b = {x, W, N, p.x_stride};
   d.rows = {dwg, dwu, F, wide, F};
-  d.S = parts_of(2 * wide, W, N);
-  d.sums = d.S > 1 ? sums : nullptr;
+  d.grid = grid_of(2 * wide, W, N);
+  d.sums = d.grid.S > 1 ? sums : nullptr;
   if ((e = launch_grad<T, false, false, false>(d, 2 * wide, st)) != hipSuccess) return e;
-  return d.S > 1 ? launch_join<T>(d, wide + F, st) : hipSuccess;
+  return d.sums ? launch_join<T>(d, wide + F, st) : hipSuccess;
 }
 
 }  // namespace
@@ -143,7 +143,12 @@ hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, co
 size_t gated_ff_workspace_bytes(const argus_gated_ff_t&) { return 0; }
 
 size_t gated_ff_bwd_workspace_bytes(const argus_gated_ff_t& p) {
-  const size_t a = sums_bytes(p.n_tokens, p.width, 2 * wide_of(p)), b = sums_bytes(2 * wide_of(p), p.width, p.n_tokens);
+  const int64_t wide = wide_of(p);
+  auto sums = [&](int64_t rows, int64_t k) {
+    const Grid g = grid_of(rows, p.width, k);
+    return g.S > 1 ? sums_bytes(g, is_big(rows, p.width), p.width) : 0;
+  };
+  const size_t a = sums(p.n_tokens, 2 * wide), b = sums(2 * wide, p.n_tokens);
   return point_bytes(p) + (a > b ? a : b);
 }
 

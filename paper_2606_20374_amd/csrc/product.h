@@ -210,7 +210,6 @@ struct Tile {
   static constexpr int kLoads = LoadA::N + LoadB::N;  // of one half of each
 
   f32x4 acc[FM][FN];
-  T* stage;  // LDS that run leaves free
 
   static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
   static __device__ __forceinline__ int row_of(int b) { return b / HM * (TM / 2) + wave() / WN * (HM * 16) + b % HM * 16; }
@@ -241,29 +240,35 @@ struct Tile {
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  // Rounds the values v(j, e) of row block i and of the columns of half h to T
-  // and writes them by way of LDS: 64 bytes of a row together, where a lane of
-  // the result holds 8. row(r) is the tile's row r in memory, or null; columns
-  // from `cols` on (a multiple of 8) are left out.
-  template <class V, class R>
-  __device__ __forceinline__ void write(int i, int h, int64_t cols, V v, R row) {
-    constexpr int W = HN * 16 + 8;  // 16 bytes more: rows in other banks
-    static_assert(HN == 2 && 16 * W * WM * WN <= TM / 2 * kStep);
+  // Rounds the values v(j, e) of row block i and of the columns of halves H .. H +
+  // NH - 1 to T and writes them by way of LDS: 64 bytes of a row together, where
+  // a lane of the result holds 8. row(r) is the tile's row r in memory, or null;
+  // columns from `cols` on (a multiple of 8) are left out.
+  template <int H, int NH, class V, class R>
+  __device__ __forceinline__ void write(int i, int64_t cols, V v, R row) {
+    constexpr int W = HN * 16 + 8, kEach = TM / 2 * kStep / (WM * WN / 2);  // 16 bytes more: rows in other banks
+    static_assert(HN == 2 && 2 * 16 * W <= kEach);
     const int lane = threadIdx.x & 63;
-    T* s = stage + wave() * 16 * W;
+    T* s = (wave() & 1 ? lds<1, TM>() : lds<0, TM>()) + (wave() >> 1) * kEach;
 #pragma unroll
-    for (int j = 0; j < HN; ++j) {
-      Vec<T, 4> o;
+    for (int h = 0; h < NH; ++h)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o.e[e] = (T)v(h * HN + j, e);
-      *(uint2*)(s + (lane & 15) * W + j * 16 + 4 * (lane >> 4)) = __builtin_bit_cast(uint2, o);
-    }
+      for (int j = 0; j < HN; ++j) {
+        Vec<T, 4> o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o.e[e] = (T)v((H + h) * HN + j, e);
+        *(uint2*)(s + (h * 16 + (lane & 15)) * W + j * 16 + 4 * (lane >> 4)) = __builtin_bit_cast(uint2, o);
+      }
     asm volatile("" ::: "memory");  // one wavefront: LDS takes its instructions in order
     const int c = (lane & 3) * 8;
-    const uint4 x = *(const uint4*)(s + (lane >> 2) * W + c);
-    asm volatile("" ::: "memory");
     T* to = row(row_of(i) + (lane >> 2));
-    if (to && col_of(h * HN) + c < cols) *(uint4*)(to + col_of(h * HN) + c) = x;
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const uint4 x = *(const uint4*)(s + (h * 16 + (lane >> 2)) * W + c);
+      const int64_t col = col_of((H + h) * HN) + c;
+      if (to && col < cols) *(uint4*)(to + col) = x;
+    }
+    asm volatile("" ::: "memory");
   }
 
   // Adds the products of k = k_begin .. k_end - 1 (k_begin a multiple of kStep).
@@ -285,7 +290,6 @@ struct Tile {
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-    stage = a00;
     if (k_begin >= k_end) return;
     constexpr int RA = 2 * HM * (ROWS_A ? 1 : 2), RB = 2 * HN * (ROWS_B ? 1 : 2);
     s16x8 fa[2][2][HM], fb[2][2][HN];
@@ -355,13 +359,13 @@ struct Tile {
   }
 };
 
-// Tile (m, n) of this workgroup, of mt by nt. Workgroups go to the eight XCDs
-// in turn; each XCD takes a consecutive part of the order, which runs through
+// Tile (m, n) of workgroup `at` of mt by nt. Workgroups go to the eight XCDs in
+// turn; each XCD takes a consecutive part of the order, which runs through
 // bands of kBand rows of tiles, so that tiles which share operands are in the
 // same L2 at the same time.
 constexpr int kBand = 8;
-__device__ __forceinline__ void my_tile(int mt, int nt, int& m, int& n) {
-  const int id = (int)xcd_item(blockIdx.x, (int64_t)mt * nt);
+__device__ __forceinline__ void tile_at(int at, int mt, int nt, int& m, int& n) {
+  const int id = (int)xcd_item(at, (int64_t)mt * nt);
   const int band = id / (kBand * nt), in = id - band * (kBand * nt);
   const int high = mt - band * kBand < kBand ? mt - band * kBand : kBand;
   n = in / high;
@@ -389,11 +393,26 @@ __device__ __forceinline__ T* row_at(const Rows& r, int64_t m, int64_t cols) {
   return nullptr;
 }
 
+// A grid of mt by nt tiles in S parts of k, for the most rows there can be. Where
+// the rows are counted on the device and are fewer, the same workgroups take
+// more parts of k, at most `most`.
+struct Grid {
+  int32_t mt, nt, S, most;
+};
+__device__ __forceinline__ Grid counted(Grid g, int64_t count, int tile) {
+  const int all = g.mt * g.nt * g.S;
+  g.mt = (int)((count + tile - 1) / tile);
+  if (g.mt < 1) g.mt = 1;
+  const int s = all / (g.mt * g.nt);
+  g.S = s < g.most ? s : g.most > g.S ? g.most : g.S;
+  return g;
+}
+
 // The gradients' products: B is one operand, or two one after the other along
 // k (the second begins at k1, a multiple of kStep). The rows of A may be
 // counted on the device (*n), or k (COUNT_K): then B is b1 where fewer are
 // counted than there are, else b. Written in T, times f scale where f is there,
-// or, by S parts, as 32-bit sums [S][rows][cols], added to what is there where
+// or, by S parts, as 32-bit sums [S][mt TM][cols], added to what is there where
 // `add` is set.
 struct Grad {
   Operand a, b, b1;
@@ -401,7 +420,8 @@ struct Grad {
   const uint32_t* n;
   Rows rows;
   float* sums;
-  int32_t mt, nt, S, add;
+  Grid grid;
+  int32_t tile, add;  // rows of a tile
   const float* f;
   float scale;
 };
@@ -410,21 +430,23 @@ __device__ __forceinline__ float factor_of(const Grad& g) { return g.f ? *g.f * 
 template <class TT, bool ROWS_A, bool TWO, bool COUNT_K>
 __global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
   using T = typename TT::T;
-  int m, n, begin, end;
-  my_tile(g.mt, g.nt, m, n);
-  const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
-  int64_t kept = g.rows.at1 + g.rows.n1;  // rows of the product
+  Grid grid = g.grid;
   if (g.n) {
     const int64_t count = __builtin_amdgcn_readfirstlane((int)*g.n);
     if (COUNT_K) {
       if (count < g.a.k) g.b = g.b1;
       g.a.k = g.b.k = count;
     } else {
-      if (m0 >= count) return;
+      grid = counted(grid, count, TT::TM);
       g.a.rows = count;
     }
   }
-  my_part(g.a.k, blockIdx.y, g.S, begin, end);
+  const int part = blockIdx.x / (grid.mt * grid.nt);
+  if (part >= grid.S) return;
+  int m, n, begin, end;
+  tile_at(blockIdx.x - part * (grid.mt * grid.nt), grid.mt, grid.nt, m, n);
+  const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
+  my_part(g.a.k, part, grid.S, begin, end);
   TT t;
   const typename TT::LoadA la(g.a, m0);
   const typename TT::LoadB lb(g.b, n0);
@@ -446,20 +468,18 @@ __global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
     const float f = factor_of(g);
 #pragma unroll
     for (int i = 0; i < TT::FM; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        t.write(i, h, cols - n0, [&](int j, int e) { return t.acc[i][j][e] * f; },
-                [&](int r) {
-                  T* row = m0 + r < g.a.rows ? row_at<T>(g.rows, m0 + r, cols) : nullptr;
-                  return row ? row + n0 : nullptr;
-                });
+      t.template write<0, 2>(i, cols - n0, [&](int j, int e) { return t.acc[i][j][e] * f; },
+                             [&](int r) {
+                               T* row = m0 + r < g.a.rows ? row_at<T>(g.rows, m0 + r, cols) : nullptr;
+                               return row ? row + n0 : nullptr;
+                             });
     return;
   }
 #pragma unroll
   for (int i = 0; i < TT::FM; ++i) {
     const int64_t row = m0 + TT::row_of(i) + (lane & 15);
-    if (row >= g.a.rows || row >= kept) continue;
-    float* sum = g.sums + ((int64_t)blockIdx.y * kept + row) * cols;
+    if (row >= g.a.rows) continue;
+    float* sum = g.sums + ((int64_t)part * grid.mt * TT::TM + row) * cols;
 #pragma unroll
     for (int j = 0; j < TT::FN; ++j) {
       const int64_t c = n0 + TT::col_of(j) + 4 * (lane >> 4);
@@ -474,7 +494,17 @@ __global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
   }
 }
 
-// Adds the S parts' sums in their order, eight columns to a thread.
+// Sum of the S parts, in their order, of eight columns.
+__device__ __forceinline__ Vec<float, 8> sum_parts(const float* sums, const Grid& g, int tile, int64_t row, int64_t cols, int64_t c) {
+  Vec<float, 8> v{};
+  for (int s = 0; s < g.S; ++s) {
+    const Vec<float, 8> a = load_vec<8>(sums + (((int64_t)s * g.mt * tile + row) * cols + c));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v.e[j] += a.e[j];
+  }
+  return v;
+}
+
 template <class T>
 __global__ __launch_bounds__(256) void grad_join(Grad g, int64_t rows) {
   const int64_t cols = g.b.rows, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
@@ -483,15 +513,10 @@ __global__ __launch_bounds__(256) void grad_join(Grad g, int64_t rows) {
   T* out = row_at<T>(g.rows, row, cols);
   if (!out) return;
   const float f = factor_of(g);
-  float v[8] = {};
-  for (int s = 0; s < g.S; ++s) {
-    const Vec<float, 8> a = load_vec<8>(g.sums + s * rows * cols + i);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += a.e[j];
-  }
+  const Vec<float, 8> v = sum_parts(g.sums, g.grid, g.tile, row, cols, i - row * cols);
   Vec<T, 8> o;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o.e[j] = (T)(v[j] * f);
+  for (int j = 0; j < 8; ++j) o.e[j] = (T)(v.e[j] * f);
   store_vec<8>(out + i - row * cols, o);
 }
 
@@ -515,19 +540,23 @@ inline int32_t parts_of(int64_t rows, int64_t cols, int64_t k) {
   const int64_t s = want < most ? want : most;
   return s < 1 ? 1 : s > 64 ? 64 : (int32_t)s;
 }
-inline size_t sums_bytes(int64_t rows, int64_t cols, int64_t k) {
-  const int32_t s = parts_of(rows, cols, k);
-  return s > 1 ? align256((size_t)s * (size_t)rows * (size_t)cols * 4) : 0;
+inline Grid grid_of(int64_t rows, int64_t cols, int64_t k) {
+  const int t = is_big(rows, cols) ? 256 : 128;
+  const int64_t most = k / kPart < 64 ? k / kPart : 64;
+  return {(int32_t)ceil_div(rows, t), (int32_t)ceil_div(cols, t), parts_of(rows, cols, k), most < 1 ? 1 : (int32_t)most};
+}
+// 32-bit sums of a product, where it is taken in parts.
+inline size_t sums_bytes(const Grid& g, bool big, int64_t cols) {
+  return align256((size_t)g.S * (size_t)g.mt * (big ? 256 : 128) * (size_t)cols * 4);
 }
 
-// One gradient product of `rows` rows; S parts (1 and no sums: written in T at once).
+// One gradient product of `rows` rows, g.grid of grid_of (without sums: in one part).
 template <class T, bool ROWS_A, bool TWO, bool COUNT_K>
-hipError_t launch_grad(Grad g, int64_t rows, hipStream_t st) {
+hipError_t launch_grad(Grad& g, int64_t rows, hipStream_t st) {
   auto go = [&](auto tile) {
     using TT = decltype(tile);
-    g.mt = (int32_t)ceil_div(rows, TT::TM);
-    g.nt = (int32_t)ceil_div(g.b.rows, TT::TN);
-    hipLaunchKernelGGL((grad_kernel<TT, ROWS_A, TWO, COUNT_K>), dim3((unsigned)(g.mt * g.nt), (unsigned)g.S),
+    g.tile = TT::TM;
+    hipLaunchKernelGGL((grad_kernel<TT, ROWS_A, TWO, COUNT_K>), dim3((unsigned)(g.grid.mt * g.grid.nt * g.grid.S)),
                        dim3(TT::THREADS), 0, st, g);
     return hipGetLastError();
   };
