@@ -24,7 +24,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // The learned tokens, in order.
 struct Tokens {
-  uint32_t* n;     // [1] how many
+  uint32_t* n;     // [2] how many, and a counter of workgroups that are done
   float* most;     // [1] largest |c| that is finite, 1 if that is 0; backward
   int32_t* index;  // [n] token
   int32_t* label;  // [n] forward
@@ -56,7 +56,10 @@ __global__ __launch_bounds__(kIndexThreads) void ce_index(CeArgs a, IndexArgs o)
   __shared__ uint32_t sums[kIndexThreads / 64];
   __shared__ float tops[kIndexThreads / 64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  if (o.status && threadIdx.x == 0) *o.status = 0;
+  if (threadIdx.x == 0) {
+    a.t.n[1] = 0;
+    if (o.status) *o.status = 0;
+  }
   __syncthreads();
   float mean = 0;
   if (o.dmean) {
@@ -214,34 +217,130 @@ __global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, fl
   }
 }
 
-// A token to a wavefront.
-__global__ __launch_bounds__(256) void ce_join(CeArgs a, const float2* part, const float* own, int nt, float* loss,
-                                               float* lse) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= *a.t.n) return;
+// Operands of few tokens: NB blocks of 16 ids from v0 on, and the learned tokens,
+// which need not lie together.
+template <int NB>
+__device__ __forceinline__ void few_weights(const CeArgs& a, int64_t v0, __amdgpu_buffer_rsrc_t (&w)[NB], int (&off)[NB]) {
   const int lane = threadIdx.x & 63;
-  float top = -__builtin_inff(), sum = 0;
-  for (int j = lane; j < nt; j += 64) top = fmaxf(top, part[row * nt + j].x);
 #pragma unroll
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float from = top == -__builtin_inff() ? 0.0f : top;
-  for (int j = lane; j < nt; j += 64) {
-    const float2 p = part[row * nt + j];
-    sum += p.y * __builtin_amdgcn_exp2f((p.x - from) * kLog2e);
+  for (int b = 0; b < NB; ++b) {
+    w[b] = buffer((const char*)a.w.p + (v0 + 16 * b) * a.w.stride * 2, ((a.V - v0 - 16 * b - 1) * a.w.stride + a.w.k) * 2);
+    off[b] = (int)(((lane & 15) * a.w.stride + 8 * (lane >> 4)) * 2);
   }
-  sum = wave_sum_f32(sum);
-  if (lane == 0) {
-    const float rest = logf(sum), all = from + rest;
-    // the largest logit's distance first: a sure token's loss is what is left of the sum
-    loss[a.t.index[row]] = (from - own[row]) + rest + a.z_loss * all * all;
-    lse[a.t.index[row]] = all;
+}
+template <int NT>
+__device__ __forceinline__ void few_tokens(const CeArgs& a, int count, int (&xoff)[NT]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = t * 16 + (lane & 15);
+    xoff[t] = row < count ? (int)((a.t.index[row] * a.x.stride + 8 * (lane >> 4)) * 2) : kNowhere;
   }
 }
 
-__global__ __launch_bounds__(1024) void ce_mean(const float* loss, int64_t T, const uint32_t* n, float* mean) {
+// As ce_fwd for at most kFew tokens: 16 NB ids to a workgroup.
+template <int NT, int NB, int U>
+__global__ __launch_bounds__(64 * kFewWaves) void ce_few(CeArgs a, float2* part, float* own, int nt) {
+  const int lane = threadIdx.x & 63, q = lane >> 4, wave = threadIdx.x >> 6;
+  const int count = (int)*a.t.n, n = (int)xcd_item(blockIdx.x, nt);
+  const int64_t v0 = (int64_t)n * (16 * NB);
+  __amdgpu_buffer_rsrc_t w[NB];
+  int off[NB], xoff[NT];
+  few_weights<NB>(a, v0, w, off);
+  few_tokens<NT>(a, count, xoff);
+  Few<bf16_t, NT, NB, U> s;
+  s.run(w, off, buffer(a.x.p, ((a.T - 1) * a.x.stride + a.x.k) * 2), xoff, (int)a.x.k);
+  s.join();
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = t * 16 + (lane & 15);
+    if (t % kFewWaves != wave || t * 16 >= count) continue;
+    const int64_t label = row < count ? a.t.label[row] - v0 : -1;
+    float top = -__builtin_inff(), sum = 0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = 16 * b + 4 * q + e;
+        float z = s.acc[b][t][e] * a.scale;
+        if (c == label) own[row] = z;
+        if (v0 + c >= a.V) z = -__builtin_inff();
+        s.acc[b][t][e] = z;
+        top = fmaxf(top, z);
+      }
+    top = rows_max(top);
+    const float from = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((s.acc[b][t][e] - from) * kLog2e);
+    sum = rows_sum(sum);
+    if (q == 0 && row < count) part[(int64_t)row * nt + n] = make_float2(top, sum);
+  }
+}
+
+// Adds the pair (top, sum) b to a.
+__device__ __forceinline__ float2 both(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x), from = top == -__builtin_inff() ? 0.0f : top;
+  return make_float2(top, a.y * __builtin_amdgcn_exp2f((a.x - from) * kLog2e) + b.y * __builtin_amdgcn_exp2f((b.x - from) * kLog2e));
+}
+
+// A token to WAVES wavefronts of four. With MEAN the workgroup that is done last
+// takes the mean: losses are written past the caches of its XCD and read past
+// them. Each workgroup then writes its XCD's cache back: of 16,384 tokens that
+// took 133 us, a launch of its own after 22 us takes 5.
+template <int WAVES, bool MEAN>
+__global__ __launch_bounds__(256) void ce_join(CeArgs a, const float2* part, const float* own, int nt, float* loss,
+                                               float* lse, float* mean) {
+  __shared__ float2 pairs[4];
+  __shared__ double sums[4];
+  __shared__ bool last;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = threadIdx.x % (64 * WAVES);
+  const int64_t n = *a.t.n, row = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
+  float2 p = make_float2(-__builtin_inff(), 0.0f);
+  if (row < n)
+    for (int j = in; j < nt; j += 64 * WAVES) p = both(p, part[row * nt + j]);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) p = both(p, make_float2(__shfl_xor(p.x, d), __shfl_xor(p.y, d)));
+  if (WAVES > 1) {
+    if (lane == 0) pairs[wave] = p;
+    __syncthreads();
+    p = pairs[0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) p = both(p, pairs[w]);
+  }
+  if (row < n && in == 0) {
+    const float from = p.x == -__builtin_inff() ? 0.0f : p.x, rest = logf(p.y), all = from + rest;
+    // the largest logit's distance first: a sure token's loss is what is left of the sum
+    __hip_atomic_store(loss + a.t.index[row], (from - own[row]) + rest + a.z_loss * all * all, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+    lse[a.t.index[row]] = all;
+  }
+  if (!MEAN) return;
+  __syncthreads();
+  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.t.n + 1, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  double s = 0;
+  for (int64_t i = threadIdx.x; i < n; i += 256 * 8) {
+    float v[8];  // all under way before the first is added
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      v[j] = i + 256 * j < n ? __hip_atomic_load(loss + a.t.index[i + 256 * j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += v[j];
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if (lane == 0) sums[wave] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) *mean = (float)((sums[0] + sums[1] + sums[2] + sums[3]) / (double)(n ? n : 1));
+}
+
+__global__ __launch_bounds__(1024) void ce_mean(CeArgs a, const float* loss, float* mean) {
   __shared__ double sums[16];
   double s = 0;
-  for (int64_t t = threadIdx.x; t < T; t += 1024) s += loss[t];
+  for (int64_t t = threadIdx.x; t < a.T; t += 1024) s += loss[t];
 #pragma unroll
   for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
@@ -249,7 +348,7 @@ __global__ __launch_bounds__(1024) void ce_mean(const float* loss, int64_t T, co
   if (threadIdx.x) return;
   s = 0;
   for (int j = 0; j < 16; ++j) s += sums[j];
-  *mean = (float)(s / (*n ? *n : 1));
+  *mean = (float)(s / (*a.t.n ? *a.t.n : 1));
 }
 
 // dz of the ids [v0, v0 + cols) of the vocabulary, `cols` a multiple of 64.
@@ -302,6 +401,40 @@ __global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64
   }
 }
 
+// As ce_dz for at most kFew tokens and the whole vocabulary.
+template <int NT, int NB, int U>
+__global__ __launch_bounds__(64 * kFewWaves) void ce_dz_few(CeArgs a, bf16_t* dz, int64_t cols, int64_t stride) {
+  const int lane = threadIdx.x & 63, q = lane >> 4, wave = threadIdx.x >> 6, count = (int)*a.t.n;
+  const int64_t v0 = xcd_item(blockIdx.x, gridDim.x) * (16 * NB);
+  __amdgpu_buffer_rsrc_t w[NB];
+  int off[NB], xoff[NT];
+  few_weights<NB>(a, v0, w, off);
+  few_tokens<NT>(a, count, xoff);
+  Few<bf16_t, NT, NB, U> s;
+  s.run(w, off, buffer(a.x.p, ((a.T - 1) * a.x.stride + a.x.k) * 2), xoff, (int)a.x.k);
+  s.join();
+  const float sc = a.scale * kLog2e, inv = 1.0f / *a.t.most;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = t * 16 + (lane & 15);
+    if (t % kFewWaves != wave || row >= count) continue;
+    const float4 r = a.t.row[row];
+    const int64_t label = __float_as_int(r.w) - v0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int64_t c = v0 + 16 * b + 4 * q;
+      Vec<bf16_t, 4> o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float p = r.z * inv * __builtin_amdgcn_exp2f(fmaf(s.acc[b][t][e], sc, r.x));
+        if (16 * b + 4 * q + e == label) p -= r.y * inv;
+        o.e[e] = (bf16_t)(c + e < a.V ? p : 0.0f);
+      }
+      if (c < cols) store_vec<4>(dz + row * stride + c, o);
+    }
+  }
+}
+
 // dx of every token from the parts' sums: zeros where it is not learned.
 __global__ __launch_bounds__(256) void ce_dx(Tokens t, Grad g, int64_t T, int64_t W, bf16_t* dx) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
@@ -335,7 +468,13 @@ struct Space {
   }
 };
 
-int64_t tiles_n(const argus_cross_entropy_t& p) { return ceil_div(p.n_vocab, is_big(p.n_tokens, p.n_vocab) ? 256 : 128); }
+// Ids that one workgroup of the forward product takes. Few tokens: enough to
+// join a token's sums in a few steps, yet enough workgroups.
+int few_ids(const argus_cross_entropy_t& p) { return p.n_vocab >= 65536 ? 128 : 32; }
+bool is_few(const argus_cross_entropy_t& p) { return p.n_tokens <= kFew && p.n_tokens * p.x_stride < (1 << 29); }
+int64_t tiles_n(const argus_cross_entropy_t& p) {
+  return ceil_div(p.n_vocab, is_few(p) ? few_ids(p) : is_big(p.n_tokens, p.n_vocab) ? 256 : 128);
+}
 // Ids of a piece: at most 2^27 values of dz where the tokens allow it.
 int64_t piece_of(const argus_cross_entropy_t& p) {
   int64_t ids = ((int64_t)1 << 27) / (p.n_tokens > 0 ? p.n_tokens : 1) / 256 * 256;
@@ -354,7 +493,7 @@ Forward forward_space(const argus_cross_entropy_t& p, void* ws) {
   Space s{(char*)ws};
   const size_t T = (size_t)p.n_tokens;
   Forward f{};
-  f.t.n = s.take<uint32_t>(1);
+  f.t.n = s.take<uint32_t>(2);
   f.t.index = s.take<int32_t>(T);
   f.t.label = s.take<int32_t>(T);
   f.t.x = s.take<bf16_t>(T * (size_t)p.width);
@@ -378,7 +517,7 @@ Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
   Backward b{};
   b.piece = piece_of(p);
   b.to_dx = grid_of(p.n_tokens > 0 ? p.n_tokens : 1, p.width, b.piece);
-  b.t.n = s.take<uint32_t>(1);
+  b.t.n = s.take<uint32_t>(2);
   b.t.most = s.take<float>(1);
   b.t.index = s.take<int32_t>(T);
   b.t.place = s.take<int32_t>(T);
@@ -403,10 +542,10 @@ CeArgs args_of(const argus_cross_entropy_t& p, const Tokens& t, const void* x, c
           p.labels, p.ids_64, p.n_tokens, p.n_vocab, p.scale, p.z_loss};
 }
 
-hipError_t launch_tokens(const CeArgs& a, const IndexArgs& o, hipStream_t st) {
+hipError_t launch_tokens(const CeArgs& a, const IndexArgs& o, bool rows, hipStream_t st) {
   hipLaunchKernelGGL(ce_index, dim3(1), dim3(kIndexThreads), 0, st, a, o);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.T == 0) return e;
+  if (e != hipSuccess || !rows) return e;
   hipLaunchKernelGGL(ce_gather, dim3((unsigned)ceil_div(a.T, 4)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
@@ -420,22 +559,43 @@ hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, c
                                 const argus_cross_entropy_out_t& o, void* ws, hipStream_t st) {
   const Forward f = forward_space(p, ws);
   const CeArgs a = args_of(p, f.t, x, w);
-  hipError_t e = launch_tokens(a, {o.loss, o.lse, o.n_valid, nullptr, nullptr, nullptr, nullptr, o.dev_status}, st);
+  hipError_t e = launch_tokens(a, {o.loss, o.lse, o.n_valid, nullptr, nullptr, nullptr, nullptr, o.dev_status},
+                               p.n_tokens > 0 && !is_few(p), st);
   if (e != hipSuccess) return e;
-  if (p.n_tokens > 0) {
-    auto go = [&](auto tile) {
-      using TT = decltype(tile);
-      const int mt = (int)ceil_div(p.n_tokens, TT::TM), nt = (int)ceil_div(p.n_vocab, TT::TN);
-      hipLaunchKernelGGL(ce_fwd<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, f.part, f.own, mt, nt);
-      return hipGetLastError();
-    };
-    e = is_big(p.n_tokens, p.n_vocab) ? go(Big<bf16_t, true, true>{}) : go(Small<bf16_t, true, true>{});
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(ce_join, dim3((unsigned)ceil_div(p.n_tokens, 4)), dim3(256), 0, st, a, f.part, f.own,
-                       (int)tiles_n(p), o.loss, o.lse);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int64_t T = p.n_tokens, V = p.n_vocab;
+  const int nt = (int)tiles_n(p);
+  auto go = [&](auto tile) {
+    using TT = decltype(tile);
+    const int mt = (int)ceil_div(T, TT::TM);
+    hipLaunchKernelGGL(ce_fwd<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, f.part, f.own, mt, nt);
+  };
+  auto few = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)nt), dim3(64 * kFewWaves), 0, st, a, f.part, f.own, nt);
+  };
+  if (T == 0) {
+  } else if (is_few(p)) {
+    if (few_ids(p) == 32) T <= 16 ? few(ce_few<1, 2, 4>) : few(ce_few<2, 2, 3>);
+    else T <= 16 ? few(ce_few<1, 8, 1>) : few(ce_few<2, 8, 1>);
+  } else if (is_big(T, V)) {
+    go(Big<bf16_t, true, true>{});
+  } else if (is_short(T, V)) {
+    go(Short<bf16_t>{});
+  } else {
+    go(Small<bf16_t, true, true>{});
   }
-  hipLaunchKernelGGL(ce_mean, dim3(1), dim3(1024), 0, st, o.loss, p.n_tokens, f.t.n, o.mean);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  auto join = [&](auto kern, int64_t rows) {
+    const int64_t need = ceil_div(T, rows);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(need > 0 ? need : 1)), dim3(256), 0, st, a, f.part, f.own, nt, o.loss, o.lse, o.mean);
+  };
+  // few tokens: a workgroup to each
+  if (T <= 1024) {
+    join(ce_join<4, true>, 1);
+    return hipGetLastError();
+  }
+  join(ce_join<1, false>, 4);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(ce_mean, dim3(1), dim3(1024), 0, st, a, o.loss, o.mean);
   return hipGetLastError();
 }
 
@@ -448,13 +608,13 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
   if (T == 0) {
     if (dev_status) {
       const CeArgs a = args_of(p, b.t, x, w);
-      if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, dev_status}, st)) != hipSuccess) return e;
+      if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, dev_status}, false, st)) != hipSuccess) return e;
     }
     hipLaunchKernelGGL(ce_clear, dim3(2048), dim3(256), 0, st, (bf16_t*)dw, V * W);
     return hipGetLastError();
   }
   const CeArgs a = args_of(p, b.t, x, w);
-  if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, lse, dloss, dmean, n_valid, dev_status}, st)) != hipSuccess) return e;
+  if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, lse, dloss, dmean, n_valid, dev_status}, true, st)) != hipSuccess) return e;
   Grad g{};
   for (int64_t v0 = 0; v0 < V; v0 += b.piece) {
     const int64_t ids = V - v0 < b.piece ? V - v0 : b.piece, cols = ceil_div(ids, 64) * 64;
@@ -464,7 +624,18 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
       hipLaunchKernelGGL(ce_dz<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, b.dz, v0, cols, b.piece, mt, nt);
       return hipGetLastError();
     };
-    e = is_big(T, cols) ? go(Big<bf16_t, true, true>{}) : go(Small<bf16_t, true, true>{});
+    auto few = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div(cols, few_ids(p))), dim3(64 * kFewWaves), 0, st, a, b.dz, cols, b.piece);
+      return hipGetLastError();
+    };
+    if (is_few(p)) {
+      if (few_ids(p) == 32) e = T <= 16 ? few(ce_dz_few<1, 2, 4>) : few(ce_dz_few<2, 2, 3>);
+      else e = T <= 16 ? few(ce_dz_few<1, 8, 1>) : few(ce_dz_few<2, 8, 1>);
+    } else if (is_big(T, cols)) {
+      e = go(Big<bf16_t, true, true>{});
+    } else {
+      e = is_short(T, cols) ? go(Short<bf16_t>{}) : go(Small<bf16_t, true, true>{});
+    }
     if (e != hipSuccess) return e;
     g = Grad{};
     g.a = {b.dz, T, cols, b.piece};

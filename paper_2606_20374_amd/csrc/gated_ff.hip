@@ -61,6 +61,53 @@ __global__ __launch_bounds__(TT::THREADS) void ff_fwd(FfArgs a) {
   }
 }
 
+// FB blocks of 16 gate rows and the same up rows, NT blocks of 16 tokens.
+template <class T, int NT, int FB, int U>
+__global__ __launch_bounds__(64 * kFewWaves) void ff_few(FfArgs a) {
+  const int lane = threadIdx.x & 63, q = lane >> 4, wave = threadIdx.x >> 6;
+  const int64_t F = a.wg.rows, N = a.x.rows, f0 = xcd_item(blockIdx.x, gridDim.x) * (16 * FB);
+  __amdgpu_buffer_rsrc_t w[2 * FB];
+  int off[2 * FB], xoff[NT];
+#pragma unroll
+  for (int b = 0; b < 2 * FB; ++b) {
+    const Operand& o = b < FB ? a.wg : a.wu;
+    const int64_t first = f0 + b % FB * 16;
+    w[b] = buffer((const char*)o.p + first * o.stride * 2, ((F - first - 1) * o.stride + o.k) * 2);
+    off[b] = (int)(((lane & 15) * o.stride + 8 * q) * 2);
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int64_t row = t * 16 + (lane & 15);
+    xoff[t] = row < N ? (int)((row * a.x.stride + 8 * q) * 2) : kNowhere;
+  }
+  Few<T, NT, 2 * FB, U> s;
+  s.run(w, off, buffer(a.x.p, ((N - 1) * a.x.stride + a.x.k) * 2), xoff, (int)a.x.k);
+  s.join();
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t % kFewWaves != wave) continue;
+    const int64_t row = t * 16 + (lane & 15);
+#pragma unroll
+    for (int b = 0; b < FB; ++b) {
+      const int64_t c = f0 + b * 16 + 4 * q;
+      if (row >= N || c >= F) continue;  // F is a multiple of 8
+      Vec<T, 4> h, g, u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float gv = s.acc[b][t][e], uv = s.acc[FB + b][t][e];
+        h.e[e] = (T)(activation(gv, a.act).x * uv);
+        g.e[e] = (T)gv;
+        u.e[e] = (T)uv;
+      }
+      store_vec<4>((T*)a.h + row * F + c, h);
+      if (a.g) {
+        store_vec<4>((T*)a.g + row * F + c, g);
+        store_vec<4>((T*)a.u + row * F + c, u);
+      }
+    }
+  }
+}
+
 // dg and du of a row, eight columns to a thread: [rows][2][wide], zeros from F on.
 template <class T>
 __global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, const T* g, const T* u, T* to, int64_t rows,
@@ -102,7 +149,14 @@ hipError_t forward(const argus_gated_ff_t& p, const void* x, const void* wg, con
     hipLaunchKernelGGL(ff_fwd<TT>, dim3((unsigned)(a.mt * a.nt)), dim3(TT::THREADS), 0, st, a);
     return hipGetLastError();
   };
-  return is_big(p.n_tokens, 2 * (int64_t)p.ff) ? go(Big<T, true, true>{}) : go(Small<T, true, true>{});
+  auto few = [&](auto kern, int rows) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div(p.ff, rows)), dim3(64 * kFewWaves), 0, st, a);
+    return hipGetLastError();
+  };
+  if (p.n_tokens <= 16) return few(ff_few<T, 1, 1, 4>, 16);
+  if (p.n_tokens <= kFew) return few(ff_few<T, 2, 1, 3>, 16);
+  if (is_big(p.n_tokens, 2 * (int64_t)p.ff)) return go(Big<T, true, true>{});
+  return is_short(p.n_tokens, 2 * (int64_t)p.ff) ? go(Short<T>{}) : go(Small<T, true, true>{});
 }
 
 template <class T>

@@ -246,10 +246,10 @@ struct Tile {
   // columns from `cols` on (a multiple of 8) are left out.
   template <int H, int NH, class V, class R>
   __device__ __forceinline__ void write(int i, int64_t cols, V v, R row) {
-    constexpr int W = HN * 16 + 8, kEach = TM / 2 * kStep / (WM * WN / 2);  // 16 bytes more: rows in other banks
+    constexpr int W = HN * 16 + 8, kEach = TN / 2 * kStep / (WM * WN / 2);  // 16 bytes more: rows in other banks
     static_assert(HN == 2 && 2 * 16 * W <= kEach);
     const int lane = threadIdx.x & 63;
-    T* s = (wave() & 1 ? lds<1, TM>() : lds<0, TM>()) + (wave() >> 1) * kEach;
+    T* s = (wave() & 1 ? lds<5, TN>() : lds<4, TN>()) + (wave() >> 1) * kEach;
 #pragma unroll
     for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -393,6 +393,76 @@ __device__ __forceinline__ T* row_at(const Rows& r, int64_t m, int64_t cols) {
   return nullptr;
 }
 
+// Products of few tokens, bound by the bytes of the weights: a workgroup takes NB
+// blocks of 16 weight rows, each read once, straight into registers, by 16-byte
+// pieces of which a wavefront has U times 2 NB under way; its wavefronts take
+// every kFewWaves-th 64 k, and their sums are joined in LDS. The tokens' rows, 16
+// to a block, come from L2.
+constexpr int kFewWaves = 4;
+constexpr int kFew = 32;  // tokens, at most: from 33 on tiles are as fast
+
+template <class T, int NT, int NB, int U>
+struct Few {
+  f32x4 acc[NB][NT];
+
+  // w[b]: the rows of block b, `off[b]` this lane's bytes from its first row on
+  // (row lane % 16, k = 8 (lane / 16)); x and xoff the same of the tokens.
+  __device__ __forceinline__ void run(const __amdgpu_buffer_rsrc_t (&w)[NB], const int (&off)[NB],
+                                      __amdgpu_buffer_rsrc_t x, const int (&xoff)[NT], int K) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = (threadIdx.x & 63) >> 4 << 3;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0, 0, 0, 0};
+    for (int k0 = wave * 64; k0 < K; k0 += kFewWaves * 64 * U) {
+      s16x8 wf[U][2][NB], xf[U][2][NT];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k = k0 + u * kFewWaves * 64 + 32 * h;
+          const bool there = k + at < K;
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+            wf[u][h][b] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(w[b], there ? off[b] : kNowhere, k * 2, 0));
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            xf[u][h][t] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(x, there ? xoff[t] : kNowhere, k * 2, 0));
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[b][t] = mfma(wf[u][h][b], xf[u][h][t], acc[b][t], T{});
+    }
+  }
+
+  // Sums over the wavefronts, in their order: tokens t are then wavefront t %
+  // kFewWaves's.
+  __device__ __forceinline__ void join() {
+    __shared__ f32x4 part[kFewWaves][NB * NT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) part[wave][b * NT + t][lane] = acc[b][t];
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (t % kFewWaves != wave) continue;
+        f32x4 v = part[0][b * NT + t][lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) v += part[w][b * NT + t][lane];
+        acc[b][t] = v;
+      }
+  }
+};
+
 // A grid of mt by nt tiles in S parts of k, for the most rows there can be. Where
 // the rows are counted on the device and are fewer, the same workgroups take
 // more parts of k, at most `most`.
@@ -524,14 +594,24 @@ template <class T, bool ROWS_A, bool ROWS_B>
 using Big = Tile<T, 256, 256, 2, 4, ROWS_A, ROWS_B>;
 template <class T, bool ROWS_A, bool ROWS_B>
 using Small = Tile<T, 128, 128, 2, 2, ROWS_A, ROWS_B>;
+template <class T>
+using Short = Tile<T, 64, 128, 2, 2, true, true>;  // both operands with k innermost
 
 // Tiles of 256 x 256 need a CU's LDS each; of 128 x 128 two fit.
 constexpr int kCus = 256;
-inline bool is_big(int64_t rows, int64_t cols) { return ceil_div(rows, 256) * ceil_div(cols, 256) >= kCus * 3 / 4; }
+inline bool is_big(int64_t rows, int64_t cols) {
+  return rows > 128 && cols > 128 && ceil_div(rows, 256) * ceil_div(cols, 256) >= kCus * 3 / 4;
+}
 inline int64_t tiles_of(int64_t rows, int64_t cols, bool big) {
   const int t = big ? 256 : 128;
   return ceil_div(rows, t) * ceil_div(cols, t);
 }
+// Forward products of so few tiles that not every CU has one of 128 x 128: more
+// and shorter ones, three to a CU. Feed-forward of 100 tokens, 2,048 wide with
+// 8,192 inside (128 tiles): 24.5 us for 28.1; 5,120 with 2,048: 35 for 47; with 256
+// tiles 28.6 for 29.4; with 384 tiles 39.0 for 37.4.
+inline bool is_short(int64_t rows, int64_t cols) { return tiles_of(rows, cols, false) <= kCus; }
+
 // Parts of k where the tiles alone do not fill the chip: at least kPart of k in each.
 constexpr int64_t kPart = 512;
 inline int32_t parts_of(int64_t rows, int64_t cols, int64_t k) {
