@@ -576,12 +576,8 @@ hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, c
   } else if (is_few(p)) {
     if (few_ids(p) == 32) T <= 16 ? few(ce_few<1, 2, 4>) : few(ce_few<2, 2, 3>);
     else T <= 16 ? few(ce_few<1, 8, 1>) : few(ce_few<2, 8, 1>);
-  } else if (is_big(T, V)) {
-    go(Big<bf16_t, true, true>{});
-  } else if (is_short(T, V)) {
-    go(Short<bf16_t>{});
   } else {
-    go(Small<bf16_t, true, true>{});
+    with_tile<bf16_t>(T, V, go);
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   auto join = [&](auto kern, int64_t rows) {
@@ -631,10 +627,8 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     if (is_few(p)) {
       if (few_ids(p) == 32) e = T <= 16 ? few(ce_dz_few<1, 2, 4>) : few(ce_dz_few<2, 2, 3>);
       else e = T <= 16 ? few(ce_dz_few<1, 8, 1>) : few(ce_dz_few<2, 8, 1>);
-    } else if (is_big(T, cols)) {
-      e = go(Big<bf16_t, true, true>{});
     } else {
-      e = is_short(T, cols) ? go(Short<bf16_t>{}) : go(Small<bf16_t, true, true>{});
+      e = with_tile<bf16_t>(T, cols, go);
     }
     if (e != hipSuccess) return e;
     g = Grad{};

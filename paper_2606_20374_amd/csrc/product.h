@@ -21,6 +21,7 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "ops_internal.h"
 
@@ -46,8 +47,8 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16_t) {
 constexpr int kNowhere = 0x7ffffff0;
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int64_t bytes) {
-  if (bytes < 0) bytes = 0;
-  if (bytes > kNowhere) bytes = kNowhere;
+  bytes = bytes < 0 ? 0 : bytes;
+  bytes = bytes > kNowhere ? kNowhere : bytes;
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
 }
 
@@ -133,8 +134,8 @@ struct LoadCols {
   template <class T>
   __device__ __forceinline__ void load(int half, int k0, int k_end, T* tile) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t left = k < k_end ? k - k0 : (int64_t)k_end - k0;
-    const auto r = buffer(p + k0 * stride * 2, left > 0 ? ((left - 1) * stride + cols) * 2 : 0);
+    const int left = (int)(k < k_end ? k : k_end) - k0;
+    const auto r = buffer(p + k0 * stride * 2, ((int64_t)(left - 1) * stride + cols) * 2);
 #pragma unroll
     for (int i = 0; i < N; ++i) load_lds(r, tile + (i * THREADS + wave * 64) * 8, off[half][i], 0);
   }
@@ -199,8 +200,9 @@ __device__ __forceinline__ void meet() {
 // Wavefronts lie WM by WN over it, each with the same share of both halves, so
 // that it takes the tile's quarters one after the other; a feed-forward tile
 // holds gate columns in one half and up columns in the other.
-template <class T_, int TM_, int TN_, int WM_, int WN_, bool ROWS_A, bool ROWS_B>
+template <class T_, int TM_, int TN_, int WM_, int WN_, bool ROWS_A, bool ROWS_B, int STAGES = 2>
 struct Tile {
+  static_assert(STAGES == 2 || STAGES == 4);
   using T = T_;
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, THREADS = 64 * WM * WN;
   static constexpr int FM = TM / WM / 16, FN = TN / WN / 16, HM = FM / 2, HN = FN / 2;
@@ -215,19 +217,27 @@ struct Tile {
   static __device__ __forceinline__ int row_of(int b) { return b / HM * (TM / 2) + wave() / WN * (HM * 16) + b % HM * 16; }
   static __device__ __forceinline__ int col_of(int b) { return b / HN * (TN / 2) + wave() % WN * (HN * 16) + b % HN * 16; }
 
-  // A half tile. Each is an array of its own: reads of one do not wait for loads
-  // into another.
-  template <int WHICH, int SIZE>
+  // What is loaded together, the same half of A and of B (with four stages both
+  // halves), is an array of its own: the compiler waits before a read for the
+  // loads into its array, and tells seven arrays apart. (With arrays for each half
+  // of A and B it waited for all loads every other step.)
+  static constexpr int kArrays = 4, kA = TM / 2 * kStep, kB = TN / 2 * kStep;
+  static constexpr int kArray = (kA + kB) * (STAGES / 2);
+  template <int WHICH>
   static __device__ __forceinline__ T* lds() {
-    __shared__ __align__(16) T half[SIZE / 2 * kStep];
-    return half;
+    __shared__ __align__(16) T array[kArray];
+    return array;
+  }
+  template <int... I>
+  static __device__ __forceinline__ void all_lds(T* (&p)[kArrays], std::integer_sequence<int, I...>) {
+    ((p[I] = lds<I>()), ...);
   }
 
   // Order of a quarter's instructions: its reads from LDS and its loads one by
   // one between the products.
-  template <int LOADS, int READS>
+  template <int LOADS, int READS, int PRODUCTS = 2 * HM * HN>
   static __device__ __forceinline__ void interleave() {
-    constexpr int kProducts = 2 * HM * HN, kAll = READS + LOADS;
+    constexpr int kProducts = PRODUCTS, kAll = READS + LOADS;
 #pragma unroll
     for (int i = 0; i < kProducts; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -246,10 +256,10 @@ struct Tile {
   // columns from `cols` on (a multiple of 8) are left out.
   template <int H, int NH, class V, class R>
   __device__ __forceinline__ void write(int i, int64_t cols, V v, R row) {
-    constexpr int W = HN * 16 + 8, kEach = TN / 2 * kStep / (WM * WN / 2);  // 16 bytes more: rows in other banks
+    constexpr int W = HN * 16 + 8, kEach = kArray / (WM * WN / 2);  // 16 bytes more: rows in other banks
     static_assert(HN == 2 && 2 * 16 * W <= kEach);
     const int lane = threadIdx.x & 63;
-    T* s = (wave() & 1 ? lds<5, TN>() : lds<4, TN>()) + (wave() >> 1) * kEach;
+    T* s = (wave() & 1 ? lds<1>() : lds<0>()) + (wave() >> 1) * kEach;
 #pragma unroll
     for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -273,16 +283,25 @@ struct Tile {
 
   // Adds the products of k = k_begin .. k_end - 1 (k_begin a multiple of kStep).
   //
-  // Two tiles deep, by halves. A step of 64 k takes the quarters (A0, B0), (A0,
-  // B1), (A1, B1), (A1, B0), and during each reads the half that the next one
-  // but one (A0, B0: of the next step) needs. At its first barrier the step's
-  // A0 and B0 have been read by all, and their places get those of the step
-  // after the next; at the second, before (A1, B1), A1 and B1. So each load has
-  // one and a half steps, and two barriers a step are enough.
+  // Two stages: tiles are taken by halves. A step of 64 k takes the quarters (A0,
+  // B0), (A0, B1), (A1, B1), (A1, B0), and during each reads the half that the
+  // next one but one (A0, B0: of the next step) needs. At its first barrier the
+  // step's A0 and B0 have been read by all, and their places get those of the
+  // step after the next; at the second, before (A1, B1), A1 and B1. So each load
+  // has one and a half steps, and two barriers a step are enough.
+  //
+  // Four stages, for workgroups that are alone on their CU: a step reads all
+  // operands of the next one, so that a wavefront with few products does not
+  // wait for LDS at each of them, and a load has three steps.
   template <bool MORE = false>  // to what is there
   __device__ __forceinline__ void run(const LoadA& la, const LoadB& lb, int k_begin, int k_end) {
-    T *a00 = lds<0, TM>(), *a01 = lds<1, TM>(), *a10 = lds<2, TM>(), *a11 = lds<3, TM>();
-    T *b00 = lds<4, TN>(), *b01 = lds<5, TN>(), *b10 = lds<6, TN>(), *b11 = lds<7, TN>();
+    T *arrays[kArrays], *A[2 * STAGES], *B[2 * STAGES];
+    all_lds(arrays, std::make_integer_sequence<int, kArrays>{});
+#pragma unroll
+    for (int i = 0; i < 2 * STAGES; ++i) {
+      A[i] = STAGES == 2 ? arrays[i] : arrays[i / 2] + i % 2 * (kA + kB);
+      B[i] = A[i] + kA;
+    }
     const Read<ROWS_A, TM / 2, HM> ra(wave() / WN * (HM * 16));
     const Read<ROWS_B, TN / 2, HN> rb(wave() % WN * (HN * 16));
     if constexpr (!MORE)
@@ -292,7 +311,7 @@ struct Tile {
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
     if (k_begin >= k_end) return;
     constexpr int RA = 2 * HM * (ROWS_A ? 1 : 2), RB = 2 * HN * (ROWS_B ? 1 : 2);
-    s16x8 fa[2][2][HM], fb[2][2][HN];
+    s16x8 fa[STAGES][2][HM], fb[STAGES][2][HN];
     auto read_a = [&](int to, const T* A) __attribute__((always_inline)) {
 #pragma unroll
       for (int s = 0; s < 2; ++s)
@@ -305,54 +324,93 @@ struct Tile {
 #pragma unroll
         for (int j = 0; j < HN; ++j) fb[to][s][j] = rb.get(B, j, s);
     };
-    // quarter (i, j), the operands of B in fb[of]
-    auto multiply = [&](int hi, int hj, int of) __attribute__((always_inline)) {
+    // quarter (hi, hj), with the operands fa[x] and fb[y]
+    auto multiply = [&](int hi, int hj, int x, int y) __attribute__((always_inline)) {
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int i = 0; i < HM; ++i)
 #pragma unroll
           for (int j = 0; j < HN; ++j)
-            acc[hi * HM + i][hj * HN + j] = mfma(fb[of][s][j], fa[hi][s][i], acc[hi * HM + i][hj * HN + j], T{});
+            acc[hi * HM + i][hj * HN + j] = mfma(fb[y][s][j], fa[x][s][i], acc[hi * HM + i][hj * HN + j], T{});
     };
     auto load = [&](int half, int k0, T* A, T* B) __attribute__((always_inline)) {
       la.load(half, k0, k_end, A);
       lb.load(half, k0, k_end, B);
     };
     int k = k_begin;
-    load(0, k, a00, b00);
-    load(1, k, a01, b01);
-    load(0, k + kStep, a10, b10);
-    load(1, k + kStep, a11, b11);
-    wait_loads<3 * kLoads>();
-    meet();
-    read_a(0, a00);
-    read_b(0, b00);
-    auto step = [&](int x, T* A0, T* A1, T* B0, T* B1, const T* nextA, const T* nextB) __attribute__((always_inline)) {
-      wait_loads<2 * kLoads>();
+    // The loops below have one way in and one out: with a way out in the middle
+    // the compiler allows for paths that leave steps out, on which loads would
+    // still be under way, and waits for all of them in every round.
+    const int steps = (k_end - k_begin + kStep - 1) / kStep;
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load(h, k + s * kStep, A[2 * s + h], B[2 * s + h]);
+    if constexpr (STAGES == 2) {
+      wait_loads<3 * kLoads>();
       meet();
-      load(0, k + 2 * kStep, A0, B0);
-      read_b(x ^ 1, B1);
-      multiply(0, 0, x);
-      interleave<kLoads, RB>();
-      read_a(1, A1);
-      multiply(0, 1, x ^ 1);
-      interleave<0, RA>();
-      wait_loads<2 * kLoads>();
+      read_a(0, A[0]);
+      read_b(0, B[0]);
+      auto step = [&](int x) __attribute__((always_inline)) {
+        const int next = 2 * (x ^ 1);
+        wait_loads<2 * kLoads>();
+        meet();
+        load(0, k + 2 * kStep, A[2 * x], B[2 * x]);
+        read_b(x ^ 1, B[2 * x + 1]);
+        multiply(0, 0, 0, x);
+        interleave<kLoads, RB>();
+        read_a(1, A[2 * x + 1]);
+        multiply(0, 1, 0, x ^ 1);
+        interleave<0, RA>();
+        wait_loads<2 * kLoads>();
+        meet();
+        load(1, k + 2 * kStep, A[2 * x + 1], B[2 * x + 1]);
+        read_a(0, A[next]);
+        multiply(1, 1, 1, x ^ 1);
+        interleave<kLoads, RA>();
+        read_b(x ^ 1, B[next]);
+        multiply(1, 0, 1, x);
+        interleave<0, RB>();
+        k += kStep;
+      };
+      for (int n = steps / 2; n > 0; --n) {
+        step(0);
+        step(1);
+      }
+      if (steps & 1) step(0);
+    } else {
+      auto read = [&](int to, int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          read_a(2 * to + h, A[2 * s + h]);
+          read_b(2 * to + h, B[2 * s + h]);
+        }
+      };
+      wait_loads<6 * kLoads>();
       meet();
-      load(1, k + 2 * kStep, A1, B1);
-      read_a(0, nextA);
-      multiply(1, 1, x ^ 1);
-      interleave<kLoads, RA>();
-      read_b(x ^ 1, nextB);
-      multiply(1, 0, x);
-      interleave<0, RB>();
-      k += kStep;
-      return k < k_end;
-    };
-    while (true) {
-      if (!step(0, a00, a01, b00, b01, a10, b10)) break;
-      if (!step(1, a10, a11, b10, b11, a00, b00)) break;
+      read(0, 0);
+      auto step = [&](int s) __attribute__((always_inline)) {
+        const int x = s & 1;
+        wait_loads<4 * kLoads>();
+        meet();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load(h, k + 4 * kStep, A[2 * s + h], B[2 * s + h]);
+        read(x ^ 1, (s + 1) % 4);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) multiply(h >> 1, h & 1, 2 * x + (h >> 1), 2 * x + (h & 1));
+        interleave<2 * kLoads, 2 * (RA + RB), 2 * FM * FN>();
+        k += kStep;
+      };
+      for (int n = steps / 4; n > 0; --n) {
+        step(0);
+        step(1);
+        step(2);
+        step(3);
+      }
+      if (steps & 3) step(0);
+      if ((steps & 3) > 1) step(1);
+      if ((steps & 3) > 2) step(2);
     }
     wait_loads<0>();  // none may write into LDS that another use has taken
     meet();
@@ -592,10 +650,10 @@ __global__ __launch_bounds__(256) void grad_join(Grad g, int64_t rows) {
 
 template <class T, bool ROWS_A, bool ROWS_B>
 using Big = Tile<T, 256, 256, 2, 4, ROWS_A, ROWS_B>;
-template <class T, bool ROWS_A, bool ROWS_B>
-using Small = Tile<T, 128, 128, 2, 2, ROWS_A, ROWS_B>;
-template <class T>
-using Short = Tile<T, 64, 128, 2, 2, true, true>;  // both operands with k innermost
+template <class T, bool ROWS_A, bool ROWS_B, int STAGES = 2>
+using Small = Tile<T, 128, 128, 2, 2, ROWS_A, ROWS_B, STAGES>;
+template <class T, int STAGES = 2>
+using Short = Tile<T, 64, 128, 2, 2, true, true, STAGES>;  // both operands with k innermost
 
 // Tiles of 256 x 256 need a CU's LDS each; of 128 x 128 two fit.
 constexpr int kCus = 256;
@@ -611,6 +669,15 @@ inline int64_t tiles_of(int64_t rows, int64_t cols, bool big) {
 // 8,192 inside (128 tiles): 24.5 us for 28.1; 5,120 with 2,048: 35 for 47; with 256
 // tiles 28.6 for 29.4; with 384 tiles 39.0 for 37.4.
 inline bool is_short(int64_t rows, int64_t cols) { return tiles_of(rows, cols, false) <= kCus; }
+// A CU with a single workgroup waits for its loads: four stages in place of two.
+inline bool is_deep(int64_t workgroups) { return workgroups <= kCus; }
+// Calls go with the tile for a forward product.
+template <class T, class F>
+auto with_tile(int64_t rows, int64_t cols, F go) {
+  if (is_big(rows, cols)) return go(Big<T, true, true>{});
+  if (!is_short(rows, cols)) return go(Small<T, true, true>{});
+  return is_deep(ceil_div(rows, 64) * ceil_div(cols, 128)) ? go(Short<T, 4>{}) : go(Short<T>{});
+}
 
 // Parts of k where the tiles alone do not fill the chip: at least kPart of k in each.
 constexpr int64_t kPart = 512;
@@ -641,7 +708,8 @@ hipError_t launch_grad(Grad& g, int64_t rows, hipStream_t st) {
     return hipGetLastError();
   };
   if (rows <= 0 || g.b.rows <= 0) return hipSuccess;
-  return is_big(rows, g.b.rows) ? go(Big<T, ROWS_A, false>{}) : go(Small<T, ROWS_A, false>{});
+  if (is_big(rows, g.b.rows)) return go(Big<T, ROWS_A, false>{});
+  return is_deep((int64_t)g.grid.mt * g.grid.nt * g.grid.S) ? go(Small<T, ROWS_A, false, 4>{}) : go(Small<T, ROWS_A, false>{});
 }
 template <class T>
 hipError_t launch_join(const Grad& g, int64_t rows, hipStream_t st) {
