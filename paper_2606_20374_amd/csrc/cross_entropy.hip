@@ -40,7 +40,24 @@ struct CeArgs {
   int32_t ids_64;
   int64_t T, V;
   float scale, z_loss;
+  int32_t* status;
 };
+
+// Where an operator is small, every token is taken and those that are not learned
+// are dropped at the end: index is null, rows are tokens, and n is T.
+__device__ __forceinline__ int64_t count_of(const CeArgs& a) {
+  return a.t.index ? (int64_t)__builtin_amdgcn_readfirstlane((int)*a.t.n) : a.T;
+}
+__device__ __forceinline__ int64_t token_of(const CeArgs& a, int64_t row) { return a.t.index ? a.t.index[row] : row; }
+// The label of a token, at or above V where it is out of range.
+__device__ __forceinline__ int64_t raw_label(const CeArgs& a, int64_t t) {
+  return a.ids_64 ? ((const int64_t*)a.labels)[t] : (int64_t)((const int32_t*)a.labels)[t];
+}
+__device__ __forceinline__ int64_t label_of(const CeArgs& a, int64_t row) {
+  if (a.t.index) return a.t.label[row];
+  const int64_t l = raw_label(a, row);
+  return l < a.V ? l : -1;
+}
 
 constexpr int kIndexThreads = 1024, kEach = 8;
 
@@ -76,7 +93,7 @@ __global__ __launch_bounds__(kIndexThreads) void ce_index(CeArgs a, IndexArgs o)
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
       id[j] = -1;
-      if (mine + j < a.T) id[j] = a.ids_64 ? ((const int64_t*)a.labels)[mine + j] : ((const int32_t*)a.labels)[mine + j];
+      if (mine + j < a.T) id[j] = raw_label(a, mine + j);
       if (id[j] >= a.V) {
         range = true;
         id[j] = -1;
@@ -137,6 +154,53 @@ __global__ __launch_bounds__(kIndexThreads) void ce_index(CeArgs a, IndexArgs o)
   }
 }
 
+// Backward, small: rows of zeros in the place of those of tokens that are not
+// learned, and what ce_index notes of each token. A row to a wavefront.
+__global__ __launch_bounds__(256) void ce_rows(CeArgs a, IndexArgs o) {
+  __shared__ float tops[4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * 4 + w;
+  float mean = 0;
+  if (o.dmean) {
+    const uint32_t d = *o.divisor;
+    mean = *o.dmean / (float)(d ? d : 1);
+  }
+  if (row < a.T) {
+    const int64_t id = label_of(a, row);
+    const bf16_t* from = (const bf16_t*)a.x.p + row * a.x.stride;
+    bf16_t* to = a.t.x + row * a.x.k;
+    Vec<bf16_t, 8> none;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) none.e[j] = (bf16_t)0.0f;
+    for (int64_t c = lane * 8; c < a.x.k; c += 512) store_vec<8>(to + c, id >= 0 ? load_vec<8>(from + c) : none);
+    if (lane == 0) {
+      const float lse = id >= 0 ? o.lse[row] : 0.0f, c = mean + (o.dloss ? o.dloss[row] : 0.0f);
+      // exp(-infinity) for a token that is not learned
+      a.t.row[row] = id >= 0 ? make_float4(-lse * kLog2e, c, c * (1.0f + 2.0f * a.z_loss * lse), __int_as_float((int32_t)id))
+                             : make_float4(-__builtin_inff(), 0.0f, 0.0f, __int_as_float(-1));
+      a.t.place[row] = id >= 0 ? (int32_t)row : -1;
+    }
+  }
+  if (blockIdx.x) return;
+  float top = 0;
+  bool range = false;
+  for (int64_t t = threadIdx.x; t < a.T; t += 256) {
+    const int64_t id = raw_label(a, t);
+    const float c = fabsf(mean + (o.dloss ? o.dloss[t] : 0.0f));
+    if (id >= 0 && id < a.V && c < __builtin_inff()) top = fmaxf(top, c);
+    range |= id >= a.V;
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) tops[w] = top;
+  if (threadIdx.x == 0 && o.status) *o.status = 0;
+  __syncthreads();
+  if (range && o.status) atomicOr(o.status, ARGUS_DEV_TOKEN_RANGE);
+  if (threadIdx.x) return;
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  *a.t.most = top > 0.0f ? top : 1.0f;
+}
+
 // A row to a wavefront.
 __global__ __launch_bounds__(256) void ce_gather(CeArgs a) {
   const int64_t n = *a.t.n, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -147,7 +211,7 @@ __global__ __launch_bounds__(256) void ce_gather(CeArgs a) {
 }
 
 __device__ __forceinline__ Operand learned(const CeArgs& a, int64_t n) {
-  if (n == a.T) return a.x;
+  if (!a.t.index || n == a.T) return a.x;
   return {a.t.x, n, a.x.k, a.x.k};
 }
 
@@ -159,10 +223,17 @@ __device__ __forceinline__ float rows_max(float v) {
   return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
 }
 
+// Before the join, where no launch has numbered the tokens.
+__device__ __forceinline__ void clear_for_join(const CeArgs& a) {
+  a.t.n[1] = 0;
+  if (a.status) *a.status = 0;
+}
+
 template <class TT>
 __global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, float* own, int mt, int nt) {
   __shared__ float2 join[TT::WN][TT::TM];
-  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n);
+  const int64_t count = count_of(a);
+  if (!a.t.index && blockIdx.x == 0 && threadIdx.x == 0) clear_for_join(a);
   mt = (int)((count + TT::TM - 1) / TT::TM);
   if (blockIdx.x >= (unsigned)mt * nt) return;
   int m, n;
@@ -176,7 +247,7 @@ __global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, fl
 #pragma unroll
   for (int i = 0; i < TT::FM; ++i) {
     const int at = TT::row_of(i) + (lane & 15);
-    const int64_t label = m0 + at < count ? a.t.label[m0 + at] - n0 : -1;
+    const int64_t label = m0 + at < count ? label_of(a, m0 + at) - n0 : -1;
     float top = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < TT::FN; ++j)
@@ -234,7 +305,7 @@ __device__ __forceinline__ void few_tokens(const CeArgs& a, int count, int (&xof
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = t * 16 + (lane & 15);
-    xoff[t] = row < count ? (int)((a.t.index[row] * a.x.stride + 8 * (lane >> 4)) * 2) : kNowhere;
+    xoff[t] = row < count ? (int)((token_of(a, row) * a.x.stride + 8 * (lane >> 4)) * 2) : kNowhere;
   }
 }
 
@@ -242,7 +313,8 @@ __device__ __forceinline__ void few_tokens(const CeArgs& a, int count, int (&xof
 template <int NT, int NB, int U>
 __global__ __launch_bounds__(64 * kFewWaves) void ce_few(CeArgs a, float2* part, float* own, int nt) {
   const int lane = threadIdx.x & 63, q = lane >> 4, wave = threadIdx.x >> 6;
-  const int count = (int)*a.t.n, n = (int)xcd_item(blockIdx.x, nt);
+  const int count = (int)count_of(a), n = (int)xcd_item(blockIdx.x, nt);
+  if (!a.t.index && blockIdx.x == 0 && threadIdx.x == 0) clear_for_join(a);
   const int64_t v0 = (int64_t)n * (16 * NB);
   __amdgpu_buffer_rsrc_t w[NB];
   int off[NB], xoff[NT];
@@ -255,7 +327,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void ce_few(CeArgs a, float2* part,
   for (int t = 0; t < NT; ++t) {
     const int row = t * 16 + (lane & 15);
     if (t % kFewWaves != wave || t * 16 >= count) continue;
-    const int64_t label = row < count ? a.t.label[row] - v0 : -1;
+    const int64_t label = row < count ? label_of(a, row) - v0 : -1;
     float top = -__builtin_inff(), sum = 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -291,12 +363,13 @@ __device__ __forceinline__ float2 both(float2 a, float2 b) {
 // took 133 us, a launch of its own after 22 us takes 5.
 template <int WAVES, bool MEAN>
 __global__ __launch_bounds__(256) void ce_join(CeArgs a, const float2* part, const float* own, int nt, float* loss,
-                                               float* lse, float* mean) {
+                                               float* lse, float* mean, uint32_t* n_valid) {
   __shared__ float2 pairs[4];
   __shared__ double sums[4];
+  __shared__ uint32_t counts[4];
   __shared__ bool last;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = threadIdx.x % (64 * WAVES);
-  const int64_t n = *a.t.n, row = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
+  const int64_t n = count_of(a), row = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
   float2 p = make_float2(-__builtin_inff(), 0.0f);
   if (row < n)
     for (int j = in; j < nt; j += 64 * WAVES) p = both(p, part[row * nt + j]);
@@ -310,11 +383,19 @@ __global__ __launch_bounds__(256) void ce_join(CeArgs a, const float2* part, con
     for (int w = 1; w < 4; ++w) p = both(p, pairs[w]);
   }
   if (row < n && in == 0) {
-    const float from = p.x == -__builtin_inff() ? 0.0f : p.x, rest = logf(p.y), all = from + rest;
-    // the largest logit's distance first: a sure token's loss is what is left of the sum
-    __hip_atomic_store(loss + a.t.index[row], (from - own[row]) + rest + a.z_loss * all * all, __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-    lse[a.t.index[row]] = all;
+    const int64_t t = token_of(a, row);
+    const float from = p.x == -__builtin_inff() ? 0.0f : p.x, rest = logf(p.y);
+    float all = from + rest, l;
+    if (a.t.index || (raw_label(a, t) >= 0 && raw_label(a, t) < a.V)) {
+      // the largest logit's distance first: a sure token's loss is what is left of the sum
+      l = (from - own[row]) + rest + a.z_loss * all * all;
+    } else {
+      l = 0.0f;
+      all = -__builtin_inff();
+      if (a.status && raw_label(a, t) >= a.V) atomicOr(a.status, ARGUS_DEV_TOKEN_RANGE);
+    }
+    __hip_atomic_store(loss + t, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    lse[t] = all;
   }
   if (!MEAN) return;
   __syncthreads();
@@ -322,19 +403,32 @@ __global__ __launch_bounds__(256) void ce_join(CeArgs a, const float2* part, con
   __syncthreads();
   if (!last) return;
   double s = 0;
-  for (int64_t i = threadIdx.x; i < n; i += 256 * 8) {
-    float v[8];  // all under way before the first is added
+  uint32_t c = 0;
+  for (int64_t i = threadIdx.x; i < a.T; i += 256 * 4) {
+    float v[4];  // all under way before the first is added
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      v[j] = i + 256 * j < n ? __hip_atomic_load(loss + a.t.index[i + 256 * j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+      const int64_t t = i + 256 * j;
+      v[j] = t < a.T ? __hip_atomic_load(loss + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
+      c += t < a.T && raw_label(a, t) >= 0 && raw_label(a, t) < a.V;
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s += v[j];
+    for (int j = 0; j < 4; ++j) s += v[j];
   }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-  if (lane == 0) sums[wave] = s;
+  for (int d = 32; d; d >>= 1) {
+    s += __shfl_xor(s, d);
+    c += __shfl_xor(c, d);
+  }
+  if (lane == 0) {
+    sums[wave] = s;
+    counts[wave] = c;
+  }
   __syncthreads();
-  if (threadIdx.x == 0) *mean = (float)((sums[0] + sums[1] + sums[2] + sums[3]) / (double)(n ? n : 1));
+  if (threadIdx.x) return;
+  c = counts[0] + counts[1] + counts[2] + counts[3];
+  *n_valid = c;
+  *mean = (float)((sums[0] + sums[1] + sums[2] + sums[3]) / (double)(c ? c : 1));
 }
 
 __global__ __launch_bounds__(1024) void ce_mean(CeArgs a, const float* loss, float* mean) {
@@ -355,7 +449,7 @@ __global__ __launch_bounds__(1024) void ce_mean(CeArgs a, const float* loss, flo
 template <class TT>
 __global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64_t v0, int64_t cols, int64_t stride,
                                                      int mt, int nt) {
-  const int64_t count = __builtin_amdgcn_readfirstlane((int)*a.t.n);
+  const int64_t count = count_of(a);
   mt = (int)((count + TT::TM - 1) / TT::TM);
   if (blockIdx.x >= (unsigned)mt * nt) return;
   int m, n;
@@ -404,7 +498,7 @@ __global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64
 // As ce_dz for at most kFew tokens and the whole vocabulary.
 template <int NT, int NB, int U>
 __global__ __launch_bounds__(64 * kFewWaves) void ce_dz_few(CeArgs a, bf16_t* dz, int64_t cols, int64_t stride) {
-  const int lane = threadIdx.x & 63, q = lane >> 4, wave = threadIdx.x >> 6, count = (int)*a.t.n;
+  const int lane = threadIdx.x & 63, q = lane >> 4, wave = threadIdx.x >> 6, count = (int)count_of(a);
   const int64_t v0 = xcd_item(blockIdx.x, gridDim.x) * (16 * NB);
   __amdgpu_buffer_rsrc_t w[NB];
   int off[NB], xoff[NT];
@@ -445,7 +539,7 @@ __global__ __launch_bounds__(256) void ce_dx(Tokens t, Grad g, int64_t T, int64_
   for (int j = 0; j < 8; ++j) o.e[j] = (bf16_t)0.0f;
   if (at >= 0) {
     const float f = factor_of(g);
-    const Vec<float, 8> v = sum_parts(g.sums, counted(g.grid, *t.n, g.tile), g.tile, at, W, i - row * W);
+    const Vec<float, 8> v = sum_parts(g.sums, g.n ? counted(g.grid, *g.n, g.tile) : g.grid, g.tile, at, W, i - row * W);
 #pragma unroll
     for (int j = 0; j < 8; ++j) o.e[j] = (bf16_t)(v.e[j] * f);
   }
@@ -472,6 +566,11 @@ struct Space {
 // join a token's sums in a few steps, yet enough workgroups.
 int few_ids(const argus_cross_entropy_t& p) { return p.n_vocab >= 65536 ? 128 : 32; }
 bool is_few(const argus_cross_entropy_t& p) { return p.n_tokens <= kFew && p.n_tokens * p.x_stride < (1 << 29); }
+// Numbering the tokens costs two launches, about 10 us; taking them all costs at
+// most 8 G multiplications, about that.
+bool is_small(const argus_cross_entropy_t& p) {
+  return is_few(p) || (p.n_tokens <= 1024 && p.n_tokens * p.n_vocab * p.width <= (int64_t)1 << 32);
+}
 int64_t tiles_n(const argus_cross_entropy_t& p) {
   return ceil_div(p.n_vocab, is_few(p) ? few_ids(p) : is_big(p.n_tokens, p.n_vocab) ? 256 : 128);
 }
@@ -539,7 +638,7 @@ Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
 
 CeArgs args_of(const argus_cross_entropy_t& p, const Tokens& t, const void* x, const void* w) {
   return {t, {x, p.n_tokens, p.width, p.x_stride}, {w, p.n_vocab, p.width, p.w_stride},
-          p.labels, p.ids_64, p.n_tokens, p.n_vocab, p.scale, p.z_loss};
+          p.labels, p.ids_64, p.n_tokens, p.n_vocab, p.scale, p.z_loss, nullptr};
 }
 
 hipError_t launch_tokens(const CeArgs& a, const IndexArgs& o, bool rows, hipStream_t st) {
@@ -558,11 +657,14 @@ size_t cross_entropy_bwd_workspace_bytes(const argus_cross_entropy_t& p) { retur
 hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, const void* w,
                                 const argus_cross_entropy_out_t& o, void* ws, hipStream_t st) {
   const Forward f = forward_space(p, ws);
-  const CeArgs a = args_of(p, f.t, x, w);
-  hipError_t e = launch_tokens(a, {o.loss, o.lse, o.n_valid, nullptr, nullptr, nullptr, nullptr, o.dev_status},
-                               p.n_tokens > 0 && !is_few(p), st);
-  if (e != hipSuccess) return e;
+  CeArgs a = args_of(p, f.t, x, w);
   const int64_t T = p.n_tokens, V = p.n_vocab;
+  const bool small = T > 0 && is_small(p);
+  a.status = o.dev_status;
+  hipError_t e;
+  if (small) a.t.index = nullptr;
+  else if ((e = launch_tokens(a, {o.loss, o.lse, o.n_valid, nullptr, nullptr, nullptr, nullptr, o.dev_status}, T > 0, st)) != hipSuccess)
+    return e;
   const int nt = (int)tiles_n(p);
   auto go = [&](auto tile) {
     using TT = decltype(tile);
@@ -582,7 +684,7 @@ hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, c
   if ((e = hipGetLastError()) != hipSuccess) return e;
   auto join = [&](auto kern, int64_t rows) {
     const int64_t need = ceil_div(T, rows);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(need > 0 ? need : 1)), dim3(256), 0, st, a, f.part, f.own, nt, o.loss, o.lse, o.mean);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(need > 0 ? need : 1)), dim3(256), 0, st, a, f.part, f.own, nt, o.loss, o.lse, o.mean, o.n_valid);
   };
   // few tokens: a workgroup to each
   if (T <= 1024) {
@@ -609,8 +711,19 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     hipLaunchKernelGGL(ce_clear, dim3(2048), dim3(256), 0, st, (bf16_t*)dw, V * W);
     return hipGetLastError();
   }
-  const CeArgs a = args_of(p, b.t, x, w);
-  if ((e = launch_tokens(a, {nullptr, nullptr, nullptr, lse, dloss, dmean, n_valid, dev_status}, true, st)) != hipSuccess) return e;
+  CeArgs a = args_of(p, b.t, x, w);
+  const IndexArgs io{nullptr, nullptr, nullptr, lse, dloss, dmean, n_valid, dev_status};
+  const bool small = is_small(p);
+  if (small) {
+    a.t.index = nullptr;
+    hipLaunchKernelGGL(ce_rows, dim3((unsigned)ceil_div(T, 4)), dim3(256), 0, st, a, io);
+    e = hipGetLastError();
+    a.x = {b.t.x, T, W, W};
+  } else {
+    e = launch_tokens(a, io, true, st);
+  }
+  if (e != hipSuccess) return e;
+  const bool whole = small && b.piece >= V && b.to_dx.S == 1;  // dx leaves the product as it is
   Grad g{};
   for (int64_t v0 = 0; v0 < V; v0 += b.piece) {
     const int64_t ids = V - v0 < b.piece ? V - v0 : b.piece, cols = ceil_div(ids, 64) * 64;
@@ -634,26 +747,31 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     g = Grad{};
     g.a = {b.dz, T, cols, b.piece};
     g.b = {(const char*)w + v0 * p.w_stride * 2, W, ids, p.w_stride};
-    g.n = b.t.n;
+    g.n = small ? nullptr : b.t.n;
     g.f = b.t.most;
     g.scale = p.scale;
     g.grid = b.to_dx;
-    g.sums = b.dx;
     g.add = v0 > 0;
-    if ((e = launch_grad<bf16_t, true, false, false>(g, T, st)) != hipSuccess) return e;
+    if (whole) {
+      g.rows = {dx, nullptr, T, T, 0};
+      g.place = b.t.place;
+    } else {
+      g.sums = b.dx;
+    }
     Grad d{};
     d.a = {b.dz, cols, T, b.piece};
-    d.b = {x, W, T, p.x_stride};
+    d.b = {a.x.p, W, T, a.x.stride};
     d.b1 = {b.t.x, W, T, W};
-    d.n = b.t.n;
+    d.n = g.n;
     d.f = b.t.most;
     d.scale = p.scale;
     d.rows = {(bf16_t*)dw + v0 * W, nullptr, ids, ids, 0};
     d.grid = grid_of(ids, W, T);
     d.sums = d.grid.S > 1 ? b.dw : nullptr;
-    if ((e = launch_grad<bf16_t, false, false, true>(d, ids, st)) != hipSuccess) return e;
+    if ((e = launch_grads<bf16_t, false, true>(g, T, d, ids, st)) != hipSuccess) return e;
     if (d.sums && (e = launch_join<bf16_t>(d, ids, st)) != hipSuccess) return e;
   }
+  if (whole) return hipSuccess;
   hipLaunchKernelGGL(ce_dx, dim3((unsigned)ceil_div(T * W, 2048)), dim3(256), 0, st, b.t, g, T, W, (bf16_t*)dx);
   return hipGetLastError();
 }

@@ -137,6 +137,12 @@ __global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, con
 int64_t wide_of(const argus_gated_ff_t& p) { return ceil_div(p.ff, 64) * 64; }
 size_t point_bytes(const argus_gated_ff_t& p) { return align256((size_t)p.n_tokens * 2 * (size_t)wide_of(p) * 2); }
 
+size_t sums_of(const argus_gated_ff_t& p, int64_t rows, int64_t k) {
+  const Grid g = grid_of(rows, p.width, k);
+  return g.S > 1 ? sums_bytes(g, is_big(rows, p.width), p.width) : 0;
+}
+size_t dx_sums(const argus_gated_ff_t& p) { return sums_of(p, p.n_tokens, 2 * wide_of(p)); }
+
 template <class T>
 hipError_t forward(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g, void* u,
                    hipStream_t st) {
@@ -170,25 +176,23 @@ hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, co
     hipLaunchKernelGGL(ff_point<T>, dim3((unsigned)(need < 16384 ? need : 16384)), dim3(256), 0, st, (const T*)dh,
                        p.dh_stride, (const T*)g, (const T*)u, point, N, p.ff, (int32_t)wide, p.act);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    Grad d{};
-    d.a = {point, N, 2 * wide, 2 * wide};
-    d.b = {wg, W, F, p.wg_stride};
-    d.b1 = {wu, W, F, p.wu_stride};
-    d.k1 = wide;
-    d.rows = {dx, nullptr, N, N, 0};
-    d.grid = grid_of(N, W, 2 * wide);
-    d.sums = d.grid.S > 1 ? sums : nullptr;
-    if ((e = launch_grad<T, true, true, false>(d, N, st)) != hipSuccess) return e;
-    if (d.sums && (e = launch_join<T>(d, N, st)) != hipSuccess) return e;
   }
-  Grad d{};
-  d.a = {point, 2 * wide, N, 2 * wide};
-  d.b = {x, W, N, p.x_stride};
-  d.rows = {dwg, dwu, F, wide, F};
-  d.grid = grid_of(2 * wide, W, N);
-  d.sums = d.grid.S > 1 ? sums : nullptr;
-  if ((e = launch_grad<T, false, false, false>(d, 2 * wide, st)) != hipSuccess) return e;
-  return d.sums ? launch_join<T>(d, wide + F, st) : hipSuccess;
+  Grad dinput{}, dweights{};
+  dinput.a = {point, N, 2 * wide, 2 * wide};
+  dinput.b = {wg, W, F, p.wg_stride};
+  dinput.b1 = {wu, W, F, p.wu_stride};
+  dinput.k1 = wide;
+  dinput.rows = {dx, nullptr, N, N, 0};
+  dinput.grid = grid_of(N, W, 2 * wide);
+  dinput.sums = dinput.grid.S > 1 ? sums : nullptr;
+  dweights.a = {point, 2 * wide, N, 2 * wide};
+  dweights.b = {x, W, N, p.x_stride};
+  dweights.rows = {dwg, dwu, F, wide, F};
+  dweights.grid = grid_of(2 * wide, W, N);
+  dweights.sums = dweights.grid.S > 1 ? sums + dx_sums(p) / 4 : nullptr;
+  if ((e = launch_grads<T, true, false>(dinput, N, dweights, 2 * wide, st)) != hipSuccess) return e;
+  if (dinput.sums && (e = launch_join<T>(dinput, N, st)) != hipSuccess) return e;
+  return dweights.sums ? launch_join<T>(dweights, wide + F, st) : hipSuccess;
 }
 
 }  // namespace
@@ -196,13 +200,7 @@ hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, co
 size_t gated_ff_workspace_bytes(const argus_gated_ff_t&) { return 0; }
 
 size_t gated_ff_bwd_workspace_bytes(const argus_gated_ff_t& p) {
-  const int64_t wide = wide_of(p);
-  auto sums = [&](int64_t rows, int64_t k) {
-    const Grid g = grid_of(rows, p.width, k);
-    return g.S > 1 ? sums_bytes(g, is_big(rows, p.width), p.width) : 0;
-  };
-  const size_t a = sums(p.n_tokens, 2 * wide), b = sums(2 * wide, p.n_tokens);
-  return point_bytes(p) + (a > b ? a : b);
+  return point_bytes(p) + dx_sums(p) + sums_of(p, 2 * wide_of(p), p.n_tokens);
 }
 
 hipError_t launch_gated_ff(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g,

@@ -196,6 +196,21 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
+// Arrays of a workgroup's LDS. Kernels that hold tiles of several layouts use
+// the same ones for all.
+template <class T, int SIZE>
+struct Lds {
+  template <int WHICH>
+  static __device__ __forceinline__ T* array() {
+    __shared__ __align__(16) T a[SIZE];
+    return a;
+  }
+  template <int N, int... I>
+  static __device__ __forceinline__ void all(T* (&p)[N], std::integer_sequence<int, I...>) {
+    ((p[I] = array<I>()), ...);
+  }
+};
+
 // The tile of a workgroup, in two halves of its rows and two of its columns.
 // Wavefronts lie WM by WN over it, each with the same share of both halves, so
 // that it takes the tile's quarters one after the other; a feed-forward tile
@@ -223,15 +238,7 @@ struct Tile {
   // of A and B it waited for all loads every other step.)
   static constexpr int kArrays = 4, kA = TM / 2 * kStep, kB = TN / 2 * kStep;
   static constexpr int kArray = (kA + kB) * (STAGES / 2);
-  template <int WHICH>
-  static __device__ __forceinline__ T* lds() {
-    __shared__ __align__(16) T array[kArray];
-    return array;
-  }
-  template <int... I>
-  static __device__ __forceinline__ void all_lds(T* (&p)[kArrays], std::integer_sequence<int, I...>) {
-    ((p[I] = lds<I>()), ...);
-  }
+  using Shared = Lds<T, kArray>;
 
   // Order of a quarter's instructions: its reads from LDS and its loads one by
   // one between the products.
@@ -259,7 +266,7 @@ struct Tile {
     constexpr int W = HN * 16 + 8, kEach = kArray / (WM * WN / 2);  // 16 bytes more: rows in other banks
     static_assert(HN == 2 && 2 * 16 * W <= kEach);
     const int lane = threadIdx.x & 63;
-    T* s = (wave() & 1 ? lds<1>() : lds<0>()) + (wave() >> 1) * kEach;
+    T* s = (wave() & 1 ? Shared::template array<1>() : Shared::template array<0>()) + (wave() >> 1) * kEach;
 #pragma unroll
     for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -296,7 +303,7 @@ struct Tile {
   template <bool MORE = false>  // to what is there
   __device__ __forceinline__ void run(const LoadA& la, const LoadB& lb, int k_begin, int k_end) {
     T *arrays[kArrays], *A[2 * STAGES], *B[2 * STAGES];
-    all_lds(arrays, std::make_integer_sequence<int, kArrays>{});
+    Shared::all(arrays, std::make_integer_sequence<int, kArrays>{});
 #pragma unroll
     for (int i = 0; i < 2 * STAGES; ++i) {
       A[i] = STAGES == 2 ? arrays[i] : arrays[i / 2] + i % 2 * (kA + kB);
@@ -552,11 +559,12 @@ struct Grad {
   int32_t tile, add;  // rows of a tile
   const float* f;
   float scale;
+  const int32_t* place;
 };
 __device__ __forceinline__ float factor_of(const Grad& g) { return g.f ? *g.f * g.scale : 1.0f; }
 
-template <class TT, bool ROWS_A, bool TWO, bool COUNT_K>
-__global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
+template <class TT, bool TWO, bool COUNT_K>
+__device__ __forceinline__ void grad_body(Grad g, int block) {
   using T = typename TT::T;
   Grid grid = g.grid;
   if (g.n) {
@@ -569,10 +577,10 @@ __global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
       g.a.rows = count;
     }
   }
-  const int part = blockIdx.x / (grid.mt * grid.nt);
+  const int part = block / (grid.mt * grid.nt);
   if (part >= grid.S) return;
   int m, n, begin, end;
-  tile_at(blockIdx.x - part * (grid.mt * grid.nt), grid.mt, grid.nt, m, n);
+  tile_at(block - part * (grid.mt * grid.nt), grid.mt, grid.nt, m, n);
   const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
   my_part(g.a.k, part, grid.S, begin, end);
   TT t;
@@ -595,12 +603,15 @@ __global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
   if (!g.sums) {
     const float f = factor_of(g);
 #pragma unroll
-    for (int i = 0; i < TT::FM; ++i)
-      t.template write<0, 2>(i, cols - n0, [&](int j, int e) { return t.acc[i][j][e] * f; },
+    for (int i = 0; i < TT::FM; ++i) {
+      const int64_t mine = m0 + TT::row_of(i) + (lane & 15);
+      const bool none = g.place && mine < g.a.rows && g.place[mine] < 0;
+      t.template write<0, 2>(i, cols - n0, [&](int j, int e) { return none ? 0.0f : t.acc[i][j][e] * f; },
                              [&](int r) {
                                T* row = m0 + r < g.a.rows ? row_at<T>(g.rows, m0 + r, cols) : nullptr;
                                return row ? row + n0 : nullptr;
                              });
+    }
     return;
   }
 #pragma unroll
@@ -620,6 +631,18 @@ __global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
       *(float4*)(sum + c) = v;
     }
   }
+}
+
+template <class TT, bool TWO, bool COUNT_K>
+__global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
+  grad_body<TT, TWO, COUNT_K>(g, blockIdx.x);
+}
+// Both gradients of an operator that have few tiles: the input's (A with k
+// innermost) first, then the weights'.
+template <class T, int STAGES, bool TWO, bool COUNT_K>
+__global__ __launch_bounds__(256) void grad_pair(Grad x, Grad w, int blocks_x) {
+  if ((int)blockIdx.x < blocks_x) grad_body<Tile<T, 128, 128, 2, 2, true, false, STAGES>, TWO, false>(x, blockIdx.x);
+  else grad_body<Tile<T, 128, 128, 2, 2, false, false, STAGES>, false, COUNT_K>(w, blockIdx.x - blocks_x);
 }
 
 // Sum of the S parts, in their order, of eight columns.
@@ -703,13 +726,28 @@ hipError_t launch_grad(Grad& g, int64_t rows, hipStream_t st) {
   auto go = [&](auto tile) {
     using TT = decltype(tile);
     g.tile = TT::TM;
-    hipLaunchKernelGGL((grad_kernel<TT, ROWS_A, TWO, COUNT_K>), dim3((unsigned)(g.grid.mt * g.grid.nt * g.grid.S)),
+    hipLaunchKernelGGL((grad_kernel<TT, TWO, COUNT_K>), dim3((unsigned)(g.grid.mt * g.grid.nt * g.grid.S)),
                        dim3(TT::THREADS), 0, st, g);
     return hipGetLastError();
   };
   if (rows <= 0 || g.b.rows <= 0) return hipSuccess;
   if (is_big(rows, g.b.rows)) return go(Big<T, ROWS_A, false>{});
   return is_deep((int64_t)g.grid.mt * g.grid.nt * g.grid.S) ? go(Small<T, ROWS_A, false, 4>{}) : go(Small<T, ROWS_A, false>{});
+}
+// The gradients of an operator's input (rows_x rows) and of its weights.
+template <class T, bool TWO, bool COUNT_K>
+hipError_t launch_grads(Grad& x, int64_t rows_x, Grad& w, int64_t rows_w, hipStream_t st) {
+  hipError_t e;
+  if (rows_x > 0 && rows_w > 0 && !is_big(rows_x, x.b.rows) && !is_big(rows_w, w.b.rows)) {
+    x.tile = w.tile = 128;
+    const int64_t nx = (int64_t)x.grid.mt * x.grid.nt * x.grid.S, n = nx + (int64_t)w.grid.mt * w.grid.nt * w.grid.S;
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(256), 0, st, x, w, (int)nx); };
+    if (is_deep(n)) go(grad_pair<T, 4, TWO, COUNT_K>);
+    else go(grad_pair<T, 2, TWO, COUNT_K>);
+    return hipGetLastError();
+  }
+  if ((e = launch_grad<T, true, TWO, false>(x, rows_x, st)) != hipSuccess) return e;
+  return launch_grad<T, false, false, COUNT_K>(w, rows_w, st);
 }
 template <class T>
 hipError_t launch_join(const Grad& g, int64_t rows, hipStream_t st) {
