@@ -24,8 +24,15 @@ __device__ __forceinline__ float2 activation(float g, int act) {
     return make_float2(g * s, s * (1.0f + g * (1.0f - s)));
   }
   if (act == ARGUS_GELU) {
-    const float cdf = 0.5f * (1.0f + erff(g * 0.70710678f));
-    return make_float2(g * cdf, cdf + g * 0.39894228f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * g * g));
+    // Phi(-z) = exp(-z^2 / 2) t S(t), t = 1 / (1 + 0.28 z), for z >= 0: the form of
+    // Abramowitz and Stegun 7.1.26, S fitted here to 5e-7 of the value itself, so
+    // that the tail keeps its digits (1 + erf is a difference of ones there).
+    const float e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * g * g), t = __builtin_amdgcn_rcpf(1.0f + 0.28f * fabsf(g));
+    float s = 0.024720103f;
+    for (float c : {-0.09359359f, 0.09242878f, -0.006449664f, 0.0727752f, 0.08363075f, 0.10308467f, 0.111699805f, 0.11170386f})
+      s = fmaf(s, t, c);
+    const float tail = e * t * s, cdf = g < 0.0f ? tail : 1.0f - tail;
+    return make_float2(g * cdf, cdf + g * e * 0.39894228f);
   }
   // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)), y = sqrt(2 / pi) (g + 0.044715 g^3)
   const float s = logistic(1.5957691f * (g + 0.044715f * g * g * g));

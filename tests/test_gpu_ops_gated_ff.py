@@ -28,7 +28,7 @@ def _act(g, act):
         s = torch.sigmoid(g)
         return g * s, s + g * s * (1 - s), 1 + g.abs()
     if act == "gelu":
-        c = torch.special.ndtr(g)
+        c = 0.5 * torch.erfc(-g * math.sqrt(0.5))  # special.ndtr loses its tail
         return g * c, c + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi), 1 + g * g
     s = torch.sigmoid(2 * k * (g + 0.044715 * g**3))
     return g * s, s + g * s * (1 - s) * 2 * k * (1 + 0.134145 * g * g), 1 + 2 * g.abs() + 0.1 * g.abs()**3
@@ -102,18 +102,20 @@ def test_forward(T, W, F, dtype):
     assert list(lean) == ["h"] and torch.equal(lean["h"], got["h"])
 
 
+@pytest.mark.parametrize("dtype", list(UNIT))
 @pytest.mark.parametrize("act", ACTS)
-def test_activations_over_their_range(act):
-    # one element to a sum: g itself goes from far below to far above 0
+def test_activations_over_their_range(act, dtype):
+    # one element to a sum: g itself goes from far below to far above 0, where
+    # bfloat16 still holds the activation's tail
     W = 8
-    x = torch.zeros(2, W, device=DEV, dtype=torch.float16)
+    x = torch.zeros(2, W, device=DEV, dtype=dtype)
     x[:, 0] = 1
     x[:, 1] = torch.tensor([1.0, -2.0])
-    wg, wu = torch.zeros(4000, W, device=DEV, dtype=torch.float16), torch.zeros(4000, W, device=DEV, dtype=torch.float16)
-    wg[:, 0], wu[:, 1] = torch.linspace(-12, 12, 4000, device=DEV).half(), 1.0
+    wg, wu = torch.zeros(4000, W, device=DEV, dtype=dtype), torch.zeros(4000, W, device=DEV, dtype=dtype)
+    wg[:, 0], wu[:, 1] = torch.linspace(-12, 12, 4000, device=DEV).to(dtype), 1.0
     got = pa.gated_ff(x, wg, wu, act, save=True)
     _check_forward(got, x, wg, wu, act)
-    dh = torch.full((2, 4000), 0.5, device=DEV, dtype=torch.float16)
+    dh = torch.full((2, 4000), 0.5, device=DEV, dtype=dtype)
     _check_backward(pa.gated_ff_bwd(dh, x, wg, wu, got["g"], got["u"], act), dh, x, wg, wu, got["g"], got["u"], act)
 
 
