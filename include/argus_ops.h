@@ -271,7 +271,8 @@ int argus_rotary(const argus_rotary_t* p, const void* x, void* out, void* stream
  * products have 32-bit sums, h is made of those and rounded once.
  * Backward, from the rounded g and u: dg = d_h u act'(g), du = d_h act(g),
  * both rounded to dtype as operands; dx = dg wg + du wu, dwg = dg^T x,
- * dwu = du^T x.
+ * dwu = du^T x. A row of x or d_h that holds a NaN or an infinity reaches its own
+ * token's rows and the weights' gradients alone.
  */
 enum { ARGUS_SILU = 0, ARGUS_GELU = 1, ARGUS_GELU_TANH = 2 };
 
@@ -307,7 +308,9 @@ int argus_gated_ff_bwd(const argus_gated_ff_t* p, const void* d_h, const void* x
  * number of tokens that are learned (mean 0 if none). A token whose label is
  * below 0 is not learned; one whose label is at or above n_vocab neither, and
  * raises ARGUS_DEV_TOKEN_RANGE: loss 0, lse -infinity, and no gradient,
- * whatever their rows of x hold. The logits are not kept.
+ * whatever their rows of x hold. The logits are not kept. A NaN among a learned
+ * token's logits, or one of +infinity, makes its lse and loss, and by them the
+ * mean, NaN; one of -infinity counts as an exponential of 0.
  * Backward, with c = dmean / max(n_valid, 1) + dloss[token] for a token that
  * is learned: dz[v] = c scale (exp(z[v] - lse) (1 + 2 z_loss lse) - [v =
  * label]), rounded to bfloat16 as an operand; dx = dz w, dw = dz^T x. n_valid

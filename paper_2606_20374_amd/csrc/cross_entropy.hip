@@ -25,7 +25,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The learned tokens, in order.
 struct Tokens {
   uint32_t* n;     // [2] how many, and a counter of workgroups that are done
-  float* most;     // [1] largest |c| that is finite, 1 if that is 0; backward
+  float* most;     // [1] largest |c| that is finite, 1 where that is next to 0; backward
   int32_t* index;  // [n] token
   int32_t* label;  // [n] forward
   int32_t* place;  // [T] number of a token, -1: not learned; backward
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kIndexThreads) void ce_index(CeArgs a, IndexArgs o)
     if (o.n_valid) *o.n_valid = base;
     if (a.t.most) {
       for (int j = 0; j < kIndexThreads / 64; ++j) top = fmaxf(top, tops[j]);
-      *a.t.most = top > 0.0f ? top : 1.0f;
+      *a.t.most = top > 0x1p-100f ? top : 1.0f;  // one that can be divided by
     }
   }
 }
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256) void ce_rows(CeArgs a, IndexArgs o) {
   if (range && o.status) atomicOr(o.status, ARGUS_DEV_TOKEN_RANGE);
   if (threadIdx.x) return;
   top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  *a.t.most = top > 0.0f ? top : 1.0f;
+  *a.t.most = top > 0x1p-100f ? top : 1.0f;  // one that can be divided by
 }
 
 // A row to a wavefront.

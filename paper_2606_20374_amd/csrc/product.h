@@ -233,9 +233,8 @@ struct Tile {
   static __device__ __forceinline__ int col_of(int b) { return b / HN * (TN / 2) + wave() % WN * (HN * 16) + b % HN * 16; }
 
   // What is loaded together, the same half of A and of B (with four stages both
-  // halves), is an array of its own: the compiler waits before a read for the
-  // loads into its array, and tells seven arrays apart. (With arrays for each half
-  // of A and B it waited for all loads every other step.)
+  // halves), is an array of its own: the compiler, too, waits before a read for
+  // the loads into its array, and tells only a few arrays apart.
   static constexpr int kArrays = 4, kA = TM / 2 * kStep, kB = TN / 2 * kStep;
   static constexpr int kArray = (kA + kB) * (STAGES / 2);
   using Shared = Lds<T, kArray>;

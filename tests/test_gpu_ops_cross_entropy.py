@@ -123,6 +123,39 @@ def test_gradients_of_single_losses():
     _check_backward(got, x, w, labels, f["lse"], dloss.double() - 2.0 / 1000)
 
 
+@pytest.mark.parametrize("T", [12, 140, 1_500])
+@pytest.mark.parametrize("size", [1e-40, 1e-30, 1e30])
+def test_gradients_of_any_size(T, size):
+    # the largest part of the losses' gradient is taken out of the operand
+    x, w, labels = _data(T, 1_000, 64)
+    f = pa.cross_entropy(x, w, labels)
+    dloss = size * torch.rand(T, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    dloss[1] = 0
+    got = pa.cross_entropy_bwd(x, w, labels, f["lse"], dloss=dloss)
+    assert got["dx"].isfinite().all() and got["dw"].isfinite().all() and not got["dx"][1].any()
+    if size > 1e-35:  # below, products of subnormal numbers are 0
+        unit = pa.cross_entropy_bwd(x, w, labels, f["lse"], dloss=dloss / size)
+        for k in ("dx", "dw"):  # the same but for the roundings of c / C, of C and of the output
+            a, b = got[k].double() / size, unit[k].double()
+            assert float((a - b).norm()) <= UNIT * float(b.norm()), k
+
+
+@pytest.mark.parametrize("T", [9, 100, 2_000])
+def test_infinite_logits(T):
+    x, w, labels = _data(T, 600, 64, absent=0.0)
+    w = w.clone()
+    x[3, 5], x[4, 5] = 2.0, -2.0
+    w[7, 5] = math.inf  # +infinity for token 3, -infinity for token 4
+    x[:, 5][torch.arange(T, device=DEV) > 4] = -1.0
+    x[:3, 5] = -1.0
+    labels[labels == 7] = 8
+    got = pa.cross_entropy(x, w, labels)
+    assert got["loss"][3].isnan() and got["mean"].isnan()
+    rest = torch.arange(T, device=DEV) != 3
+    z = x[rest].double() @ w.double().T
+    assert (got["lse"][rest].double() - torch.logsumexp(z, 1)).abs().max() < 1e-4
+
+
 def test_gradient_against_differences():
     x, w, labels = _data(96, 200, 64, absent=0.25)
     f = pa.cross_entropy(x, w, labels, z_loss=1e-2)
