@@ -56,7 +56,7 @@ __device__ __forceinline__ int64_t raw_label(const CeArgs& a, int64_t t) {
 __device__ __forceinline__ int64_t label_of(const CeArgs& a, int64_t row) {
   if (a.t.index) return a.t.label[row];
   const int64_t l = raw_label(a, row);
-  return l < a.V ? l : -1;
+  return l >= 0 && l < a.V ? l : -1;
 }
 
 constexpr int kIndexThreads = 1024, kEach = 8;
@@ -295,7 +295,8 @@ __device__ __forceinline__ void few_weights(const CeArgs& a, int64_t v0, __amdgp
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    w[b] = buffer((const char*)a.w.p + (v0 + 16 * b) * a.w.stride * 2, ((a.V - v0 - 16 * b - 1) * a.w.stride + a.w.k) * 2);
+    const int64_t first = v0 + 16 * b < a.V ? v0 + 16 * b : a.V - 1;  // of a block past the end: dropped
+    w[b] = buffer((const char*)a.w.p + first * a.w.stride * 2, ((a.V - first - 1) * a.w.stride + a.w.k) * 2);
     off[b] = (int)(((lane & 15) * a.w.stride + 8 * (lane >> 4)) * 2);
   }
 }

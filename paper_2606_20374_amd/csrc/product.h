@@ -43,7 +43,8 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16_t) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// Past every buffer's end: reads as zeros.
+// Past every buffer's end: reads as zeros. A lane's offset is compared with what
+// the scalar offset leaves of the buffer, so that one has to lie inside.
 constexpr int kNowhere = 0x7ffffff0;
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int64_t bytes) {
@@ -81,6 +82,7 @@ struct LoadRows {
   __device__ __forceinline__ LoadRows(const Operand& o, int64_t row0, const Operand& p, int64_t row1) {
     const int row = threadIdx.x >> 3;
     at = ((threadIdx.x & 7) ^ ((threadIdx.x >> 4) & 7)) * 8;
+    row1 = row1 < p.rows ? row1 : p.rows - 1;  // a half past the end: of one row, and dropped
     r[0] = buffer((const char*)o.p + row0 * o.stride * 2, ((o.rows - row0 - 1) * o.stride + o.k) * 2);
     r[1] = buffer((const char*)p.p + row1 * p.stride * 2, ((p.rows - row1 - 1) * p.stride + p.k) * 2);
 #pragma unroll
@@ -92,10 +94,10 @@ struct LoadRows {
   // Half of the tile of k = k0 .. k0 + 63, zeros from k_end on.
   template <class T>
   __device__ __forceinline__ void load(int half, int k0, int k_end, T* tile) const {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), from = k0 < k_end ? k0 * 2 : 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      load_lds(r[half], tile + (i * THREADS + wave * 64) * 8, k0 + at < k_end ? off[half][i] : kNowhere, k0 * 2);
+      load_lds(r[half], tile + (i * THREADS + wave * 64) * 8, k0 + at < k_end ? off[half][i] : kNowhere, from);
   }
 };
 
@@ -484,14 +486,14 @@ struct Few {
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int k = k0 + u * kFewWaves * 64 + 32 * h;
+          const int k = k0 + u * kFewWaves * 64 + 32 * h, from = k < K ? k * 2 : 0;
           const bool there = k + at < K;
 #pragma unroll
           for (int b = 0; b < NB; ++b)
-            wf[u][h][b] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(w[b], there ? off[b] : kNowhere, k * 2, 0));
+            wf[u][h][b] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(w[b], there ? off[b] : kNowhere, from, 0));
 #pragma unroll
           for (int t = 0; t < NT; ++t)
-            xf[u][h][t] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(x, there ? xoff[t] : kNowhere, k * 2, 0));
+            xf[u][h][t] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(x, there ? xoff[t] : kNowhere, from, 0));
         }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -572,6 +574,7 @@ __device__ __forceinline__ void grad_body(Grad g, int block) {
       if (count < g.a.k) g.b = g.b1;
       g.a.k = g.b.k = count;
     } else {
+      if (count == 0) return;
       grid = counted(grid, count, TT::TM);
       g.a.rows = count;
     }
