@@ -425,17 +425,20 @@ struct Tile {
   }
 };
 
-// Tile (m, n) of workgroup `at` of mt by nt. Workgroups go to the eight XCDs in
-// turn; each XCD takes a consecutive part of the order, which runs through
-// bands of kBand rows of tiles, so that tiles which share operands are in the
-// same L2 at the same time.
+// Tile (m, n) and part of k of workgroup `at` of S by mt by nt. Workgroups go to
+// the eight XCDs in turn; each XCD takes a consecutive piece of the order, which
+// runs through the parts and in each through bands of kBand rows of tiles, so
+// that tiles which share operands are in the same L2 at the same time.
 constexpr int kBand = 8;
-__device__ __forceinline__ void tile_at(int at, int mt, int nt, int& m, int& n) {
-  const int id = (int)xcd_item(at, (int64_t)mt * nt);
+__device__ __forceinline__ int tile_at(int at, int mt, int nt, int& m, int& n, int S = 1) {
+  int id = (int)xcd_item(at, (int64_t)S * mt * nt);
+  const int part = id / (mt * nt);
+  id -= part * (mt * nt);
   const int band = id / (kBand * nt), in = id - band * (kBand * nt);
   const int high = mt - band * kBand < kBand ? mt - band * kBand : kBand;
   n = in / high;
   m = band * kBand + in - n * high;
+  return part;
 }
 
 // Part s of S of k steps: multiples of kStep.
@@ -480,14 +483,14 @@ struct Few {
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0, 0, 0, 0};
-    for (int k0 = wave * 64; k0 < K; k0 += kFewWaves * 64 * U) {
+    auto round = [&](int k0, auto whole) __attribute__((always_inline)) {
       s16x8 wf[U][2][NB], xf[U][2][NT];
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int k = k0 + u * kFewWaves * 64 + 32 * h, from = k < K ? k * 2 : 0;
-          const bool there = k + at < K;
+          const int k = k0 + u * kFewWaves * 64 + 32 * h, from = whole || k < K ? k * 2 : 0;
+          const bool there = whole || k + at < K;
 #pragma unroll
           for (int b = 0; b < NB; ++b)
             wf[u][h][b] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(w[b], there ? off[b] : kNowhere, from, 0));
@@ -495,6 +498,7 @@ struct Few {
           for (int t = 0; t < NT; ++t)
             xf[u][h][t] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(x, there ? xoff[t] : kNowhere, from, 0));
         }
+      __builtin_amdgcn_sched_barrier(0);  // all loads first
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -503,7 +507,11 @@ struct Few {
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[b][t] = mfma(wf[u][h][b], xf[u][h][t], acc[b][t], T{});
-    }
+    };
+    constexpr int kRound = kFewWaves * 64 * U;
+    int k0 = wave * 64;
+    for (; k0 + kRound - (kFewWaves - 1) * 64 <= K; k0 += kRound) round(k0, std::true_type{});
+    for (; k0 < K; k0 += kRound) round(k0, std::false_type{});
   }
 
   // Sums over the wavefronts, in their order: tokens t are then wavefront t %
@@ -579,10 +587,9 @@ __device__ __forceinline__ void grad_body(Grad g, int block) {
       g.a.rows = count;
     }
   }
-  const int part = block / (grid.mt * grid.nt);
-  if (part >= grid.S) return;
+  if (block >= grid.S * grid.mt * grid.nt) return;
   int m, n, begin, end;
-  tile_at(block - part * (grid.mt * grid.nt), grid.mt, grid.nt, m, n);
+  const int part = tile_at(block, grid.mt, grid.nt, m, n, grid.S);
   const int64_t m0 = (int64_t)m * TT::TM, n0 = (int64_t)n * TT::TN;
   my_part(g.a.k, part, grid.S, begin, end);
   TT t;
