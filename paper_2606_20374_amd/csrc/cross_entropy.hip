@@ -575,12 +575,13 @@ bool is_small(const argus_cross_entropy_t& p) {
 int64_t tiles_n(const argus_cross_entropy_t& p) {
   return ceil_div(p.n_vocab, is_few(p) ? few_ids(p) : is_big(p.n_tokens, p.n_vocab) ? 256 : 128);
 }
-// Ids of a piece: at most 2^27 values of dz where the tokens allow it.
+// Ids of a piece: at most 2^27 values of dz where the tokens allow it, and as
+// many in all pieces as tiles allow.
 int64_t piece_of(const argus_cross_entropy_t& p) {
   int64_t ids = ((int64_t)1 << 27) / (p.n_tokens > 0 ? p.n_tokens : 1) / 256 * 256;
   if (ids < 4096) ids = 4096;
   const int64_t all = ceil_div(p.n_vocab, 64) * 64;
-  return ids < all ? ids : all;
+  return ids < all ? ceil_div(ceil_div(p.n_vocab, ceil_div(p.n_vocab, ids)), 256) * 256 : all;
 }
 
 struct Forward {
@@ -608,7 +609,7 @@ struct Backward {
   bf16_t* dz;
   float *dx, *dw;
   int64_t piece;
-  Grid to_dx;  // of a piece's product
+  Plan plan;  // of a piece
   size_t bytes;
 };
 Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
@@ -616,7 +617,7 @@ Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
   const size_t T = (size_t)p.n_tokens;
   Backward b{};
   b.piece = piece_of(p);
-  b.to_dx = grid_of(p.n_tokens > 0 ? p.n_tokens : 1, p.width, b.piece);
+  b.plan = plan_grads(p.n_tokens > 0 ? p.n_tokens : 1, b.piece, b.piece, p.n_tokens, p.width);
   b.t.n = s.take<uint32_t>(2);
   b.t.most = s.take<float>(1);
   b.t.index = s.take<int32_t>(T);
@@ -624,15 +625,8 @@ Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
   b.t.row = s.take<float4>(T);
   b.t.x = s.take<bf16_t>(T * (size_t)p.width);
   b.dz = s.take<bf16_t>(T * (size_t)b.piece);
-  b.dx = s.take<float>(sums_bytes(b.to_dx, is_big(p.n_tokens, p.width), p.width) / 4);
-  size_t dw = 0;  // the last piece may be in more parts than the others
-  for (int64_t ids : {b.piece < p.n_vocab ? b.piece : (int64_t)p.n_vocab, p.n_vocab % b.piece}) {
-    if (ids == 0) continue;
-    const Grid g = grid_of(ids, p.width, p.n_tokens);
-    const size_t need = g.S > 1 ? sums_bytes(g, is_big(ids, p.width), p.width) : 0;
-    if (need > dw) dw = need;
-  }
-  b.dw = s.take<float>(dw / 4);
+  b.dx = s.take<float>(sums_bytes(b.plan, b.plan.x, p.width) / 4);
+  b.dw = s.take<float>(b.plan.w.S > 1 ? sums_bytes(b.plan, b.plan.w, p.width) / 4 : 0);
   b.bytes = s.at;
   return b;
 }
@@ -724,7 +718,7 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     e = launch_tokens(a, io, true, st);
   }
   if (e != hipSuccess) return e;
-  const bool whole = small && b.piece >= V && b.to_dx.S == 1;  // dx leaves the product as it is
+  const bool whole = small && b.piece >= V && b.plan.x.S == 1;  // dx leaves the product as it is
   Grad g{};
   for (int64_t v0 = 0; v0 < V; v0 += b.piece) {
     const int64_t ids = V - v0 < b.piece ? V - v0 : b.piece, cols = ceil_div(ids, 64) * 64;
@@ -751,7 +745,7 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     g.n = small ? nullptr : b.t.n;
     g.f = b.t.most;
     g.scale = p.scale;
-    g.grid = b.to_dx;
+    g.grid = b.plan.x;
     g.add = v0 > 0;
     if (whole) {
       g.rows = {dx, nullptr, T, T, 0};
@@ -767,9 +761,10 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     d.f = b.t.most;
     d.scale = p.scale;
     d.rows = {(bf16_t*)dw + v0 * W, nullptr, ids, ids, 0};
-    d.grid = grid_of(ids, W, T);
+    d.grid = b.plan.w;
+    d.grid.mt = (int32_t)ceil_div(ids, b.plan.tile());
     d.sums = d.grid.S > 1 ? b.dw : nullptr;
-    if ((e = launch_grads<bf16_t, false, true>(g, T, d, ids, st)) != hipSuccess) return e;
+    if ((e = launch_grads<bf16_t, false, true>(b.plan, g, d, st)) != hipSuccess) return e;
     if (d.sums && (e = launch_join<bf16_t>(d, ids, st)) != hipSuccess) return e;
   }
   if (whole) return hipSuccess;

@@ -144,11 +144,8 @@ __global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, con
 int64_t wide_of(const argus_gated_ff_t& p) { return ceil_div(p.ff, 64) * 64; }
 size_t point_bytes(const argus_gated_ff_t& p) { return align256((size_t)p.n_tokens * 2 * (size_t)wide_of(p) * 2); }
 
-size_t sums_of(const argus_gated_ff_t& p, int64_t rows, int64_t k) {
-  const Grid g = grid_of(rows, p.width, k);
-  return g.S > 1 ? sums_bytes(g, is_big(rows, p.width), p.width) : 0;
-}
-size_t dx_sums(const argus_gated_ff_t& p) { return sums_of(p, p.n_tokens, 2 * wide_of(p)); }
+Plan plan_of(const argus_gated_ff_t& p) { return plan_grads(p.n_tokens, 2 * wide_of(p), 2 * wide_of(p), p.n_tokens, p.width); }
+size_t sums_of(const argus_gated_ff_t& p, const Plan& plan, const Grid& g) { return g.S > 1 ? sums_bytes(plan, g, p.width) : 0; }
 
 template <class T>
 hipError_t forward(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g, void* u,
@@ -175,6 +172,7 @@ template <class T>
 hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, const void* wg, const void* wu, const void* g,
                     const void* u, void* dx, void* dwg, void* dwu, void* ws, hipStream_t st) {
   const int64_t wide = wide_of(p), W = p.width, F = p.ff, N = p.n_tokens;
+  const Plan plan = plan_of(p);
   T* point = (T*)ws;
   float* sums = (float*)((char*)ws + point_bytes(p));
   hipError_t e;
@@ -190,14 +188,14 @@ hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, co
   dinput.b1 = {wu, W, F, p.wu_stride};
   dinput.k1 = wide;
   dinput.rows = {dx, nullptr, N, N, 0};
-  dinput.grid = grid_of(N, W, 2 * wide);
+  dinput.grid = plan.x;
   dinput.sums = dinput.grid.S > 1 ? sums : nullptr;
   dweights.a = {point, 2 * wide, N, 2 * wide};
   dweights.b = {x, W, N, p.x_stride};
   dweights.rows = {dwg, dwu, F, wide, F};
-  dweights.grid = grid_of(2 * wide, W, N);
-  dweights.sums = dweights.grid.S > 1 ? sums + dx_sums(p) / 4 : nullptr;
-  if ((e = launch_grads<T, true, false>(dinput, N, dweights, 2 * wide, st)) != hipSuccess) return e;
+  dweights.grid = plan.w;
+  dweights.sums = dweights.grid.S > 1 ? sums + sums_of(p, plan, plan.x) / 4 : nullptr;
+  if ((e = launch_grads<T, true, false>(plan, dinput, dweights, st)) != hipSuccess) return e;
   if (dinput.sums && (e = launch_join<T>(dinput, N, st)) != hipSuccess) return e;
   return dweights.sums ? launch_join<T>(dweights, wide + F, st) : hipSuccess;
 }
@@ -207,7 +205,8 @@ hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, co
 size_t gated_ff_workspace_bytes(const argus_gated_ff_t&) { return 0; }
 
 size_t gated_ff_bwd_workspace_bytes(const argus_gated_ff_t& p) {
-  return point_bytes(p) + dx_sums(p) + sums_of(p, 2 * wide_of(p), p.n_tokens);
+  const Plan plan = plan_of(p);
+  return point_bytes(p) + sums_of(p, plan, plan.x) + sums_of(p, plan, plan.w);
 }
 
 hipError_t launch_gated_ff(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g,

@@ -20,6 +20,7 @@
 // steps of 32 k, which ask for half lines, 13% (k innermost) and 4%.
 #pragma once
 
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -642,16 +643,14 @@ __device__ __forceinline__ void grad_body(Grad g, int block) {
   }
 }
 
-template <class TT, bool TWO, bool COUNT_K>
-__global__ __launch_bounds__(TT::THREADS) void grad_kernel(Grad g) {
-  grad_body<TT, TWO, COUNT_K>(g, blockIdx.x);
-}
-// Both gradients of an operator that have few tiles: the input's (A with k
-// innermost) first, then the weights'.
-template <class T, int STAGES, bool TWO, bool COUNT_K>
-__global__ __launch_bounds__(256) void grad_pair(Grad x, Grad w, int blocks_x) {
-  if ((int)blockIdx.x < blocks_x) grad_body<Tile<T, 128, 128, 2, 2, true, false, STAGES>, TWO, false>(x, blockIdx.x);
-  else grad_body<Tile<T, 128, 128, 2, 2, false, false, STAGES>, false, COUNT_K>(w, blockIdx.x - blocks_x);
+// Both gradients of an operator: the input's (tiles X, A with k innermost) and
+// the weights' (tiles W). The longer workgroups, `first` of them, go first.
+template <class X, class W, bool TWO, bool COUNT_K>
+__global__ __launch_bounds__(X::THREADS) void grad_pair(Grad x, Grad w, int first, int w_first) {
+  const bool of_w = ((int)blockIdx.x < first) == (w_first != 0);
+  const int block = (int)blockIdx.x < first ? blockIdx.x : blockIdx.x - first;
+  if (of_w) grad_body<W, false, COUNT_K>(w, block);
+  else grad_body<X, TWO, false>(x, block);
 }
 
 // Sum of the S parts, in their order, of eight columns.
@@ -711,52 +710,89 @@ auto with_tile(int64_t rows, int64_t cols, F go) {
   return is_deep(ceil_div(rows, 64) * ceil_div(cols, 128)) ? go(Short<T, 4>{}) : go(Short<T>{});
 }
 
-// Parts of k where the tiles alone do not fill the chip: at least kPart of k in each.
-constexpr int64_t kPart = 512;
-inline int32_t parts_of(int64_t rows, int64_t cols, int64_t k) {
-  if (rows <= 0 || is_big(rows, cols)) return 1;
-  const int64_t want = 2 * kCus / tiles_of(rows, cols, false), most = k / kPart;
-  const int64_t s = want < most ? want : most;
-  return s < 1 ? 1 : s > 64 ? 64 : (int32_t)s;
-}
-inline Grid grid_of(int64_t rows, int64_t cols, int64_t k) {
-  const int t = is_big(rows, cols) ? 256 : 128;
-  const int64_t most = k / kPart < 64 ? k / kPart : 64;
-  return {(int32_t)ceil_div(rows, t), (int32_t)ceil_div(cols, t), parts_of(rows, cols, k), most < 1 ? 1 : (int32_t)most};
-}
-// 32-bit sums of a product, where it is taken in parts.
-inline size_t sums_bytes(const Grid& g, bool big, int64_t cols) {
-  return align256((size_t)g.S * (size_t)g.mt * (big ? 256 : 128) * (size_t)cols * 4);
+// How the two gradients of an operator are taken: tiles and parts of k. Their
+// workgroups share the chip, so that the parts of one fill what the tiles of the
+// other leave.
+struct Plan {
+  bool big, deep, w_first;
+  Grid x, w;  // no sums where S is 1
+  int tile() const { return big ? 256 : 128; }
+};
+constexpr int64_t kPart = 512;  // k of a part, at least
+constexpr int kMostParts = 64;
+
+// The time that n1 workgroups of a1 and then n2 of a2 take on `slots` places.
+inline float time_of(float n1, float a1, float n2, float a2, float slots) {
+  const float rounds = floorf(n1 / slots), late = n1 - rounds * slots, t0 = rounds * a1, t1 = t0 + a1;
+  if (n2 <= 0) return late > 0 ? t1 : t0;
+  float j = floorf(((n1 * a1 + n2 * a2) / slots - t0) / a2), m;
+  do {
+    m = t0 + j * a2;
+    j += 1;
+  } while ((slots - late) * (j - 1) + late * fmaxf(0.0f, floorf((m - t1) / a2 + 1e-3f)) < n2);
+  return late > 0 ? fmaxf(m, t1) : m;
 }
 
-// One gradient product of `rows` rows, g.grid of grid_of (without sums: in one part).
-template <class T, bool ROWS_A, bool TWO, bool COUNT_K>
-hipError_t launch_grad(Grad& g, int64_t rows, hipStream_t st) {
-  auto go = [&](auto tile) {
-    using TT = decltype(tile);
-    g.tile = TT::TM;
-    hipLaunchKernelGGL((grad_kernel<TT, TWO, COUNT_K>), dim3((unsigned)(g.grid.mt * g.grid.nt * g.grid.S)),
-                       dim3(TT::THREADS), 0, st, g);
+inline Plan plan_grads(int64_t rows_x, int64_t k_x, int64_t rows_w, int64_t k_w, int64_t cols) {
+  // Microseconds of a step of 64 k, and of a workgroup's start and end, which
+  // writes 16 bits a value, or 32 for parts: measured as they are in rounds of
+  // workgroups that fill the chip.
+  struct Kind {
+    int tile, slots;
+    float step, ends, ends_sums;
+  };
+  constexpr Kind kinds[3] = {{256, kCus, 1.4f, 8.0f, 14.0f}, {128, 2 * kCus, 1.05f, 4.0f, 6.0f}, {128, kCus, 0.62f, 3.0f, 4.0f}};
+  constexpr int cuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  const float steps_x = (float)ceil_div(k_x, kStep), steps_w = (float)ceil_div(k_w, kStep);
+  const int most_x = (int)(k_x / kPart < 1 ? 1 : k_x / kPart < kMostParts ? k_x / kPart : kMostParts);
+  const int most_w = (int)(k_w / kPart < 1 ? 1 : k_w / kPart < kMostParts ? k_w / kPart : kMostParts);
+  const float longest = steps_x > steps_w ? steps_x : steps_w;
+  Plan best{};
+  float least = 0;
+  for (const Kind& kind : kinds) {
+    const int64_t mx = ceil_div(rows_x, kind.tile), mw = ceil_div(rows_w, kind.tile), n = ceil_div(cols, kind.tile);
+    int was_x = 0, was_w = 0;
+    for (int cut : cuts) {
+      const float length = longest / (float)cut;
+      const int sx = (int)fminf((float)most_x, fmaxf(1.0f, roundf(steps_x / length)));
+      const int sw = (int)fminf((float)most_w, fmaxf(1.0f, roundf(steps_w / length)));
+      if (sx == was_x && sw == was_w) continue;
+      was_x = sx;
+      was_w = sw;
+      const float nx = (float)(mx * n * sx), nw = (float)(mw * n * sw);
+      if (kind.tile == 128 && kind.slots == kCus && nx + nw > kCus) break;
+      const float ax = ceilf(steps_x / sx) * kind.step + (sx > 1 ? kind.ends_sums : kind.ends);
+      const float aw = ceilf(steps_w / sw) * kind.step + (sw > 1 ? kind.ends_sums : kind.ends);
+      float t = aw > ax ? time_of(nw, aw, nx, ax, kind.slots) : time_of(nx, ax, nw, aw, kind.slots);
+      // sums are read again, at 5 TB/s
+      if (sx > 1) t += 4.0f + (float)sx * (float)(rows_x * cols) * 4e-6f / 5.0f;
+      if (sw > 1) t += 4.0f + (float)sw * (float)(rows_w * cols) * 4e-6f / 5.0f;
+      if (least > 0 && t >= least) continue;
+      least = t;
+      best = {kind.tile == 256, kind.tile == 128 && kind.slots == kCus, aw > ax,
+              {(int32_t)mx, (int32_t)n, sx, most_x}, {(int32_t)mw, (int32_t)n, sw, most_w}};
+    }
+  }
+  return best;
+}
+// 32-bit sums of a product.
+inline size_t sums_bytes(const Plan& p, const Grid& g, int64_t cols) {
+  return align256((size_t)g.S * (size_t)g.mt * (size_t)p.tile() * (size_t)cols * 4);
+}
+
+// The gradients of an operator's input and of its weights, of a plan's grids.
+template <class T, bool TWO, bool COUNT_K>
+hipError_t launch_grads(const Plan& p, Grad& x, Grad& w, hipStream_t st) {
+  x.tile = w.tile = p.tile();
+  const int nx = x.grid.mt * x.grid.nt * x.grid.S, nw = w.grid.mt * w.grid.nt * w.grid.S;
+  auto go = [&](auto tx, auto tw) {
+    using X = decltype(tx);
+    hipLaunchKernelGGL((grad_pair<X, decltype(tw), TWO, COUNT_K>), dim3((unsigned)(nx + nw)), dim3(X::THREADS), 0, st, x, w,
+                       p.w_first ? nw : nx, (int)p.w_first);
     return hipGetLastError();
   };
-  if (rows <= 0 || g.b.rows <= 0) return hipSuccess;
-  if (is_big(rows, g.b.rows)) return go(Big<T, ROWS_A, false>{});
-  return is_deep((int64_t)g.grid.mt * g.grid.nt * g.grid.S) ? go(Small<T, ROWS_A, false, 4>{}) : go(Small<T, ROWS_A, false>{});
-}
-// The gradients of an operator's input (rows_x rows) and of its weights.
-template <class T, bool TWO, bool COUNT_K>
-hipError_t launch_grads(Grad& x, int64_t rows_x, Grad& w, int64_t rows_w, hipStream_t st) {
-  hipError_t e;
-  if (rows_x > 0 && rows_w > 0 && !is_big(rows_x, x.b.rows) && !is_big(rows_w, w.b.rows)) {
-    x.tile = w.tile = 128;
-    const int64_t nx = (int64_t)x.grid.mt * x.grid.nt * x.grid.S, n = nx + (int64_t)w.grid.mt * w.grid.nt * w.grid.S;
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(256), 0, st, x, w, (int)nx); };
-    if (is_deep(n)) go(grad_pair<T, 4, TWO, COUNT_K>);
-    else go(grad_pair<T, 2, TWO, COUNT_K>);
-    return hipGetLastError();
-  }
-  if ((e = launch_grad<T, true, TWO, false>(x, rows_x, st)) != hipSuccess) return e;
-  return launch_grad<T, false, false, COUNT_K>(w, rows_w, st);
+  if (p.big) return go(Big<T, true, false>{}, Big<T, false, false>{});
+  return p.deep ? go(Small<T, true, false, 4>{}, Small<T, false, false, 4>{}) : go(Small<T, true, false>{}, Small<T, false, false>{});
 }
 template <class T>
 hipError_t launch_join(const Grad& g, int64_t rows, hipStream_t st) {
