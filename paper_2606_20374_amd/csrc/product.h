@@ -683,31 +683,62 @@ template <class T, bool ROWS_A, bool ROWS_B>
 using Big = Tile<T, 256, 256, 2, 4, ROWS_A, ROWS_B>;
 template <class T, bool ROWS_A, bool ROWS_B, int STAGES = 2>
 using Small = Tile<T, 128, 128, 2, 2, ROWS_A, ROWS_B, STAGES>;
+// Both operands with k innermost:
+template <class T>
+using Wide = Tile<T, 128, 256, 2, 4, true, true>;
+template <class T>
+using Middle = Tile<T, 192, 128, 2, 2, true, true>;
 template <class T, int STAGES = 2>
-using Short = Tile<T, 64, 128, 2, 2, true, true, STAGES>;  // both operands with k innermost
+using Short = Tile<T, 64, 128, 2, 2, true, true, STAGES>;
 
-// Tiles of 256 x 256 need a CU's LDS each; of 128 x 128 two fit.
+// Tiles of a forward product, by the time that their workgroups take. A CU holds
+// `each` of them; where it has fewer, a step is shorter. Feed-forward (tokens,
+// width, inner width), big, wide, middle, small and short tiles, us: 100 x 2,048 x
+// 8,192 43, 34, 29, 26, 22; 300 x 2,048 x 8,192 46, 33, 32, 38, 42; 500 x 4,096 x 5,120
+// 80, 60, 53, 70, 76; 1,000 x 1,000 x 2,720 29, 20, 25, 23, 25; 4,000 x 4,096 x 5,120 271,
+// 281, 291, 310, 407.
 constexpr int kCus = 256;
-inline bool is_big(int64_t rows, int64_t cols) {
-  return rows > 128 && cols > 128 && ceil_div(rows, 256) * ceil_div(cols, 256) >= kCus * 3 / 4;
+enum Kind { kBig, kWide, kMiddle, kSmall, kShort };
+struct KindCost {
+  int tm, tn, each;
+  float step[3], ends[2], once;  // us a step with 1, 2, 3 on a CU, a workgroup's ends, and once
+};
+// LOSS: the cross entropy's, whose tiles take longer to end; big, small and short
+// ones only.
+template <bool LOSS>
+Kind kind_of(int64_t rows, int64_t cols, int64_t k) {
+  constexpr KindCost costs[] = {{256, 256, 1, {1.18f, 0, 0}, {8.5f, 11.0f}, 0},
+                                {128, 256, 1, {0.87f, 0, 0}, {6.0f, 0}, 0},
+                                {192, 128, 2, {0.69f, 1.25f, 0}, {4.0f, 0}, 4.0f},
+                                {128, 128, 2, {0.72f, 1.05f, 0}, {1.0f, 3.5f}, 3.0f},
+                                {64, 128, 3, {0.55f, 0.85f, 1.13f}, {0.0f, 2.0f}, 3.0f}};
+  const float steps = (float)ceil_div(k, kStep);
+  Kind best = kBig;
+  float least = 0;
+  for (int i = 0; i < 5; ++i) {
+    if (LOSS && (i == kWide || i == kMiddle)) continue;
+    const KindCost& c = costs[i];
+    const int64_t n = ceil_div(rows, c.tm) * ceil_div(cols, c.tn), rounds = n / (c.each * kCus), rest = n - rounds * c.each * kCus;
+    float t = c.once + (float)rounds * (steps * c.step[c.each - 1] + c.ends[LOSS]);
+    if (rest) t += steps * c.step[ceil_div(rest, kCus) - 1] + c.ends[LOSS];
+    if (i > 0 && t >= least) continue;
+    least = t;
+    best = (Kind)i;
+  }
+  return best;
 }
-inline int64_t tiles_of(int64_t rows, int64_t cols, bool big) {
-  const int t = big ? 256 : 128;
-  return ceil_div(rows, t) * ceil_div(cols, t);
-}
-// Forward products of so few tiles that not every CU has one of 128 x 128: more
-// and shorter ones, three to a CU. Feed-forward of 100 tokens, 2,048 wide with
-// 8,192 inside (128 tiles): 24.5 us for 28.1; 5,120 with 2,048: 35 for 47; with 256
-// tiles 28.6 for 29.4; with 384 tiles 39.0 for 37.4.
-inline bool is_short(int64_t rows, int64_t cols) { return tiles_of(rows, cols, false) <= kCus; }
-// A CU with a single workgroup waits for its loads: four stages in place of two.
-inline bool is_deep(int64_t workgroups) { return workgroups <= kCus; }
-// Calls go with the tile for a forward product.
-template <class T, class F>
-auto with_tile(int64_t rows, int64_t cols, F go) {
-  if (is_big(rows, cols)) return go(Big<T, true, true>{});
-  if (!is_short(rows, cols)) return go(Small<T, true, true>{});
-  return is_deep(ceil_div(rows, 64) * ceil_div(cols, 128)) ? go(Short<T, 4>{}) : go(Short<T>{});
+// Calls go with the tile of a kind.
+template <class T, bool LOSS, class F>
+auto with_tile(int64_t rows, int64_t cols, int64_t k, F go) {
+  const Kind kind = kind_of<LOSS>(rows, cols, k);
+  if (kind == kBig) return go(Big<T, true, true>{});
+  if constexpr (!LOSS) {
+    if (kind == kWide) return go(Wide<T>{});
+    if (kind == kMiddle) return go(Middle<T>{});
+  }
+  if (kind == kSmall) return go(Small<T, true, true>{});
+  // one to a CU waits for its loads: four stages in place of two
+  return ceil_div(rows, 64) * ceil_div(cols, 128) <= kCus ? go(Short<T, 4>{}) : go(Short<T>{});
 }
 
 // How the two gradients of an operator are taken: tiles and parts of k. Their
@@ -737,11 +768,11 @@ inline Plan plan_grads(int64_t rows_x, int64_t k_x, int64_t rows_w, int64_t k_w,
   // Microseconds of a step of 64 k, and of a workgroup's start and end, which
   // writes 16 bits a value, or 32 for parts: measured as they are in rounds of
   // workgroups that fill the chip.
-  struct Kind {
+  struct How {
     int tile, slots;
     float step, ends, ends_sums;
   };
-  constexpr Kind kinds[3] = {{256, kCus, 1.4f, 8.0f, 14.0f}, {128, 2 * kCus, 1.05f, 4.0f, 6.0f}, {128, kCus, 0.62f, 3.0f, 4.0f}};
+  constexpr How hows[3] = {{256, kCus, 1.4f, 8.0f, 14.0f}, {128, 2 * kCus, 1.05f, 4.0f, 6.0f}, {128, kCus, 0.62f, 3.0f, 4.0f}};
   constexpr int cuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   const float steps_x = (float)ceil_div(k_x, kStep), steps_w = (float)ceil_div(k_w, kStep);
   const int most_x = (int)(k_x / kPart < 1 ? 1 : k_x / kPart < kMostParts ? k_x / kPart : kMostParts);
@@ -749,7 +780,7 @@ inline Plan plan_grads(int64_t rows_x, int64_t k_x, int64_t rows_w, int64_t k_w,
   const float longest = steps_x > steps_w ? steps_x : steps_w;
   Plan best{};
   float least = 0;
-  for (const Kind& kind : kinds) {
+  for (const How& kind : hows) {
     const int64_t mx = ceil_div(rows_x, kind.tile), mw = ceil_div(rows_w, kind.tile), n = ceil_div(cols, kind.tile);
     int was_x = 0, was_w = 0;
     for (int cut : cuts) {

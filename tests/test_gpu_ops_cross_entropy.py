@@ -87,7 +87,7 @@ def _check_backward(got, x, w, labels, lse, c, scale=1.0, z_loss=0.0):
 
 SIZES = [(1, 1, 8), (1, 50_257, 64), (3, 5, 16), (2, 1_000, 4_096), (16, 300, 72), (17, 129, 40), (33, 2_000, 104), (64, 64, 32),
          (65, 8_000, 512), (130, 127, 264), (200, 1_031, 1_000), (500, 4_099, 136), (1_025, 260, 24)]
-LARGE = [(3_130, 4_011, 72), (6_200, 2_100, 40)]  # tiles of 256 x 256
+LARGE = [(3_130, 4_011, 72), (6_200, 2_100, 40)]  # more workgroups than CUs
 
 
 @pytest.mark.parametrize("T,V,W", SIZES + LARGE)
@@ -99,7 +99,7 @@ def test_forward(T, V, W):
         assert int(got["dev_status"]) == 0
 
 
-# the last: several pieces of the vocabulary, and each product on large tiles
+# the last: a wide one, and several pieces of the vocabulary
 @pytest.mark.parametrize("T,V,W", SIZES + LARGE + [(4_090, 4_011, 3_208), (4_100, 40_003, 64)])
 def test_backward(T, V, W):
     scale, z_loss = (0.7, 1e-3) if T % 2 else (1.0, 0.0)
@@ -109,6 +109,20 @@ def test_backward(T, V, W):
     got = pa.cross_entropy_bwd(x, w, labels, f["lse"], f["n_valid"], dmean=dmean, scale=scale, z_loss=z_loss)
     n = max(1, int(f["n_valid"]))
     _check_backward(got, x, w, labels, f["lse"], torch.full((T,), float(dmean) / n, dtype=torch.float64, device=DEV), scale, z_loss)
+
+
+# tiles of 128 x 128 and 256 x 256, parts of both products, pieces of the
+# vocabulary with parts, few of many tokens learned
+@pytest.mark.parametrize("T,V,W,absent", [(450, 7_777, 1_096, 0.1), (3_000, 4_100, 520, 0.1), (1_501, 20_011, 520, 0.5),
+                                          (1_501, 20_011, 520, 0.97), (1_300, 8_100, 1_000, 0.93), (2_100, 70_001, 72, 0.8),
+                                          (30_011, 300, 136, 0.3), (5_000, 60_001, 264, 0.6)])
+def test_tiles_parts_and_pieces(T, V, W, absent):
+    x, w, labels = _data(T, V, W, absent=absent, pad=8)
+    f = pa.cross_entropy(x, w, labels, z_loss=1e-3)
+    _check_forward(f, x, w, labels, 1.0, 1e-3)
+    got = pa.cross_entropy_bwd(x, w, labels, f["lse"], f["n_valid"], dmean=torch.ones(1, device=DEV), z_loss=1e-3)
+    n = int(f["n_valid"])
+    _check_backward(got, x, w, labels, f["lse"], torch.full((T,), 1 / n, dtype=torch.float64, device=DEV), 1.0, 1e-3)
 
 
 def test_gradients_of_single_losses():

@@ -88,7 +88,7 @@ def _check_backward(got, dh, x, wg, wu, g, u, act):
 # one token to several tiles of each size; widths below, at and past a tile's k
 SIZES = [(1, 8, 8), (1, 4096, 1000), (2, 64, 72), (4, 1024, 512), (15, 40, 136), (16, 256, 64), (17, 96, 264), (33, 104, 128),
          (64, 512, 320), (65, 32, 8), (127, 24, 248), (128, 72, 64), (130, 1000, 200), (257, 520, 392), (999, 1000, 344)]
-LARGE = [(3_130, 72, 2_056), (6_300, 136, 1_000)]  # tiles of 256 x 256 forward
+LARGE = [(3_130, 72, 2_056), (6_300, 136, 1_000)]  # more workgroups than CUs
 
 
 @pytest.mark.parametrize("dtype", list(UNIT))
@@ -127,6 +127,18 @@ def test_backward(T, W, F, dtype):
     f = pa.gated_ff(x, wg, wu, act, save=True)
     got = pa.gated_ff_bwd(dh, x, wg, wu, f["g"], f["u"], act)
     _check_backward(got, dh, x, wg, wu, f["g"], f["u"], act)
+
+
+# forward: tiles of 192 x 128, 128 x 256, 128 x 128 and 256 x 256; backward: the
+# input's gradient in parts, the weights', both; large tiles and small ones
+@pytest.mark.parametrize("T,W,F", [(500, 1000, 5_112), (201, 1000, 12_000), (6_300, 136, 1_000), (1_001, 520, 8_000), (999, 1000, 2_720),
+                                   (2_000, 264, 5_000), (20_011, 136, 200), (10_000, 512, 1_000)])
+def test_tiles_and_parts(T, W, F):
+    x, wg, wu, dh = _data(T, W, F, torch.bfloat16, 8)
+    f = pa.gated_ff(x, wg, wu, "gelu", save=True)
+    _check_forward(f, x, wg, wu, "gelu")
+    got = pa.gated_ff_bwd(dh, x, wg, wu, f["g"], f["u"], "gelu")
+    _check_backward(got, dh, x, wg, wu, f["g"], f["u"], "gelu")
 
 
 @pytest.mark.parametrize("T", [7, 200, 3_130])
