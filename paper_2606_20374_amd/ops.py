@@ -426,13 +426,15 @@ def _turned(t: torch.Tensor, what: str):
     """(address, token stride, head stride) of a [tokens, heads, dim] tensor."""
     if not (t.is_cuda and t.dim() == 3):
         raise AssertionError("libargus takes [tokens, heads, dim] device tensors")
-    if t.stride(2) != 1 and t.shape[2] > 1:
+    (n, h, d), (tok, head, inner) = t.shape, t.stride()
+    if inner != 1 and d > 1:
         raise AssertionError(f"{what}: the last dimension has to be contiguous")
-    n, h, d = t.shape
-    return t.data_ptr(), t.stride(0) if n > 1 else h * d, t.stride(1) if h > 1 else d
+    return t.data_ptr(), tok if n > 1 else h * d, head if h > 1 else d
 
 
 def _rotary(x, freq, pos, interleaved, scale, inverse, out, name):
+    if x.dim() != 3:
+        raise AssertionError("libargus takes [tokens, heads, dim] device tensors")
     n, heads, dim = x.shape
     if freq.dtype != torch.float64 or freq.dim() != 1:
         raise ArgusError("rotary: frequencies are float64 [rot_dim / 2]")
@@ -440,11 +442,17 @@ def _rotary(x, freq, pos, interleaved, scale, inverse, out, name):
         raise ArgusError(f"rotary: positions of {pos.dtype}: int32 or int64 expected")
     if pos is not None:
         _need(pos, (n,), pos.dtype, "rotary: pos")
-    _need(out, x.shape, x.dtype, "rotary: " + name)
-    (xa, xt, xh), (oa, ot, oh) = _turned(x, "x"), _turned(out, name)
+    xa, xt, xh = _turned(x, "x")
+    if out is None:
+        out = {name: x.new_empty((n, heads, dim))}
+        oa, ot, oh = out[name].data_ptr(), heads * dim, dim
+    else:
+        _need(out[name], x.shape, x.dtype, "rotary: " + name)
+        oa, ot, oh = _turned(out[name], name)
     p = Rotary(n, heads, dim, 2 * freq.numel(), int(bool(interleaved)), int(inverse), _dtype(x), scale,
                int(pos is not None and pos.dtype == torch.int64), _ptr(pos), _ptr(freq), xt, xh, ot, oh)
     _call("argus_rotary", x.device, ctypes.byref(p), xa, oa)
+    return out
 
 
 def rotary(x: torch.Tensor, freq: torch.Tensor, pos: Optional[torch.Tensor] = None, interleaved: bool = False,
@@ -452,19 +460,13 @@ def rotary(x: torch.Tensor, freq: torch.Tensor, pos: Optional[torch.Tensor] = No
     """argus_rotary: the first 2 len(freq) elements of each head of x [tokens,
     heads, dim] turned by the token's position (int32 or int64; none: 0, 1,
     ..). freq and scale: of rotary_freq. out={"out": x} turns x in place."""
-    if out is None:
-        out = {"out": _empty(x.shape, x.dtype, x.device)}
-    _rotary(x, freq, pos, interleaved, scale, False, out["out"], "out")
-    return out
+    return _rotary(x, freq, pos, interleaved, scale, False, out, "out")
 
 
 def rotary_bwd(dout: torch.Tensor, freq: torch.Tensor, pos: Optional[torch.Tensor] = None, interleaved: bool = False,
                scale: float = 1.0, out: Optional[dict] = None) -> dict:
     """argus_rotary with inverse set: dx of rotary's x from dout."""
-    if out is None:
-        out = {"dx": _empty(dout.shape, dout.dtype, dout.device)}
-    _rotary(dout, freq, pos, interleaved, scale, True, out["dx"], "dx")
-    return out
+    return _rotary(dout, freq, pos, interleaved, scale, True, out, "dx")
 
 
 # ------------------------------------------------------------------- gated_ff
@@ -486,11 +488,13 @@ def gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "si
     """argus_gated_ff: h = act(x wg^T) (x wu^T) of x [tokens, width] and
     weights [ff, width], bfloat16 or float16; with save, g and u for the
     backward pass. act: silu, gelu or gelu_tanh."""
-    if out is None:
-        out = alloc_gated_ff(x.shape[0], wg.shape[0], x.dtype, save, x.device)
     p, xa, ga, ua = _gated_ff(x, wg, wu, act)
-    for f in ("h", "g", "u") if save else ("h",):
-        _need(out[f], (x.shape[0], wg.shape[0]), x.dtype, "gated_ff: " + f)
+    names, shape = ("h", "g", "u") if save else ("h",), (x.shape[0], wg.shape[0])
+    if out is None:
+        out = {f: x.new_empty(shape) for f in names}
+    else:
+        for f in names:
+            _need(out[f], shape, x.dtype, "gated_ff: " + f)
     need = _lib().argus_gated_ff_workspace(ctypes.byref(p))
     ws = _space(out, need, x.device) if need else None
     _call("argus_gated_ff", x.device, ctypes.byref(p), xa, ga, ua, _ptr(out["h"]), _ptr(out["g"]) if save else None,
@@ -534,9 +538,11 @@ def _cross_entropy(x, w, labels, scale, z_loss):
 
 
 def alloc_cross_entropy(n_tokens: int, device="cuda") -> dict:
-    loss, lse, mean = _empty(2 * n_tokens + 1, torch.float32, device).split([n_tokens, n_tokens, 1])
-    n_valid, status = _empty(2, torch.int32, device).split([1, 1])
-    return {"loss": loss, "lse": lse, "mean": mean, "n_valid": n_valid, "dev_status": status}
+    # one tensor: small calls take as long as their allocations
+    all_of = _empty(2 * n_tokens + 3, torch.float32, device)
+    loss, lse, mean, n_valid, status = torch.split_with_sizes(all_of, (n_tokens, n_tokens, 1, 1, 1))
+    return {"loss": loss, "lse": lse, "mean": mean, "n_valid": n_valid.view(torch.int32),
+            "dev_status": status.view(torch.int32)}
 
 
 def cross_entropy(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, scale: float = 1.0, z_loss: float = 0.0,
@@ -546,13 +552,15 @@ def cross_entropy(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, scale:
     label below 0 leaves a token out; one past the vocabulary too, and raises
     DEV_TOKEN_RANGE in dev_status."""
     n = x.shape[0]
+    p, xa, wa = _cross_entropy(x, w, labels, scale, z_loss)
     if out is None:
         out = alloc_cross_entropy(n, x.device)
-    p, xa, wa = _cross_entropy(x, w, labels, scale, z_loss)
-    for f, shape, dt in (("loss", (n,), torch.float32), ("lse", (n,), torch.float32), ("mean", (1,), torch.float32),
-                         ("n_valid", (1,), torch.int32)):
-        _need(out[f], shape, dt, "cross_entropy: " + f)
-    o = CrossEntropyOut(*[_ptr(out.get(f)) for f in CROSS_ENTROPY_FIELDS])
+        o = CrossEntropyOut(*[t.data_ptr() for t in out.values()])
+    else:
+        for f, shape, dt in (("loss", (n,), torch.float32), ("lse", (n,), torch.float32), ("mean", (1,), torch.float32),
+                             ("n_valid", (1,), torch.int32)):
+            _need(out[f], shape, dt, "cross_entropy: " + f)
+        o = CrossEntropyOut(*[_ptr(out.get(f)) for f in CROSS_ENTROPY_FIELDS])
     ws = _space(out, _lib().argus_cross_entropy_workspace(ctypes.byref(p)), x.device)
     _call("argus_cross_entropy", x.device, ctypes.byref(p), xa, wa, ctypes.byref(o), _ptr(ws), ws.numel())
     return out
