@@ -9,6 +9,8 @@
 // half), whatever the alignment, and writes past the caches. 65,536 tokens, 40
 // heads of 128, bf16: 253 us, 5.3 TB/s (an element to a thread: 597); 20,011
 // tokens, 24 heads of 96 of which 32 turn, f16: 48 us, 3.8 TB/s.
+#include <type_traits>
+
 #include "ops_internal.h"
 
 namespace argus {
@@ -16,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTurns = 2048;   // sines and cosines that fit a workgroup's LDS
-constexpr int kItems = 1024;   // pieces that a workgroup takes where there are enough tokens
+constexpr int kItems = 512;    // pieces that a workgroup takes where there are enough tokens
 constexpr int kGroups = 1024;  // workgroups below which it takes fewer
 constexpr int64_t kMaxGrid = 1 << 20;
 
@@ -29,22 +31,16 @@ struct RotaryArgs {
   float scale, sign;
 };
 
-template <typename T>
-constexpr int kVec = 16 / sizeof(T);
+// Pieces of N elements of a head: of what is turned, then of what is copied.
+template <int N, bool NEIGHBOURS>
+__host__ __device__ __forceinline__ int turned_pieces(int pairs) { return ((NEIGHBOURS ? 2 * pairs : pairs) + N - 1) / N; }
+template <int N>
+__host__ __device__ __forceinline__ int copied_pieces(int rest) { return (rest + N - 1) / N; }
 
-// Pieces of a head: of what is turned, then of what is copied.
-template <typename T, bool NEIGHBOURS>
-__host__ __device__ __forceinline__ int turned_pieces(int pairs) {
-  return ((NEIGHBOURS ? 2 * pairs : pairs) + kVec<T> - 1) / kVec<T>;
-}
-template <typename T>
-__host__ __device__ __forceinline__ int copied_pieces(int rest) { return (rest + kVec<T> - 1) / kVec<T>; }
-
-template <typename T, bool NEIGHBOURS>
+template <typename T, int N, bool NEIGHBOURS>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
   __shared__ __align__(16) float2 turn[kTurns];
-  constexpr int N = kVec<T>;
-  const int turned = turned_pieces<T, NEIGHBOURS>(a.pairs), per = turned + copied_pieces<T>(a.dim - 2 * a.pairs);
+  const int turned = turned_pieces<N, NEIGHBOURS>(a.pairs), per = turned + copied_pieces<N>(a.dim - 2 * a.pairs);
   for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < a.n_tokens; t0 += (int64_t)gridDim.x * a.tokens) {
     const int n = (int)(a.n_tokens - t0 < a.tokens ? a.n_tokens - t0 : a.tokens);
     for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
@@ -107,17 +103,29 @@ hipError_t launch_rotary(const argus_rotary_t& p, const void* x, void* out, hipS
                p.n_heads, p.head_dim, p.rot_dim / 2, p.pos_64, 1, p.scale, p.inverse ? -1.0f : 1.0f};
   return with_dtype(p.dtype, [&](auto t) {
     using T = decltype(t);
-    const int turned = p.interleaved ? turned_pieces<T, true>(a.pairs) : turned_pieces<T, false>(a.pairs);
-    const int64_t pieces = (int64_t)p.n_heads * (turned + copied_pieces<T>(p.head_dim - p.rot_dim));
-    int64_t tokens = ceil_div(kItems, pieces);
-    if (tokens > kTurns / a.pairs) tokens = kTurns / a.pairs;
-    if (tokens > ceil_div(p.n_tokens, kGroups)) tokens = ceil_div(p.n_tokens, kGroups);
-    a.tokens = (int32_t)tokens;
-    const int64_t need = ceil_div(p.n_tokens, tokens);
-    const dim3 grid((unsigned)(need < kMaxGrid ? need : kMaxGrid));
-    if (p.interleaved) hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(kThreads), 0, st, a);
-    return hipGetLastError();
+    constexpr int kWide = 16 / sizeof(T);
+    auto go = [&](auto n, auto neighbours) {
+      constexpr int N = n;
+      constexpr bool NEIGHBOURS = neighbours;
+      const int64_t pieces = (int64_t)p.n_heads * (turned_pieces<N, NEIGHBOURS>(a.pairs) + copied_pieces<N>(p.head_dim - p.rot_dim));
+      int64_t tokens = ceil_div(kItems, pieces);
+      if (tokens > kTurns / a.pairs) tokens = kTurns / a.pairs;
+      if (tokens > ceil_div(p.n_tokens, kGroups)) tokens = ceil_div(p.n_tokens, kGroups);
+      a.tokens = (int32_t)tokens;
+      const int64_t need = ceil_div(p.n_tokens, tokens);
+      hipLaunchKernelGGL((rotary_kernel<T, N, NEIGHBOURS>), dim3((unsigned)(need < kMaxGrid ? need : kMaxGrid)),
+                         dim3(kThreads), 0, st, a);
+      return hipGetLastError();
+    };
+    using std::integral_constant;
+    auto with = [&](auto neighbours) {
+      // half a vector where that leaves no piece across a row's end, which is
+      // taken element by element
+      const int run = neighbours ? p.rot_dim : a.pairs, rest = p.head_dim - p.rot_dim;
+      const bool half = (run % kWide || rest % kWide) && run % (kWide / 2) == 0 && rest % (kWide / 2) == 0;
+      return half ? go(integral_constant<int, kWide / 2>{}, neighbours) : go(integral_constant<int, kWide>{}, neighbours);
+    };
+    return p.interleaved ? with(std::true_type{}) : with(std::false_type{});
   });
 }
 

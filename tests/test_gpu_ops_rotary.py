@@ -60,6 +60,16 @@ def test_both_directions(tokens, heads, dim, rot, interleaved, dtype):
         _check(got, x, freq, pos, interleaved, 1.25, inverse)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,rot", [(40, 40), (20, 12), (28, 20), (36, 24), (22, 22)])
+def test_heads_that_16_bytes_do_not_divide(dim, rot, interleaved, dtype):
+    freq, _ = pa.rotary_freq(rot, device="cpu")
+    x = _x((301, 5, dim + 3), dtype, dim)
+    got = pa.rotary(x.to(DEV)[..., 1:1 + dim], freq.to(DEV), interleaved=interleaved)["out"]
+    _check(got, x[..., 1:1 + dim], freq, torch.arange(301), interleaved)
+
+
 @pytest.mark.parametrize("at", [0, 65_535, 1_000_003, 2**31 - 40, -(2**31) + 40, 2**31 + 2**20])
 def test_far_positions(at):
     freq, _ = pa.rotary_freq(64, device="cpu")
