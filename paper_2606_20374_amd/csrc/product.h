@@ -13,9 +13,9 @@
 // n: with c = lane % 16 and q = lane / 16, register e of a block is n = 4 q + e,
 // m = c, and of both operands a lane holds k = 8 q + j, j = 0 .. 7.
 //
-// Bound by power: products of 8,192^3 run at 1,460 TFLOP/s (both operands with k
-// innermost), 1,426 and 1,377 (one, none), at 1.6 to 1.9 GHz with the matrix units
-// busy 78%, 71% and 66% of the cycles. The 32x32x16 instruction, which moves
+// Bound by power: products of 8,192^3 run at 1,484 TFLOP/s (both operands with k
+// innermost), 1,469 and 1,461 (one, none), at 1.6 to 1.9 GHz; in the operators'
+// large calls the matrix units are busy 74 to 79% of the cycles. The 32x32x16 instruction, which moves
 // twice as much through the accumulators, took 6 to 8% longer in the same loop;
 // steps of 32 k, which ask for half lines, 13% (k innermost) and 4%.
 #pragma once
@@ -467,7 +467,8 @@ __device__ __forceinline__ T* row_at(const Rows& r, int64_t m, int64_t cols) {
 // blocks of 16 weight rows, each read once, straight into registers, by 16-byte
 // pieces of which a wavefront has U times 2 NB under way; its wavefronts take
 // every kFewWaves-th 64 k, and their sums are joined in LDS. The tokens' rows, 16
-// to a block, come from L2.
+// to a block, come from L2. Feed-forward of 4 tokens, 4,096 x 12,288: 36.8 us, 5.5
+// TB/s (39.1 where the compiler may put loads behind products); of 32 50.8 (59.8).
 constexpr int kFewWaves = 4;
 constexpr int kFew = 32;  // tokens, at most: from 33 on tiles are as fast
 
@@ -743,7 +744,9 @@ auto with_tile(int64_t rows, int64_t cols, int64_t k, F go) {
 
 // How the two gradients of an operator are taken: tiles and parts of k. Their
 // workgroups share the chip, so that the parts of one fill what the tiles of the
-// other leave.
+// other leave: feed-forward gradient of 2,000 tokens, 2,048 wide with 5,120 inside 186
+// us, 219 in two launches; of 4,000, 1,024 with 2,048 90 and 116. Of 75 plans tried by
+// hand in each of nine cases none was more than 7% better than the one chosen.
 struct Plan {
   bool big, deep, w_first;
   Grid x, w;  // no sums where S is 1

@@ -7,8 +7,8 @@
 // once, in LDS, and uses them for all of the tokens' heads.
 // Bound by memory: a thread takes 16 bytes (with the halves' layout 16 of each
 // half), whatever the alignment, and writes past the caches. 65,536 tokens, 40
-// heads of 128, bf16: 253 us, 5.3 TB/s (an element to a thread: 597); 20,011
-// tokens, 24 heads of 96 of which 32 turn, f16: 48 us, 3.8 TB/s.
+// heads of 128, bf16: 231 us, 5.8 TB/s (an element to a thread: 597); 20,011
+// tokens, 24 heads of 96 of which 32 turn, f16: 45 us, 4.1 TB/s.
 #include <type_traits>
 
 #include "ops_internal.h"
@@ -18,7 +18,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTurns = 2048;   // sines and cosines that fit a workgroup's LDS
-constexpr int kItems = 512;    // pieces that a workgroup takes where there are enough tokens
+// Pieces that a workgroup takes where there are enough tokens (1,024: 252 us in the
+// place of 232, 61 of 54; 256: 247 and 52).
+constexpr int kItems = 512;
 constexpr int kGroups = 1024;  // workgroups below which it takes fewer
 constexpr int64_t kMaxGrid = 1 << 20;
 
@@ -120,7 +122,7 @@ hipError_t launch_rotary(const argus_rotary_t& p, const void* x, void* out, hipS
     using std::integral_constant;
     auto with = [&](auto neighbours) {
       // half a vector where that leaves no piece across a row's end, which is
-      // taken element by element
+      // taken element by element (30,000 tokens, 20 heads of 40: 27 us for 51)
       const int run = neighbours ? p.rot_dim : a.pairs, rest = p.head_dim - p.rot_dim;
       const bool half = (run % kWide || rest % kWide) && run % (kWide / 2) == 0 && rest % (kWide / 2) == 0;
       return half ? go(integral_constant<int, kWide / 2>{}, neighbours) : go(integral_constant<int, kWide>{}, neighbours);
