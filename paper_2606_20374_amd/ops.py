@@ -511,15 +511,16 @@ def gated_ff_bwd(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.
                  u: torch.Tensor, act: str = "silu", out: Optional[dict] = None) -> dict:
     """argus_gated_ff_bwd: dx, dwg and dwu from dh and the forward's x, weights,
     g and u."""
-    n, width, ff = x.shape[0], x.shape[1], wg.shape[0]
-    if out is None:
-        out = alloc_gated_ff_bwd(n, width, ff, x.dtype, x.device)
     da, ds = _row(dh)
     p, xa, ga, ua = _gated_ff(x, wg, wu, act, ds)
-    for t, what in ((dh, "dh"), (g, "g"), (u, "u")):
-        _need(t, (n, ff), x.dtype, "gated_ff_bwd: " + what)
-    for f, shape in (("dx", (n, width)), ("dwg", (ff, width)), ("dwu", (ff, width))):
-        _need(out[f], shape, x.dtype, "gated_ff_bwd: " + f)
+    inner = (x.shape[0], wg.shape[0])
+    for t, what in ((dh, "gated_ff_bwd: dh"), (g, "gated_ff_bwd: g"), (u, "gated_ff_bwd: u")):
+        _need(t, inner, x.dtype, what)
+    if out is None:
+        out = {"dx": x.new_empty(x.shape), "dwg": x.new_empty(wg.shape), "dwu": x.new_empty(wg.shape)}
+    else:
+        for f, shape in (("dx", x.shape), ("dwg", wg.shape), ("dwu", wg.shape)):
+            _need(out[f], shape, x.dtype, "gated_ff_bwd: " + f)
     ws = _space(out, _lib().argus_gated_ff_bwd_workspace(ctypes.byref(p)), x.device)
     _call("argus_gated_ff_bwd", x.device, ctypes.byref(p), da, xa, ga, ua, _ptr(g), _ptr(u), _ptr(out["dx"]),
           _ptr(out["dwg"]), _ptr(out["dwu"]), _ptr(ws), ws.numel())
@@ -578,10 +579,8 @@ def cross_entropy_bwd(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, ls
     """argus_cross_entropy_bwd: dx and dw from the forward's inputs and lse, and
     the gradient dmean [1] of the mean (with n_valid, which divides it) or
     dloss [tokens] of the losses, or both."""
-    n, width = x.shape
-    if out is None:
-        out = alloc_cross_entropy_bwd(n, w.shape[0], width, x.device)
     p, xa, wa = _cross_entropy(x, w, labels, scale, z_loss)
+    n = x.shape[0]
     _need(lse, (n,), torch.float32, "cross_entropy_bwd: lse")
     if n_valid is not None:
         _need(n_valid, (1,), torch.int32, "cross_entropy_bwd: n_valid")
@@ -589,8 +588,11 @@ def cross_entropy_bwd(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, ls
         _need(dmean, (1,), torch.float32, "cross_entropy_bwd: dmean")
     if dloss is not None:
         _need(dloss, (n,), torch.float32, "cross_entropy_bwd: dloss")
-    _need(out["dx"], (n, width), x.dtype, "cross_entropy_bwd: dx")
-    _need(out["dw"], w.shape, x.dtype, "cross_entropy_bwd: dw")
+    if out is None:
+        out = {"dx": x.new_empty(x.shape), "dw": x.new_empty(w.shape), "dev_status": labels.new_empty(1, dtype=torch.int32)}
+    else:
+        _need(out["dx"], x.shape, x.dtype, "cross_entropy_bwd: dx")
+        _need(out["dw"], w.shape, x.dtype, "cross_entropy_bwd: dw")
     ws = _space(out, _lib().argus_cross_entropy_bwd_workspace(ctypes.byref(p)), x.device)
     _call("argus_cross_entropy_bwd", x.device, ctypes.byref(p), xa, wa, _ptr(lse), _ptr(n_valid), _ptr(dmean),
           _ptr(dloss), _ptr(out["dx"]), _ptr(out["dw"]), _ptr(out.get("dev_status")), _ptr(ws), ws.numel())
