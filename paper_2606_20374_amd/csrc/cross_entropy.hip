@@ -575,7 +575,7 @@ bool is_small(const argus_cross_entropy_t& p) {
   return is_few(p) || (p.n_tokens <= 1024 && p.n_tokens * p.n_vocab * p.width <= (int64_t)1 << 32);
 }
 int64_t tiles_n(const argus_cross_entropy_t& p) {
-  return ceil_div(p.n_vocab, is_few(p) ? few_ids(p) : kind_of<true>(p.n_tokens, p.n_vocab, p.width) == kBig ? 256 : 128);
+  return ceil_div(p.n_vocab, is_few(p) ? few_ids(p) : kind_of(p.n_tokens, p.n_vocab, p.width, kLoss) == kBig ? 256 : 128);
 }
 // Ids of a piece: at most 2^27 values of dz where the tokens allow it, and as
 // many in all pieces as tiles allow.
@@ -676,7 +676,7 @@ hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, c
     if (few_ids(p) == 32) T <= 16 ? few(ce_few<1, 2, 4>) : few(ce_few<2, 2, 3>);
     else T <= 16 ? few(ce_few<1, 8, 1>) : few(ce_few<2, 8, 1>);
   } else {
-    with_tile<bf16_t, true>(T, V, W, go);
+    with_tile<bf16_t, true>(T, V, W, false, go);
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   auto join = [&](auto kern, int64_t rows) {
@@ -738,7 +738,7 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
       if (few_ids(p) == 32) e = T <= 16 ? few(ce_dz_few<1, 2, 4>) : few(ce_dz_few<2, 2, 3>);
       else e = T <= 16 ? few(ce_dz_few<1, 8, 1>) : few(ce_dz_few<2, 8, 1>);
     } else {
-      e = with_tile<bf16_t, true>(T, cols, W, go);
+      e = with_tile<bf16_t, true>(T, cols, W, false, go);
     }
     if (e != hipSuccess) return e;
     g = Grad{};

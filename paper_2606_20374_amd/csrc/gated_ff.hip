@@ -165,7 +165,7 @@ hipError_t forward(const argus_gated_ff_t& p, const void* x, const void* wg, con
   };
   if (p.n_tokens <= 16) return few(ff_few<T, 1, 1, 4>, 16);
   if (p.n_tokens <= kFew) return few(ff_few<T, 2, 1, 3>, 16);
-  return with_tile<T, false>(p.n_tokens, 2 * (int64_t)p.ff, p.width, go);
+  return with_tile<T, false>(p.n_tokens, 2 * (int64_t)p.ff, p.width, g != nullptr, go);
 }
 
 template <class T>

@@ -702,26 +702,26 @@ constexpr int kCus = 256;
 enum Kind { kBig, kWide, kMiddle, kSmall, kShort };
 struct KindCost {
   int tm, tn, each;
-  float step[3], ends[2], once;  // us a step with 1, 2, 3 on a CU, a workgroup's ends, and once
+  float step[3], ends[3], once;  // us a step with 1, 2, 3 on a CU, a workgroup's ends, and once
 };
-// LOSS: the cross entropy's, whose tiles take longer to end; big, small and short
-// ones only.
-template <bool LOSS>
-Kind kind_of(int64_t rows, int64_t cols, int64_t k) {
-  constexpr KindCost costs[] = {{256, 256, 1, {1.18f, 0, 0}, {8.5f, 11.0f}, 0},
-                                {128, 256, 1, {0.87f, 0, 0}, {6.0f, 0}, 0},
-                                {192, 128, 2, {0.69f, 1.25f, 0}, {4.0f, 0}, 4.0f},
-                                {128, 128, 2, {0.72f, 1.05f, 0}, {1.0f, 3.5f}, 3.0f},
-                                {64, 128, 3, {0.55f, 0.85f, 1.13f}, {0.0f, 2.0f}, 3.0f}};
+// What a tile ends with: feed-forward's one output or three, or the cross entropy's
+// exponentials, for which there are big, small and short tiles only.
+enum Ends { kOne, kThree, kLoss };
+inline Kind kind_of(int64_t rows, int64_t cols, int64_t k, Ends ends) {
+  constexpr KindCost costs[] = {{256, 256, 1, {1.18f, 0, 0}, {9.0f, 14.5f, 11.0f}, 0},
+                                {128, 256, 1, {0.87f, 0, 0}, {5.0f, 7.0f, 0}, 0},
+                                {192, 128, 2, {0.69f, 1.25f, 0}, {4.0f, 9.0f, 0}, 4.0f},
+                                {128, 128, 2, {0.72f, 1.05f, 0}, {2.0f, 5.5f, 3.5f}, 3.0f},
+                                {64, 128, 3, {0.55f, 0.85f, 1.13f}, {1.0f, 2.8f, 2.0f}, 3.0f}};
   const float steps = (float)ceil_div(k, kStep);
   Kind best = kBig;
   float least = 0;
   for (int i = 0; i < 5; ++i) {
-    if (LOSS && (i == kWide || i == kMiddle)) continue;
+    if (ends == kLoss && (i == kWide || i == kMiddle)) continue;
     const KindCost& c = costs[i];
     const int64_t n = ceil_div(rows, c.tm) * ceil_div(cols, c.tn), rounds = n / (c.each * kCus), rest = n - rounds * c.each * kCus;
-    float t = c.once + (float)rounds * (steps * c.step[c.each - 1] + c.ends[LOSS]);
-    if (rest) t += steps * c.step[ceil_div(rest, kCus) - 1] + c.ends[LOSS];
+    float t = c.once + (float)rounds * (steps * c.step[c.each - 1] + c.ends[ends]);
+    if (rest) t += steps * c.step[ceil_div(rest, kCus) - 1] + c.ends[ends];
     if (i > 0 && t >= least) continue;
     least = t;
     best = (Kind)i;
@@ -730,8 +730,8 @@ Kind kind_of(int64_t rows, int64_t cols, int64_t k) {
 }
 // Calls go with the tile of a kind.
 template <class T, bool LOSS, class F>
-auto with_tile(int64_t rows, int64_t cols, int64_t k, F go) {
-  const Kind kind = kind_of<LOSS>(rows, cols, k);
+auto with_tile(int64_t rows, int64_t cols, int64_t k, bool three, F go) {
+  const Kind kind = kind_of(rows, cols, k, LOSS ? kLoss : three ? kThree : kOne);
   if (kind == kBig) return go(Big<T, true, true>{});
   if constexpr (!LOSS) {
     if (kind == kWide) return go(Wide<T>{});
