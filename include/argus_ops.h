@@ -270,7 +270,8 @@ int argus_rotary(const argus_rotary_t* p, const void* x, void* out, void* stream
  * g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 (ARGUS_GELU_TANH). The
  * products have 32-bit sums, h is made of those and rounded once.
  * Backward, from the rounded g and u: dg = d_h u act'(g), du = d_h act(g),
- * both rounded to dtype as operands; dx = dg wg + du wu, dwg = dg^T x,
+ * both rounded to dtype as operands (in float16 times a power of two that puts
+ * the largest of them below 2^15); dx = dg wg + du wu, dwg = dg^T x,
  * dwu = du^T x. A row of x or d_h that holds a NaN or an infinity reaches its own
  * token's rows and the weights' gradients alone.
  */

@@ -6,6 +6,11 @@
 // du = dh act(g), rounded to x's type as the operands that the matrix
 // instructions take (half a step each), lie side by side in the workspace;
 // dx = [dg | du] [Wg; Wu], [dWg; dWu] = [dg | du]^T x.
+// In float16 a power of two that brings the largest of them below 2^15 is taken
+// out before and put back by the products' ends: the gradient of a mean over
+// some thousand tokens lies where float16 has no digits left, and products of
+// two of its values leave its range. What is within 2^29 of the largest rounds by half
+// a step of its own.
 #include "product.h"
 
 namespace argus {
@@ -115,10 +120,77 @@ __global__ __launch_bounds__(64 * kFewWaves) void ff_few(FfArgs a) {
   }
 }
 
+// dg and du of eight columns of a row.
+template <class T>
+__device__ __forceinline__ void point_of(const T* dh, const T* g, const T* u, int act, float (&dg)[8], float (&du)[8]) {
+  const Vec<T, 8> d = load_vec<8>(dh), gv = load_vec<8>(g), uv = load_vec<8>(u);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float2 f = activation((float)gv.e[j], act);
+    dg[j] = (float)d.e[j] * (float)uv.e[j] * f.y;
+    du[j] = (float)d.e[j] * f.x;
+  }
+}
+
+// Maximum over a workgroup of four wavefronts, in every thread.
+__device__ __forceinline__ float group_max(float v) {
+  __shared__ float tops[4];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+}
+
+constexpr int kMostGroups = 1024;
+struct Range {
+  float* most;    // [groups] largest finite |dg| and |du| of each workgroup of ff_most
+  float* factor;  // [1] what the operands are to be multiplied with
+  int32_t groups;
+};
+
+// The largest finite |dg| and |du|, before they are rounded to float16. They are
+// computed again by ff_point: kept in 32 bits they would be twice as much to
+// write and read as what they are made from.
+template <class T>
+__global__ __launch_bounds__(256) void ff_most(const T* dh, int64_t stride, const T* g, const T* u, Range r, int64_t rows,
+                                               int32_t F, int32_t act) {
+  const int per = F / 8;
+  const int64_t all = rows * per;
+  float top = 0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per;
+    const int c = (int)(i - row * per) * 8;
+    float dg[8], du[8];
+    point_of(dh + row * stride + c, g + row * F + c, u + row * F + c, act, dg, du);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (fabsf(dg[j]) < __builtin_inff()) top = fmaxf(top, fabsf(dg[j]));
+      if (fabsf(du[j]) < __builtin_inff()) top = fmaxf(top, fabsf(du[j]));
+    }
+  }
+  top = group_max(top);
+  if (threadIdx.x == 0) r.most[blockIdx.x] = top;
+}
+
+// 2^n, n = -126 .. 127.
+__device__ __forceinline__ float power_of_two(int n) { return __int_as_float((n + 127) << 23); }
+
 // dg and du of a row, eight columns to a thread: [rows][2][wide], zeros from F on.
 template <class T>
-__global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, const T* g, const T* u, T* to, int64_t rows,
-                                                int32_t F, int32_t wide, int32_t act) {
+__global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, const T* g, const T* u, T* to, Range r,
+                                                int64_t rows, int32_t F, int32_t wide, int32_t act) {
+  float out = 1.0f;
+  if constexpr (std::is_same_v<T, f16_t>) {
+    float top = 0;
+    for (int i = threadIdx.x; i < r.groups; i += 256) top = fmaxf(top, r.most[i]);
+    top = group_max(top);
+    // 2^at <= top < 2^(at + 1), where top is not next to 0: 2^114 is finite as well
+    int at = (__float_as_int(top) >> 23) - 127;
+    at = at < -100 ? -100 : at;
+    out = power_of_two(14 - at);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *r.factor = power_of_two(at - 14);
+  }
   const int per = wide / 8;
   const int64_t all = rows * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
@@ -128,12 +200,12 @@ __global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, con
 #pragma unroll
     for (int j = 0; j < 8; ++j) dg.e[j] = du.e[j] = (T)0.0f;
     if (c < F) {
-      const Vec<T, 8> d = load_vec<8>(dh + row * stride + c), gv = load_vec<8>(g + row * F + c), uv = load_vec<8>(u + row * F + c);
+      float a[8], b[8];
+      point_of(dh + row * stride + c, g + row * F + c, u + row * F + c, act, a, b);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float2 f = activation((float)gv.e[j], act);
-        dg.e[j] = (T)((float)d.e[j] * (float)uv.e[j] * f.y);
-        du.e[j] = (T)((float)d.e[j] * f.x);
+        dg.e[j] = (T)(a[j] * out);
+        du.e[j] = (T)(b[j] * out);
       }
     }
     store_vec<8>(to + row * 2 * wide + c, dg);
@@ -143,6 +215,7 @@ __global__ __launch_bounds__(256) void ff_point(const T* dh, int64_t stride, con
 
 int64_t wide_of(const argus_gated_ff_t& p) { return ceil_div(p.ff, 64) * 64; }
 size_t point_bytes(const argus_gated_ff_t& p) { return align256((size_t)p.n_tokens * 2 * (size_t)wide_of(p) * 2); }
+size_t range_bytes(const argus_gated_ff_t& p) { return p.dtype == ARGUS_F16 ? align256((kMostGroups + 1) * sizeof(float)) : 0; }
 
 Plan plan_of(const argus_gated_ff_t& p) { return plan_grads(p.n_tokens, 2 * wide_of(p), 2 * wide_of(p), p.n_tokens, p.width); }
 size_t sums_of(const argus_gated_ff_t& p, const Plan& plan, const Grid& g) { return g.S > 1 ? sums_bytes(plan, g, p.width) : 0; }
@@ -174,15 +247,25 @@ hipError_t backward(const argus_gated_ff_t& p, const void* dh, const void* x, co
   const int64_t wide = wide_of(p), W = p.width, F = p.ff, N = p.n_tokens;
   const Plan plan = plan_of(p);
   T* point = (T*)ws;
-  float* sums = (float*)((char*)ws + point_bytes(p));
+  float* most = (float*)((char*)ws + point_bytes(p));
+  float* sums = (float*)((char*)most + range_bytes(p));
+  Range range{};
   hipError_t e;
   if (N > 0) {
     const int64_t need = ceil_div(N * (wide / 8), 256);
+    if constexpr (std::is_same_v<T, f16_t>) {
+      range = {most, most + kMostGroups, (int32_t)(need < kMostGroups ? need : kMostGroups)};
+      hipLaunchKernelGGL(ff_most<T>, dim3((unsigned)range.groups), dim3(256), 0, st, (const T*)dh, p.dh_stride, (const T*)g,
+                         (const T*)u, range, N, p.ff, p.act);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     hipLaunchKernelGGL(ff_point<T>, dim3((unsigned)(need < 16384 ? need : 16384)), dim3(256), 0, st, (const T*)dh,
-                       p.dh_stride, (const T*)g, (const T*)u, point, N, p.ff, (int32_t)wide, p.act);
+                       p.dh_stride, (const T*)g, (const T*)u, point, range, N, p.ff, (int32_t)wide, p.act);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   Grad dinput{}, dweights{};
+  dinput.f = dweights.f = range.factor;
+  dinput.scale = dweights.scale = 1.0f;
   dinput.a = {point, N, 2 * wide, 2 * wide};
   dinput.b = {wg, W, F, p.wg_stride};
   dinput.b1 = {wu, W, F, p.wu_stride};
@@ -206,7 +289,7 @@ size_t gated_ff_workspace_bytes(const argus_gated_ff_t&) { return 0; }
 
 size_t gated_ff_bwd_workspace_bytes(const argus_gated_ff_t& p) {
   const Plan plan = plan_of(p);
-  return point_bytes(p) + sums_of(p, plan, plan.x) + sums_of(p, plan, plan.w);
+  return point_bytes(p) + range_bytes(p) + sums_of(p, plan, plan.x) + sums_of(p, plan, plan.w);
 }
 
 hipError_t launch_gated_ff(const argus_gated_ff_t& p, const void* x, const void* wg, const void* wu, void* h, void* g,
