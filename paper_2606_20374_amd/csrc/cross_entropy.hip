@@ -177,9 +177,9 @@ __global__ __launch_bounds__(256) void ce_rows(CeArgs a, IndexArgs o) {
     for (int64_t c = lane * 8; c < a.x.k; c += 512) store_vec<8>(to + c, id >= 0 ? load_vec<8>(from + c) : none);
     if (lane == 0) {
       const float lse = id >= 0 ? o.lse[row] : 0.0f, c = mean + (o.dloss ? o.dloss[row] : 0.0f);
-      // exp(-infinity) for a token that is not learned
+      // a token that is not learned: no label, and a dz of zeros
       a.t.row[row] = id >= 0 ? make_float4(-lse * kLog2e, c, c * (1.0f + 2.0f * a.z_loss * lse), __int_as_float((int32_t)id))
-                             : make_float4(-__builtin_inff(), 0.0f, 0.0f, __int_as_float(-1));
+                             : make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
       a.t.place[row] = id >= 0 ? (int32_t)row : -1;
     }
   }
@@ -486,6 +486,14 @@ __global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64
         for (int e = 0; e < 4; ++e)
           if (label == TT::col_of(j) + 4 * q + e) t.acc[i][j][e] -= f;
     }
+    // not 0 times what its row of zeros gives: an infinite weight makes that NaN
+    if (__any(__float_as_int(rows[i].w) < 0)) {
+#pragma unroll
+      for (int j = 0; j < TT::FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (__float_as_int(rows[i].w) < 0) t.acc[i][j][e] = 0.0f;
+    }
     if (v0 + n0 + TT::TN > a.V) {
 #pragma unroll
       for (int j = 0; j < TT::FN; ++j)
@@ -516,6 +524,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void ce_dz_few(CeArgs a, bf16_t* dz
     const int row = t * 16 + (lane & 15);
     if (t % kFewWaves != wave || row >= count) continue;
     const float4 r = a.t.row[row];
+    const bool learned = __float_as_int(r.w) >= 0;
     const int64_t label = __float_as_int(r.w) - v0;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -525,7 +534,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void ce_dz_few(CeArgs a, bf16_t* dz
       for (int e = 0; e < 4; ++e) {
         float p = r.z * inv * __builtin_amdgcn_exp2f(fmaf(s.acc[b][t][e], sc, r.x));
         if (16 * b + 4 * q + e == label) p -= r.y * inv;
-        o.e[e] = (bf16_t)(c + e < a.V ? p : 0.0f);
+        o.e[e] = (bf16_t)(learned && c + e < a.V ? p : 0.0f);
       }
       if (c < cols) store_vec<4>(dz + row * stride + c, o);
     }
