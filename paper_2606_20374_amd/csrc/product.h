@@ -701,18 +701,18 @@ using Short = Tile<T, 64, 128, 2, 2, true, true, STAGES>;
 constexpr int kCus = 256;
 enum Kind { kBig, kWide, kMiddle, kSmall, kShort };
 struct KindCost {
-  int tm, tn, each;
+  int tm, tn, threads, each;
   float step[3], ends[3], once;  // us a step with 1, 2, 3 on a CU, a workgroup's ends, and once
 };
 // What a tile ends with: feed-forward's one output or three, or the cross entropy's
 // exponentials, for which there are big, small and short tiles only.
 enum Ends { kOne, kThree, kLoss };
 inline Kind kind_of(int64_t rows, int64_t cols, int64_t k, Ends ends) {
-  constexpr KindCost costs[] = {{256, 256, 1, {1.18f, 0, 0}, {9.0f, 14.5f, 11.0f}, 0},
-                                {128, 256, 1, {0.87f, 0, 0}, {5.0f, 7.0f, 0}, 0},
-                                {192, 128, 2, {0.69f, 1.25f, 0}, {4.0f, 9.0f, 0}, 4.0f},
-                                {128, 128, 2, {0.72f, 1.05f, 0}, {2.0f, 5.5f, 3.5f}, 3.0f},
-                                {64, 128, 3, {0.55f, 0.85f, 1.13f}, {1.0f, 2.8f, 2.0f}, 3.0f}};
+  constexpr KindCost costs[] = {{256, 256, 512, 1, {1.18f, 0, 0}, {9.0f, 14.5f, 11.0f}, 0},
+                                {128, 256, 512, 1, {0.87f, 0, 0}, {5.0f, 7.0f, 0}, 0},
+                                {192, 128, 256, 2, {0.69f, 1.25f, 0}, {4.0f, 9.0f, 0}, 4.0f},
+                                {128, 128, 256, 2, {0.72f, 1.05f, 0}, {2.0f, 5.5f, 3.5f}, 3.0f},
+                                {64, 128, 256, 3, {0.55f, 0.85f, 1.13f}, {1.0f, 2.8f, 2.0f}, 3.0f}};
   const float steps = (float)ceil_div(k, kStep);
   Kind best = kBig;
   float least = 0;
@@ -720,6 +720,8 @@ inline Kind kind_of(int64_t rows, int64_t cols, int64_t k, Ends ends) {
     if (ends == kLoss && (i == kWide || i == kMiddle)) continue;
     const KindCost& c = costs[i];
     const int64_t n = ceil_div(rows, c.tm) * ceil_div(cols, c.tn), rounds = n / (c.each * kCus), rest = n - rounds * c.each * kCus;
+    // an axis of a launch takes below 2^32 threads; the biggest tile's are always fewer
+    if (i > 0 && n * c.threads >= (int64_t)1 << 32) continue;
     float t = c.once + (float)rounds * (steps * c.step[c.each - 1] + c.ends[ends]);
     if (rest) t += steps * c.step[ceil_div(rest, kCus) - 1] + c.ends[ends];
     if (i > 0 && t >= least) continue;

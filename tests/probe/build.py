@@ -1,11 +1,12 @@
-"""Build the test probe libraries (libkdemathprobe.so for gfx950, libhashclaimprobe.so with host code only) in-tree."""
+"""Build the test probe libraries (libkdemathprobe.so for gfx950; libhashclaimprobe.so and libproductplanprobe.so with host code only) in-tree."""
 import os
 import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIBS = {"kde_math_probe.hip": os.path.join(HERE, "libkdemathprobe.so"),
-        "hash_claim_probe.hip": os.path.join(HERE, "libhashclaimprobe.so")}
+        "hash_claim_probe.hip": os.path.join(HERE, "libhashclaimprobe.so"),
+        "product_plan_probe.hip": os.path.join(HERE, "libproductplanprobe.so")}
 sys.path.insert(0, os.path.dirname(os.path.dirname(HERE)))
 
 
