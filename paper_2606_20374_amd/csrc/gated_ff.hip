@@ -40,8 +40,10 @@ __device__ __forceinline__ float2 activation(float g, int act) {
     return make_float2(g * cdf, cdf + g * e * 0.39894228f);
   }
   // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)), y = sqrt(2 / pi) (g + 0.044715 g^3)
+  // In the slope s (1 - s) is 0 long before the square leaves 32 bits: 0, not 0 times
+  // infinity.
   const float s = logistic(1.5957691f * (g + 0.044715f * g * g * g));
-  return make_float2(g * s, s + g * s * (1.0f - s) * 1.5957691f * (1.0f + 0.134145f * g * g));
+  return make_float2(g * s, s + g * s * (1.0f - s) * 1.5957691f * (1.0f + 0.134145f * fminf(g * g, 0x1p100f)));
 }
 
 struct FfArgs {
