@@ -20,7 +20,7 @@ using namespace product;
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 // The learned tokens, in order.
 struct Tokens {
@@ -232,11 +232,11 @@ __device__ __forceinline__ void clear_for_join(const CeArgs& a) {
 }
 
 template <class TT>
-__global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, float* own, int mt, int nt) {
+__global__ __launch_bounds__(TT::THREADS) void ce_fwd(CeArgs a, float2* part, float* own, int nt) {
   __shared__ float2 join[TT::WN][TT::TM];
   const int64_t count = count_of(a);
   if (!a.t.index && blockIdx.x == 0 && threadIdx.x == 0) clear_for_join(a);
-  mt = (int)((count + TT::TM - 1) / TT::TM);
+  const int mt = (int)((count + TT::TM - 1) / TT::TM);
   if (blockIdx.x >= (unsigned)mt * nt) return;
   int m, n;
   tile_at(blockIdx.x, mt, nt, m, n);
@@ -451,9 +451,9 @@ __global__ __launch_bounds__(1024) void ce_mean(CeArgs a, const float* loss, flo
 // dz of the ids [v0, v0 + cols) of the vocabulary, `cols` a multiple of 64.
 template <class TT>
 __global__ __launch_bounds__(TT::THREADS) void ce_dz(CeArgs a, bf16_t* dz, int64_t v0, int64_t cols, int64_t stride,
-                                                     int mt, int nt) {
+                                                     int nt) {
   const int64_t count = count_of(a);
-  mt = (int)((count + TT::TM - 1) / TT::TM);
+  const int mt = (int)((count + TT::TM - 1) / TT::TM);
   if (blockIdx.x >= (unsigned)mt * nt) return;
   int m, n;
   tile_at(blockIdx.x, mt, nt, m, n);
@@ -577,9 +577,9 @@ struct Space {
 // Ids that one workgroup of the forward product takes. Few tokens: enough to
 // join a token's sums in a few steps, yet enough workgroups.
 int few_ids(const argus_cross_entropy_t& p) { return p.n_vocab >= 65536 ? 128 : 32; }
-bool is_few(const argus_cross_entropy_t& p) { return p.n_tokens <= kFew && p.n_tokens * p.x_stride < (1 << 29); }
+bool is_few(const argus_cross_entropy_t& p) { return p.n_tokens <= kFew; }
 // Numbering the tokens costs two launches, about 10 us; taking them all costs at
-// most 8 G multiplications, about that.
+// most 4 G multiplications, about that.
 bool is_small(const argus_cross_entropy_t& p) {
   return is_few(p) || (p.n_tokens <= 1024 && p.n_tokens * p.n_vocab * p.width <= (int64_t)1 << 32);
 }
@@ -675,7 +675,7 @@ hipError_t launch_cross_entropy(const argus_cross_entropy_t& p, const void* x, c
   auto go = [&](auto tile) {
     using TT = decltype(tile);
     const int mt = (int)ceil_div(T, TT::TM);
-    hipLaunchKernelGGL(ce_fwd<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, f.part, f.own, mt, nt);
+    hipLaunchKernelGGL(ce_fwd<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, f.part, f.own, nt);
   };
   auto few = [&](auto kern) {
     hipLaunchKernelGGL(kern, dim3((unsigned)nt), dim3(64 * kFewWaves), 0, st, a, f.part, f.own, nt);
@@ -736,7 +736,7 @@ hipError_t launch_cross_entropy_bwd(const argus_cross_entropy_t& p, const void* 
     auto go = [&](auto tile) {
       using TT = decltype(tile);
       const int mt = (int)ceil_div(T, TT::TM), nt = (int)ceil_div(cols, TT::TN);
-      hipLaunchKernelGGL(ce_dz<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, b.dz, v0, cols, b.piece, mt, nt);
+      hipLaunchKernelGGL(ce_dz<TT>, dim3((unsigned)(mt * nt)), dim3(TT::THREADS), 0, st, a, b.dz, v0, cols, b.piece, nt);
       return hipGetLastError();
     };
     auto few = [&](auto kern) {
