@@ -13,7 +13,7 @@
 // bits. C is the largest |c|: with a factor that all tokens share in the
 // operand, dz of most labels, -c, would round by the same part of itself, and
 // the sums by as much (0.0029 of their norm for 0.0023).
-#include "product.h"
+#include "cross_entropy_plan.h"
 
 namespace argus {
 using namespace product;
@@ -574,27 +574,6 @@ struct Space {
   }
 };
 
-// Ids that one workgroup of the forward product takes. Few tokens: enough to
-// join a token's sums in a few steps, yet enough workgroups.
-int few_ids(const argus_cross_entropy_t& p) { return p.n_vocab >= 65536 ? 128 : 32; }
-bool is_few(const argus_cross_entropy_t& p) { return p.n_tokens <= kFew; }
-// Numbering the tokens costs two launches, about 10 us; taking them all costs at
-// most 4 G multiplications, about that.
-bool is_small(const argus_cross_entropy_t& p) {
-  return is_few(p) || (p.n_tokens <= 1024 && p.n_tokens * p.n_vocab * p.width <= (int64_t)1 << 32);
-}
-int64_t tiles_n(const argus_cross_entropy_t& p) {
-  return ceil_div(p.n_vocab, is_few(p) ? few_ids(p) : kind_of(p.n_tokens, p.n_vocab, p.width, kLoss) == kBig ? 256 : 128);
-}
-// Ids of a piece: at most 2^27 values of dz where the tokens allow it, and as
-// many in all pieces as tiles allow.
-int64_t piece_of(const argus_cross_entropy_t& p) {
-  int64_t ids = ((int64_t)1 << 27) / (p.n_tokens > 0 ? p.n_tokens : 1) / 256 * 256;
-  if (ids < 4096) ids = 4096;
-  const int64_t all = ceil_div(p.n_vocab, 64) * 64;
-  return ids < all ? ceil_div(ceil_div(p.n_vocab, ceil_div(p.n_vocab, ids)), 256) * 256 : all;
-}
-
 struct Forward {
   Tokens t;
   float2* part;
@@ -628,7 +607,7 @@ Backward backward_space(const argus_cross_entropy_t& p, void* ws) {
   const size_t T = (size_t)p.n_tokens;
   Backward b{};
   b.piece = piece_of(p);
-  b.plan = plan_grads(p.n_tokens > 0 ? p.n_tokens : 1, b.piece, b.piece, p.n_tokens, p.width);
+  b.plan = plan_of(p);
   b.t.n = s.take<uint32_t>(2);
   b.t.most = s.take<float>(1);
   b.t.index = s.take<int32_t>(T);

@@ -1,9 +1,13 @@
-"""The choice of tiles and parts of the step operators' matrix products (CPU):
-a launch that any size inside the operators' limits can have."""
+"""The choice of tiles, parts and pieces of the step operators' matrix products
+(CPU): a launch that any size inside the operators' limits can have, and that
+the sizes which test each choice on the GPU are still taken that way."""
 import ctypes
+import itertools
 import os
 
 import pytest
+
+from .test_gpu_ops_product_tiles import FF_GRAD, FORWARD, LOSS, LOSS_GRAD
 
 PROBE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "probe", "libproductplanprobe.so")
 
@@ -15,12 +19,13 @@ def _probe():
     L, I64, I32, V = ctypes.CDLL(PROBE), ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p
     L.probe_forward_tile.argtypes, L.probe_forward_tile.restype = [I64, I64, I64, I32, I32, V], None
     L.probe_gradient_plan.argtypes, L.probe_gradient_plan.restype = [I64] * 5 + [V], None
+    L.probe_loss_call.argtypes, L.probe_loss_call.restype = [I64, I32, I32, V], None
     return L
 
 
 def forward_tile(rows, cols, k, loss=False, three=False):
-    """(rows, columns, threads) of a forward product's tile."""
-    out = (ctypes.c_int32 * 3)()
+    """(rows, columns, threads, stages) of a forward product's tile."""
+    out = (ctypes.c_int32 * 4)()
     _probe().probe_forward_tile(rows, cols, k, loss, three, out)
     return tuple(out)
 
@@ -44,7 +49,7 @@ def test_forward_launches(tokens, k):
             if tokens * cols >= 2**38 if loss else cols > 2**18:
                 continue
             for three in (False,) if loss else (False, True):
-                tm, tn, threads = forward_tile(tokens, cols, k, loss, three)
+                tm, tn, threads, _ = forward_tile(tokens, cols, k, loss, three)
                 assert -(-tokens // tm) * -(-cols // tn) * threads <= MOST, (cols, loss, three)
 
 
@@ -61,3 +66,43 @@ def test_gradient_launches(tokens, width):
             # joins of parts: eight sums to a thread
             assert sx == 1 or tokens * width // 8 <= MOST
             assert sw == 1 or 2 * wide * width // 8 <= MOST
+
+
+def _tile(tm, tn, threads, stages):
+    return tm, tn, stages
+
+
+def _feed_forward_plan(T, W, F):
+    wide = -(-F // 64) * 64
+    tile, deep, sx, sw, _, _ = gradient_plan(T, 2 * wide, 2 * wide, T, W)
+    return tile, deep, sx > 1, sw > 1
+
+
+def _loss_plan(T, V, W):
+    out = (ctypes.c_int64 * 3)()
+    _probe().probe_loss_call(T, V, W, out)
+    few, small, ids = out
+    tile, deep, sx, sw, _, _ = gradient_plan(T, ids, ids, T, W)
+    assert not few
+    return not small, -(-V // ids), tile, deep, sx > 1, sw > 1
+
+
+def test_the_tested_sizes_take_every_tile():
+    assert {c: _tile(*forward_tile(c[0], 2 * c[2], c[1], three=c[3])) for c in FORWARD} == FORWARD
+    assert {c: _tile(*forward_tile(*c, loss=True)) for c in LOSS} == LOSS
+    tiles = {(64, 128, 4), (64, 128, 2), (128, 128, 2), (128, 256, 2), (192, 128, 2), (256, 256, 2)}
+    for three in (False, True):
+        assert {t for c, t in FORWARD.items() if c[3] == three} == tiles
+    assert set(LOSS.values()) == tiles - {(128, 256, 2), (192, 128, 2)}
+
+
+def test_the_tested_sizes_take_all_parts_and_pieces():
+    assert {c: _feed_forward_plan(*c) for c in FF_GRAD} == FF_GRAD
+    assert {c: _loss_plan(*c) for c in LOSS_GRAD} == LOSS_GRAD
+    tiles, either = [(128, True), (128, False), (256, False)], [False, True]
+    assert set(FF_GRAD.values()) == {(*t, x, w) for t, x, w in itertools.product(tiles, either, either)}
+    # numbered tokens: one piece in every way, several but for two that no size was found for
+    one = {p[2:] for p in LOSS_GRAD.values() if p[0] and p[1] == 1}
+    more = {p[2:] for p in LOSS_GRAD.values() if p[0] and p[1] > 1}
+    assert one == set(FF_GRAD.values())
+    assert more == one - {(128, True, False, False), (128, True, True, True)}
