@@ -9,7 +9,7 @@
 // In float16 a power of two that brings the largest of them below 2^15 is taken
 // out before and put back by the products' ends: the gradient of a mean over
 // some thousand tokens lies where float16 has no digits left, and products of
-// two of its values leave its range. What is within 2^29 of the largest rounds by half
+// two of its values leave its range. What is within 2^28 of the largest rounds by half
 // a step of its own.
 #include "product.h"
 
@@ -152,8 +152,9 @@ struct Range {
 };
 
 // The largest finite |dg| and |du|, before they are rounded to float16. They are
-// computed again by ff_point: kept in 32 bits they would be twice as much to
-// write and read as what they are made from.
+// computed again by ff_point: kept in 32 bits they would be more to write and
+// read than what they are made from. Bound by memory: 16,384 tokens of 12,288 231 us,
+// 5.2 TB/s; 999 of 2,720 5.4 us.
 template <class T>
 __global__ __launch_bounds__(256) void ff_most(const T* dh, int64_t stride, const T* g, const T* u, Range r, int64_t rows,
                                                int32_t F, int32_t act) {

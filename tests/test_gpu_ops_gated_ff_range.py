@@ -2,7 +2,7 @@
 of a mean loss, far below 2^-14, and products above 65,504.
 
 Tolerances. dg and du round by UNIT of themselves as long as they lie within
-2^29 of the largest of them; below, by half of float16's last step, which is
+2^28 of the largest of them; below, by half of float16's last step, which is
 2^-39 of the largest. Sums, activations and outputs as in the other tests of
 these operators; an output below 2^-14 rounds by 2^-25 at most. In norm two
 roundings that are independent and spread evenly are off by sqrt(2 / 3) UNIT at
